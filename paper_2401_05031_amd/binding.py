@@ -18,6 +18,9 @@ OTAS_PROMPT_REPLACE, OTAS_PROMPT_GROW = 1, 2
 OTAS_STATIC_MERGE_MAX_ROWS, OTAS_STATIC_MERGE_MAX_QUERIES = 65536, 1024
 OTAS_LINEAR_KERNELS = 11
 OTAS_CLOCK_PROBE_MAX_SAMPLES = 65536
+OTAS_ROTARY_HALF, OTAS_ROTARY_INTERLEAVED = 0, 1
+OTAS_ROTARY_PLAIN, OTAS_ROTARY_LINEAR, OTAS_ROTARY_BASE, OTAS_ROTARY_BY_PARTS = 0, 1, 2, 3
+OTAS_DECODE_ARGUMENTS, OTAS_MAX_LONG_SEQ, OTAS_MAX_TREE_NODES = 960, 1048576, 64
 _WEIGHT_FIELDS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_proj", "b_proj",
                   "ln2_g", "ln2_b", "w_fc1", "b_fc1", "w_fc2", "b_fc2")
 
@@ -44,6 +47,21 @@ class _LayerWeights(C.Structure):
 class _SchedParams(C.Structure):
     _fields_ = [("delta", C.c_double), ("eta", C.c_double), ("mu", C.c_double), ("kappa", C.c_double),
                 ("epsilon", C.c_int32), ("beta", C.c_int32)]
+
+
+class _RotaryDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("inverse", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("original_length", C.c_double), ("fast_turns", C.c_double),
+                ("slow_turns", C.c_double), ("magnitude", C.c_double)]
+
+
+class _ScoreDesc(C.Structure):
+    _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p)]
+
+
+class _KVCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("positions", C.c_void_p), ("mass", C.c_void_p),
+                ("slots", C.c_int32), ("kv_heads", C.c_int32), ("capacity", C.c_int32)]
 
 
 OTAS_GAMMA_SKIP, OTAS_GAMMA_UNDECIDED = -1, -2
@@ -104,6 +122,14 @@ def load_library():
         "otas_clock_probe_read": (i32, [vp, C.POINTER(C.c_float), i32, _I32P]),
         "otas_splitk_factor": (i32, [vp, C.c_int64, i32, i32, i32]),
         "otas_splitk_room": (i32, [vp, C.c_int64, C.c_int64]),
+        "otas_rotary": (i32, [vp, vp, i64, i32, vp, C.POINTER(_RotaryDesc), vp]),
+        "otas_attention_masked": (i32, [vp, vp, i32, _I32P, i32, i32, _I32P, vp, vp, C.POINTER(_ScoreDesc), vp]),
+        "otas_cache_append": (i32, [vp, C.POINTER(_KVCache), vp, i64, _I32P, _I32P, vp, _I32P, _I32P, i32, _I32P]),
+        "otas_attention_tree_workspace_bytes": (sz, [vp, i32, _I32P, _I32P, i32]),
+        "otas_attention_tree": (i32, [vp, C.POINTER(_KVCache), vp, _I32P, _I32P, vp, _I32P, _I32P, i32, C.POINTER(_ScoreDesc), i32,
+                                      vp, sz, vp]),
+        "otas_cache_evict_workspace_bytes": (sz, [vp, _I32P, _I32P, i32]),
+        "otas_cache_evict": (i32, [vp, C.POINTER(_KVCache), _I32P, _I32P, _I32P, i32, i32, _I32P, vp, sz, _I32P]),
         "otas_sched_create": (i32, [C.POINTER(_SchedParams), i32, _I32P, i32, _F64P, _F64P, i32, _F64P, _I32P,
                                     C.POINTER(vp)]),
         "otas_sched_destroy": (None, [vp]),
@@ -129,6 +155,8 @@ EXPORTED = ("otas_create", "otas_destroy", "otas_schedule", "otas_workspace_byte
             "otas_timing_enable", "otas_timing_kinds", "otas_timing_kind_name", "otas_timing_read",
             "otas_timing_read_launches", "otas_timing_overhead_ms", "otas_set_lanes", "otas_splitk_factor", "otas_splitk_room",
             "otas_clock_probe_start", "otas_clock_probe_read",
+            "otas_rotary", "otas_attention_masked", "otas_cache_append", "otas_attention_tree_workspace_bytes",
+            "otas_attention_tree", "otas_cache_evict_workspace_bytes", "otas_cache_evict",
             "otas_sched_create", "otas_sched_destroy", "otas_sched_rate_table", "otas_sched_add_query", "otas_sched_allocate",
             "otas_sched_num_batches", "otas_sched_batch_info", "otas_sched_batch_queries", "otas_sched_estimate",
             "otas_sched_remove")
@@ -150,6 +178,42 @@ def _i32(values: Sequence[int]):
 
 def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+def _opt_i32(values: Optional[Sequence[int]]):
+    return (None, None) if values is None else _i32(values)
+
+
+class Rotary:
+    """otas_rotary_desc: which elements of a head turn, how fast, and in which order they lie."""
+
+    def __init__(self, rot_dim: int, layout: int = OTAS_ROTARY_HALF, base: float = 10000.0, scaling: int = OTAS_ROTARY_PLAIN,
+                 factor: float = 1.0, original_length: float = 8192.0, fast_turns: float = 32.0, slow_turns: float = 1.0,
+                 magnitude: float = 1.0, inverse: bool = False):
+        self.desc = _RotaryDesc(int(rot_dim), int(layout), int(scaling), 1 if inverse else 0, base, factor, original_length,
+                                fast_turns, slow_turns, magnitude)
+
+
+class Score:
+    """otas_score_desc: scale (0: 1 / sqrt of the head width), cap (0: none), slopes float32 [H] on the GPU or None."""
+
+    def __init__(self, scale: float = 0.0, cap: float = 0.0, slopes=None):
+        self.slopes = slopes
+        self.desc = _ScoreDesc(scale, cap, _ptr(slopes))
+
+
+class KVCache:
+    """otas_kv_cache on tensors: k, v [slots, kv_heads, capacity, head width] of the model's dtype, positions int32 and mass
+    float32 (or None) [slots, capacity]."""
+
+    def __init__(self, k, v, positions, mass=None):
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v must be [slots, kv_heads, capacity, head width] of one type")
+        if tuple(positions.shape) != (k.shape[0], k.shape[2]) or (mass is not None and mass.shape != positions.shape):
+            raise ValueError("positions and mass must be [slots, capacity]")
+        self.k, self.v, self.positions, self.mass = k, v, positions, mass
+        self.slots, self.kv_heads, self.capacity, self.head_width = (int(x) for x in k.shape)
+        self.desc = _KVCache(_ptr(k), _ptr(v), _ptr(positions), _ptr(mass), self.slots, self.kv_heads, self.capacity)
 
 
 def otas_schedule(n0: int, P: int, r: int, n_lead: int, L: int) -> List[int]:
@@ -180,6 +244,7 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream().cuda_stream
         self.stream = stream
+        self.device_index = torch.cuda.current_device()
         _check(self._lib.otas_create(C.byref(self._h), C.byref(desc), arr, C.c_void_p(stream)), "otas_create")
 
     @classmethod
@@ -333,6 +398,142 @@ class Context:
         B = len(offsets) - 1
         oa, op = _i32(offsets)
         _check(self._lib.otas_attention(self._h, _ptr(qkv), _ptr(sizes), op, B, flags, _ptr(o)), "otas_attention")
+
+    # -- a decoder's operators (include/otas_decode.h).  The C side sees addresses alone: what a tensor must be is checked here.
+    def _need(self, name: str, t, shape, dtype) -> None:
+        """t is a contiguous GPU tensor of this device, type and shape (None in the shape: any size), or ValueError."""
+        if t.dtype != dtype or t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)):
+            raise ValueError(f"{name}: want {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+        if not t.is_cuda or t.device.index != self.device_index or not t.is_contiguous():
+            raise ValueError(f"{name}: want a contiguous tensor on GPU {self.device_index}")
+
+    def _need_rows(self, qkv, kv_heads: int, out, width: int) -> int:
+        """T of qkv [T, (H + 2 kv_heads) d_h]; out [T, width]."""
+        W = (self.H + 2 * int(kv_heads)) * (self.D // self.H)
+        self._need("qkv", qkv, (None, W), self.torch_dtype)
+        T = int(qkv.shape[0])
+        self._need("out", out, (T, width or W), self.torch_dtype)
+        return T
+
+    def _need_cache(self, cache) -> None:
+        import torch
+        shape = (cache.slots, cache.kv_heads, cache.capacity, self.D // self.H)
+        self._need("cache.k", cache.k, shape, self.torch_dtype)
+        self._need("cache.v", cache.v, shape, self.torch_dtype)
+        self._need("cache.positions", cache.positions, (cache.slots, cache.capacity), torch.int32)
+        if cache.mass is not None:
+            self._need("cache.mass", cache.mass, (cache.slots, cache.capacity), torch.float32)
+
+    def _need_score(self, score):
+        import torch
+        if score is None:
+            return None
+        if score.slopes is not None:
+            self._need("score.slopes", score.slopes, (self.H,), torch.float32)
+        return C.byref(score.desc)
+
+    def _need_workspace(self, workspace) -> int:
+        import torch
+        self._need("workspace", workspace, (None,), torch.uint8)
+        return workspace.numel()
+
+    @staticmethod
+    def _need_lengths(B: int, **arrays) -> None:
+        for name, a in arrays.items():
+            if a is not None and len(a) != B:
+                raise ValueError(f"{name}: want {B} numbers, got {len(a)}")
+
+    def otas_rotary(self, qkv, kv_heads, positions, rope, out) -> None:
+        """Rotary positions (rope: Rotary) on the query and key heads of packed rows; out may be qkv."""
+        import torch
+        T = self._need_rows(qkv, kv_heads, out, 0)
+        self._need("positions", positions, (T,), torch.int32)
+        _check(self._lib.otas_rotary(self._h, _ptr(qkv), T, int(kv_heads), _ptr(positions), C.byref(rope.desc), _ptr(out)),
+               "otas_rotary")
+
+    def otas_attention_masked(self, qkv, kv_heads, offsets, o, causal=True, prefix=None, documents=None, positions=None,
+                              score=None) -> None:
+        """Attention over packed rows with a causal, prefix and document mask; score: Score."""
+        import torch
+        B = len(offsets) - 1
+        T = self._need_rows(qkv, kv_heads, o, self.D)
+        oa, op = _i32(offsets)
+        pa, pp = _opt_i32(prefix)
+        self._need_lengths(B, prefix=prefix)
+        if int(oa[-1]) != T:
+            raise ValueError(f"offsets end at {int(oa[-1])}, qkv has {T} rows")
+        for name, t in (("documents", documents), ("positions", positions)):
+            if t is not None:
+                self._need(name, t, (T,), torch.int32)
+        _check(self._lib.otas_attention_masked(self._h, _ptr(qkv), int(kv_heads), op, B, 1 if causal else 0, pp, _ptr(documents),
+                                               _ptr(positions), self._need_score(score), _ptr(o)), "otas_attention_masked")
+
+    def otas_cache_append(self, cache, qkv, row_offsets, rows, positions, slots, lengths) -> np.ndarray:
+        """Puts rows (None: all, in order) behind the entries of their queries' slots; returns the new lengths."""
+        import torch
+        B = len(row_offsets) - 1
+        self._need_cache(cache)
+        self._need("qkv", qkv, (None, (self.H + 2 * cache.kv_heads) * (self.D // self.H)), self.torch_dtype)
+        T = int(qkv.shape[0])
+        self._need("positions", positions, (T,), torch.int32)
+        self._need_lengths(B, slots=slots, lengths=lengths)
+        oa, op = _i32(row_offsets)
+        ra, rp = _opt_i32(rows)
+        if rows is not None and len(rows) != int(oa[-1]):
+            raise ValueError(f"row_offsets end at {int(oa[-1])}, there are {len(rows)} rows")
+        sa, sp = _i32(slots)
+        la, lp = _i32(lengths)
+        out = np.zeros(B, dtype=np.int32)
+        _check(self._lib.otas_cache_append(self._h, C.byref(cache.desc), _ptr(qkv), T, op, rp, _ptr(positions), sp, lp, B,
+                                           out.ctypes.data_as(_I32P)), "otas_cache_append")
+        return out
+
+    def otas_attention_tree_workspace_bytes(self, kv_heads, offsets, lengths) -> int:
+        oa, op = _i32(offsets)
+        la, lp = _i32(lengths)
+        self._need_lengths(len(offsets) - 1, lengths=lengths)
+        return int(self._lib.otas_attention_tree_workspace_bytes(self._h, int(kv_heads), op, lp, len(offsets) - 1))
+
+    def otas_attention_tree(self, cache, qkv, offsets, parents, positions, slots, lengths, workspace, o, score=None,
+                            add_mass=False) -> None:
+        """Attention of drafted nodes (parents None: chains) over their queries' cache slots and their own ancestors."""
+        import torch
+        B = len(offsets) - 1
+        self._need_cache(cache)
+        T = self._need_rows(qkv, cache.kv_heads, o, self.D)
+        if positions is not None:
+            self._need("positions", positions, (T,), torch.int32)
+        self._need_lengths(B, slots=slots, lengths=lengths)
+        self._need_lengths(T, parents=parents)
+        oa, op = _i32(offsets)
+        if int(oa[-1]) != T:
+            raise ValueError(f"offsets end at {int(oa[-1])}, qkv has {T} rows")
+        pa, pp = _opt_i32(parents)
+        sa, sp = _i32(slots)
+        la, lp = _i32(lengths)
+        _check(self._lib.otas_attention_tree(self._h, C.byref(cache.desc), _ptr(qkv), op, pp, _ptr(positions), sp, lp, B,
+                                             self._need_score(score), 1 if add_mass else 0, _ptr(workspace),
+                                             self._need_workspace(workspace), _ptr(o)), "otas_attention_tree")
+
+    def otas_cache_evict_workspace_bytes(self, lengths, keep) -> int:
+        la, lp = _i32(lengths)
+        ka, kp = _i32(keep)
+        self._need_lengths(len(lengths), keep=keep)
+        return int(self._lib.otas_cache_evict_workspace_bytes(self._h, lp, kp, len(lengths)))
+
+    def otas_cache_evict(self, cache, slots, lengths, keep, workspace, lead=0, recent_from=None) -> np.ndarray:
+        """Cuts every query's slot down to its keep entries of most mass; returns the new lengths."""
+        B = len(slots)
+        self._need_cache(cache)
+        self._need_lengths(B, lengths=lengths, keep=keep, recent_from=recent_from)
+        sa, sp = _i32(slots)
+        la, lp = _i32(lengths)
+        ka, kp = _i32(keep)
+        ra, rp = _opt_i32(recent_from)
+        out = np.zeros(B, dtype=np.int32)
+        _check(self._lib.otas_cache_evict(self._h, C.byref(cache.desc), sp, lp, kp, B, int(lead), rp, _ptr(workspace),
+                                          self._need_workspace(workspace), out.ctypes.data_as(_I32P)), "otas_cache_evict")
+        return out
 
     def otas_timing_enable(self, on: bool) -> None:
         _check(self._lib.otas_timing_enable(self._h, 1 if on else 0), "otas_timing_enable")

@@ -1,0 +1,68 @@
+// What the fp32 and the bf16 attention of the decoder's operators share: which keys a row sees, how products become logits, the
+// lines of a tree of drafts.
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+#include "decode_kernels.h"
+#include "plan_args.h"
+
+namespace otas {
+
+struct RowMask {
+  int row, document, prefix, causal;
+  __device__ bool sees(int j, int doc) const {
+    return (document | doc) >= 0 && (j < prefix || (doc == document && (!causal || j <= row)));
+  }
+};
+
+struct RowScore {
+  float scale, cap, slope;
+  int position;
+  __device__ float logit(float s, int key_position) const {
+    s *= scale;
+    if (cap > 0.f) s = cap * tanhf(s / cap);
+    if (slope != 0.f) s -= slope * fabsf((float)(position - key_position));
+    return s;
+  }
+};
+
+// f(integral_constant<int, tiles of 32 columns>).
+template <typename F>
+inline hipError_t with_tiles(int dh, F f) {
+  switch ((dh + 31) / 32) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 3: return f(std::integral_constant<int, 3>{});
+    case 4: return f(std::integral_constant<int, 4>{});
+  }
+  return hipErrorInvalidValue;
+}
+
+// A 64-bit value of lane `from`.
+__device__ inline uint64_t lane_value(uint64_t v, int from) {
+  const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, from), hi = (uint32_t)__shfl((int)(uint32_t)(v >> 32), from);
+  return (uint64_t)hi << 32 | lo;
+}
+
+// Lane i: the set of nodes that node i sees, itself among them.  Every node knows its parent (a byte each from plan entry `at`
+// on, 255 = none; without has_parents the node before it); in six steps every one adds what its ancestor knows and jumps to the
+// ancestor's ancestor, which doubles the distance each time.  All lanes of the wave take part.
+template <typename P>
+__device__ inline uint64_t tree_lines(const P& plan, int at, int base, int n, bool has_parents, int lane) {
+  if (!has_parents) return lane < 63 ? (2ull << lane) - 1 : ~0ull;
+  int up = 255;
+  if (lane < n) up = (int)((uint32_t)plan[at + ((base + lane) >> 2)] >> (8 * ((base + lane) & 3)) & 255);
+  uint64_t line = 1ull << lane;
+#pragma unroll
+  for (int step = 0; step < 6; ++step) {
+    const int from = up == 255 ? lane : up;
+    const uint64_t theirs = lane_value(line, from);
+    const int next = __shfl(up, from);
+    if (up != 255) line |= theirs;
+    up = up == 255 ? 255 : next;
+  }
+  return line;
+}
+
+}  // namespace otas

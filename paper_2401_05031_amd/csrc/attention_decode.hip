@@ -1,0 +1,448 @@
+// Attention of the decoder's operators with fp32 products (f32 models, and bf16 ones of head widths that the kernels of
+// attention_decode_bf16.hip are not built for):
+//   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = exp(s_ij - max_j s_ij) over the keys j that row i sees,
+// in one pass over the keys with the running maximum and sum of the softmax.  All arithmetic is fp32, on
+// v_mfma_f32_32x32x2_f32 for both products; bf16 operands are widened.
+#include "attention_decode.h"
+
+namespace otas {
+
+// --------------------------------------------------------------------------------------- a wave's 32 rows, key by key
+// Both products are formed transposed, so that a lane owns one row: of a block of 32 keys lane half h holds in
+// accumulator element e the key 8 (e / 4) + 4 h + (e & 3), which the second product takes as k-slot h of its step e
+// straight from registers.
+template <typename T, int DT> struct FloatRows {
+  floatx4 q[4 * DT];
+  floatx16 o[DT];
+  float m, l;   // largest logit so far; sum over the lane's keys
+};
+
+template <typename T, int DT>
+__device__ __forceinline__ void load_heads(floatx4 (&x)[4 * DT], const T* p, int dh, int fk) {   // zero past the head's width
+  const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int g = 0; g < 4 * DT; ++g) x[g] = 8 * g + 4 * fk < dh ? load4<T>(p + 8 * g + 4 * fk) : zero;
+}
+
+template <typename T, int DT>
+__device__ __forceinline__ void rows_begin(FloatRows<T, DT>& r, const T* q, int dh, int fk) {
+  load_heads<T, DT>(r.q, q, dh, fk);
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) r.o[t][e] = 0.f;
+  r.m = -INFINITY;
+  r.l = 0.f;
+}
+
+// keys: k(j), v(j) addresses of key j's head (any j: those past the end give a row that may be read), logit(s, j) of the
+// lane's row (-inf where it does not see j), sees(j), partial(b) whether block b has a pair that does not see each other.
+template <typename T, int DT, class Keys>
+__device__ __forceinline__ void rows_stream(FloatRows<T, DT>& r, const Keys& keys, int dh, int b0, int b1, int step, int fr, int fk) {
+  for (int b = b0; b < b1; b += step) {
+    const int kb = b * 32;
+    floatx4 kf[4 * DT];
+    load_heads<T, DT>(kf, keys.k(kb + fr), dh, fk);
+    float vf[DT][16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const T* pv = keys.v(kb + 8 * (e >> 2) + 4 * fk + (e & 3));
+#pragma unroll
+      for (int t = 0; t < DT; ++t) vf[t][e] = to_float(pv[min(32 * t + fr, dh - 1)]);   // sums past the width are not stored
+    }
+    floatx16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int g = 0; g < 4 * DT; ++g)
+      if (8 * g < dh) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[g][u], r.q[g][u], s, 0, 0, 0);
+      }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = keys.logit(s[e], kb + 8 * (e >> 2) + 4 * fk + (e & 3));
+      mx = fmaxf(mx, s[e]);
+    }
+    const float m_new = fmaxf(r.m, xor32_max(mx));
+    const float m_ref = m_new == -INFINITY ? 0.f : m_new;   // nothing seen so far: all weights 0
+    const float alpha = expf(r.m - m_ref);
+    r.m = m_new;
+    r.l *= alpha;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) r.o[t][e] *= alpha;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = expf(s[e] - m_ref);
+      r.l += s[e];
+    }
+    if (keys.partial(kb)) {   // wave-uniform
+      bool bad = false;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bad |= !__builtin_isfinite(vf[t][e]);
+      if (__any(bad)) {   // a weight of 0 does not keep an infinite value out: add those that are seen, and them alone, by counting
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          floatx16 nan, pos, neg;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) nan[e] = pos[e] = neg[e] = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float sees = keys.sees(kb + 8 * (e >> 2) + 4 * fk + (e & 3)) ? 1.f : 0.f, v = vf[t][e];
+            nan = __builtin_amdgcn_mfma_f32_32x32x2f32(v != v ? 1.f : 0.f, sees, nan, 0, 0, 0);
+            pos = __builtin_amdgcn_mfma_f32_32x32x2f32(v == INFINITY ? 1.f : 0.f, sees, pos, 0, 0, 0);
+            neg = __builtin_amdgcn_mfma_f32_32x32x2f32(v == -INFINITY ? 1.f : 0.f, sees, neg, 0, 0, 0);
+            vf[t][e] = __builtin_isfinite(v) ? v : 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            if (nan[e] > 0.f) r.o[t][e] += NAN;
+            if (pos[e] > 0.f) r.o[t][e] += INFINITY;
+            if (neg[e] > 0.f) r.o[t][e] -= INFINITY;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+      for (int t = 0; t < DT; ++t) r.o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[t][e], s[e], r.o[t], 0, 0, 0);
+  }
+}
+
+// The four waves' shares of 32 rows into one: every thread then has, of row tid / 8, columns 4 (tid & 7) + 32 i, as sums
+// relative to the row's largest logit m, and the weights' sum l.  f(row, column, sums, m, l).
+template <int DT> constexpr size_t float_rows_lds() { return sizeof(float) * (256 + 4 * 32 * (32 * DT + 4)); }
+template <typename T, int DT, class F>
+__device__ __forceinline__ void rows_join(const FloatRows<T, DT>& r, int dh, float* lds, F f) {
+  constexpr int LDO = 32 * DT + 4;
+  float* ml = lds;         // [4][2][32]
+  float* osh = lds + 256;  // [4][32][LDO]
+  const int tid = (int)threadIdx.x, wave = tid >> 6, lane = tid & 63, fr = lane & 31, fk = lane >> 5;
+  const float l_run = xor32_sum(r.l);
+  if (fk == 0) {
+    ml[wave * 64 + fr] = r.m;
+    ml[wave * 64 + 32 + fr] = l_run;
+  }
+  __syncthreads();
+  float m_all = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, ml[w * 64 + fr]);
+  const float k = r.m == -INFINITY ? 0.f : expf(r.m - m_all);
+  float* mine = osh + (wave * 32 + fr) * LDO;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<floatx4*>(mine + 32 * t + 8 * g + 4 * fk) =
+          floatx4{r.o[t][4 * g] * k, r.o[t][4 * g + 1] * k, r.o[t][4 * g + 2] * k, r.o[t][4 * g + 3] * k};
+  __syncthreads();
+  const int row = tid >> 3;
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + row]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    if (ml[w * 64 + row] != -INFINITY) l += ml[w * 64 + 32 + row] * expf(ml[w * 64 + row] - m);
+  for (int d = (tid & 7) * 4; d < dh; d += 32) {
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v += *reinterpret_cast<const floatx4*>(osh + (w * 32 + row) * LDO + d);
+    f(row, d, v, m, l);
+  }
+}
+
+template <typename T> __device__ __forceinline__ void store_row4(T* p, floatx4 v, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  Quad<T> out;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out.x[e] = from_float<T>(l == 0.f ? 0.f : v[e] * inv);
+  *reinterpret_cast<Quad<T>*>(p) = out;
+}
+
+// --------------------------------------------------------------------------------------------------------- packed rows
+template <typename T> struct PackedKeys {
+  const T *kp, *vp;
+  size_t ld;
+  int n;
+  RowMask mask;
+  RowScore score;
+  const int32_t *documents, *positions;   // the query's, or NULL
+  int full;                               // keys below this are seen by every row of the wave
+  __device__ const T* k(int j) const { return kp + (size_t)min(j, n - 1) * ld; }
+  __device__ const T* v(int j) const { return vp + (size_t)min(j, n - 1) * ld; }
+  __device__ bool sees(int j) const { return j < n && mask.sees(j, documents ? documents[j] : 0); }
+  __device__ float logit(float s, int j) const {
+    const int at = min(j, n - 1);
+    return sees(j) ? score.logit(s, positions ? positions[at] : at) : -INFINITY;
+  }
+  __device__ bool partial(int kb) const { return documents || kb + 32 > full; }
+};
+
+// Four waves have 32 rows of a head between them and take the key blocks in turn.
+template <typename T, int DT, typename P>
+__global__ __launch_bounds__(256) void attention_masked_f32_kernel(const T* __restrict__ qkv, P plan, int B, int H, int KV, int dh, int xblks,
+                                                                   ScoreArgs sc, MaskArgs mk, T* __restrict__ o) {
+  extern __shared__ __attribute__((aligned(16))) float f32_lds[];
+  int id = (int)blockIdx.x;
+  const int xblk = xblks - 1 - id % xblks;   // under a causal mask the last rows have the most keys: first
+  id /= xblks;
+  const int h = id % H, q = id / H;
+  const int base = plan[q], n = plan[q + 1] - base, row0 = xblk * 32;
+  if (row0 >= n) return;
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;
+  const int row = min(row0 + fr, n - 1), prefix = plan[B + 1 + q];
+  const size_t ld = (size_t)(H + 2 * KV) * dh;
+  const T* first = qkv + (size_t)base * ld;
+  const int kh = h / (H / KV);
+  const int32_t* docs = mk.documents ? mk.documents + base : nullptr;
+  const int32_t* pos = mk.positions ? mk.positions + base : nullptr;
+  const PackedKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + KV + kh) * dh, ld, n,
+                           RowMask{row, docs ? docs[row] : 0, prefix, mk.causal},
+                           RowScore{sc.scale, sc.cap, sc.slopes ? sc.slopes[h] : 0.f, pos ? pos[row] : row}, docs, pos,
+                           mk.causal ? max(min(row0 + 1, n), prefix) : n};
+  const int end = mk.causal ? max(min(row0 + 32, n), prefix) : n;
+  FloatRows<T, DT> r;
+  rows_begin<T, DT>(r, first + (size_t)row * ld + (size_t)h * dh, dh, fk);
+  rows_stream<T, DT>(r, keys, dh, wave, (end + 31) >> 5, 4, fr, fk);
+  T* out = o + ((size_t)base + row0) * H * dh + (size_t)h * dh;
+  rows_join<T, DT>(r, dh, f32_lds, [&](int i, int d, floatx4 v, float, float l) {
+    if (row0 + i < n) store_row4<T>(out + (size_t)i * H * dh + d, v, l);
+  });
+}
+
+template <typename T>
+static hipError_t attention_masked_f32(const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n,
+                                       int H, int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s) {
+  const int xblks = (max_n + 31) / 32;
+  const int64_t wgs = (int64_t)xblks * H * B;
+  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  return with_plan(plan, count, d_plan, [&](auto p) {
+    typedef decltype(p) P;
+    auto run = [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      auto kern = attention_masked_f32_kernel<T, DT, P>;
+      const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
+      if (e != hipSuccess) return e;
+      kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>((const T*)qkv, p, B, H, KV, dh, xblks, sc, mk, (T*)o);
+      return hipGetLastError();
+    };
+    return with_tiles(dh, run);
+  });
+}
+
+hipError_t launch_attention_masked(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B,
+                                   int max_n, int H, int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s) {
+  if (max_n <= 0) return hipSuccess;
+  return dtype == 0 ? attention_masked_f32<float>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, mk, o, s)
+                    : attention_masked_f32<bf16_t>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, mk, o, s);
+}
+
+// ------------------------------------------------------------------------------------------------ a tree over the cache
+template <typename T> struct CachedKeys {
+  const T *kp, *vp;   // the slot's key head
+  int dh, end;        // entries
+  RowScore score;
+  const int32_t* positions;   // of the slot, read where there are slopes
+  __device__ const T* k(int j) const { return kp + (size_t)min(j, end - 1) * dh; }
+  __device__ const T* v(int j) const { return vp + (size_t)min(j, end - 1) * dh; }
+  __device__ bool sees(int j) const { return j < end; }
+  __device__ float logit(float s, int j) const { return j < end ? score.logit(s, score.slope != 0.f ? positions[min(j, end - 1)] : 0) : -INFINITY; }
+  __device__ bool partial(int kb) const { return kb + 32 > end; }
+};
+template <typename T> struct DraftKeys {
+  const T *kp, *vp;
+  size_t ld;
+  int n;
+  uint64_t line;   // the nodes that the lane's node sees
+  RowScore score;
+  const int32_t* positions;
+  __device__ const T* k(int j) const { return kp + (size_t)min(j, n - 1) * ld; }
+  __device__ const T* v(int j) const { return vp + (size_t)min(j, n - 1) * ld; }
+  __device__ bool sees(int j) const { return j < n && (line >> (j & 63) & 1); }
+  __device__ float logit(float s, int j) const { return sees(j) ? score.logit(s, score.slope != 0.f ? positions[j] : 0) : -INFINITY; }
+  __device__ bool partial(int) const { return true; }
+};
+
+// A workgroup has 32 rows (nodes x heads that share a key head) and one chunk of the cache; the first chunk's also the nodes
+// themselves.  With one chunk the rows are done, else the sums go to the workspace for the join.
+template <typename T, int DT, typename P>
+__global__ __launch_bounds__(256) void attention_tree_f32_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
+                                                                 P plan, int B, bool has_parents, TreeShape shape, ScoreArgs sc,
+                                                                 float* __restrict__ sums, float* __restrict__ tops, float* __restrict__ ends, int64_t TH,
+                                                                 T* __restrict__ o) {
+  extern __shared__ __attribute__((aligned(16))) float f32_lds[];
+  int id = (int)blockIdx.x;
+  const int part = id % shape.parts;
+  id /= shape.parts;
+  const int group = id % shape.groups;
+  id /= shape.groups;
+  const int kh = id % c.KV, q = id / c.KV, dh = c.dh, G = H / c.KV;
+  const int base = plan[q], n = plan[q + 1] - base, len = plan[2 * B + 1 + q], row0 = group * 32;
+  const int64_t slot = plan[B + 1 + q];
+  if (row0 >= n * G || (part > 0 && part * shape.chunk >= len)) return;
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;
+  const int row = min(row0 + fr, n * G - 1), node = row / G, head = kh * G + row % G;
+  const size_t ld = (size_t)(H + 2 * c.KV) * dh;
+  const T* first = qkv + (size_t)base * ld;
+  const RowScore score{sc.scale, sc.cap, sc.slopes ? sc.slopes[head] : 0.f, sc.slopes ? positions[base + node] : 0};
+  FloatRows<T, DT> r;
+  rows_begin<T, DT>(r, first + (size_t)node * ld + (size_t)head * dh, dh, fk);
+  const int begin = part * shape.chunk, end = min(len, begin + shape.chunk);   // chunks are whole blocks
+  if (begin < end) {
+    const T* heads_k = (const T*)c.k + (slot * c.KV + kh) * c.capacity * dh;
+    const T* heads_v = (const T*)c.v + (slot * c.KV + kh) * c.capacity * dh;
+    const CachedKeys<T> keys{heads_k, heads_v, dh, end, score, c.positions + slot * c.capacity};
+    rows_stream<T, DT>(r, keys, dh, (begin >> 5) + wave, (end + 31) >> 5, 4, fr, fk);
+  }
+  if (part == 0) {
+    const uint64_t line = tree_lines(plan, 3 * B + 1, base, n, has_parents, lane);
+    const DraftKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + c.KV + kh) * dh, ld, n, lane_value(line, node), score, positions + base};
+    rows_stream<T, DT>(r, keys, dh, wave, (n + 31) >> 5, 4, fr, fk);
+  }
+  const bool only = len <= shape.chunk;   // the rows' one chunk
+  rows_join<T, DT>(r, dh, f32_lds, [&](int i, int d, floatx4 v, float m, float l) {
+    if (row0 + i >= n * G) return;
+    const int64_t at = (int64_t)(base + (row0 + i) / G) * H + kh * G + (row0 + i) % G;
+    if (only) {
+      store_row4<T>(o + at * dh + d, v, l);
+      if (ends && d == 0) { ends[2 * at] = m; ends[2 * at + 1] = l; }
+    } else {
+      *reinterpret_cast<floatx4*>(sums + ((int64_t)part * TH + at) * dh + d) = v;
+      if (d == 0) { tops[2 * (part * TH + at)] = m; tops[2 * (part * TH + at) + 1] = l; }
+    }
+  });
+}
+
+// The chunks of every row into one, a wave a row.  ends (wanted where the cache's weights are added up): the row's largest logit
+// and sum.
+template <typename T, typename P>
+__global__ __launch_bounds__(256) void attention_tree_join_kernel(P plan, int B, int H, int dh, TreeShape shape, const float* __restrict__ sums,
+                                                                  const float* __restrict__ tops, float* __restrict__ ends, int64_t TH,
+                                                                  T* __restrict__ o) {
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = (int)threadIdx.x & 63;
+  if (at >= TH) return;
+  const int row = (int)(at / H);
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (plan[mid] <= row) lo = mid; else hi = mid;
+  }
+  const int len = plan[2 * B + 1 + lo], parts = (len + shape.chunk - 1) / shape.chunk;
+  if (parts <= 1) return;   // written already
+  float m = -INFINITY, l = 0.f;
+  for (int p = 0; p < parts; ++p) m = fmaxf(m, tops[2 * (p * TH + at)]);
+  float acc[2] = {0.f, 0.f};
+  for (int p = 0; p < parts; ++p) {
+    const float mp = tops[2 * (p * TH + at)];
+    if (mp == -INFINITY) continue;
+    const float k = expf(mp - m);
+    l += k * tops[2 * (p * TH + at) + 1];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (lane + 64 * i < dh) acc[i] += k * sums[(p * TH + at) * dh + lane + 64 * i];
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (lane + 64 * i < dh) o[at * dh + lane + 64 * i] = from_float<T>(l == 0.f ? 0.f : acc[i] * inv);
+  if (ends && lane == 0) { ends[2 * at] = m; ends[2 * at + 1] = l; }
+}
+
+// mass_j += sum over rows and heads of exp(s_ij - m_i) / l_i, with the logits formed again (the weights of one pass are
+// relative to maxima that the next chunk may change, and keeping them all would be 4 bytes a row and key).  A workgroup has 32
+// entries; its waves share out the key heads, whose keys a lane holds while it goes through the rows 32 at a time: here a lane owns
+// a key, so that the sum over rows is one over its own registers.  Waves are added in order.
+template <typename T, int DT, typename P>
+__global__ __launch_bounds__(256) void attention_tree_mass_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
+                                                                  P plan, int B, int xblks, ScoreArgs sc, const float* __restrict__ ends) {
+  __shared__ float part[4][32];
+  const int id = (int)blockIdx.x, q = id / xblks, e0 = (id % xblks) * 32, dh = c.dh, G = H / c.KV;
+  const int base = plan[q], n = plan[q + 1] - base, len = plan[2 * B + 1 + q];
+  const int64_t slot = plan[B + 1 + q];
+  if (e0 >= len || n == 0) return;
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;
+  const size_t ld = (size_t)(H + 2 * c.KV) * dh;
+  const int entry = min(e0 + fr, len - 1);
+  const int kpos = sc.slopes ? c.positions[slot * c.capacity + entry] : 0;
+  float got = 0.f;
+  for (int kh = wave; kh < c.KV; kh += 4) {
+    floatx4 kf[4 * DT];
+    load_heads<T, DT>(kf, (const T*)c.k + ((slot * c.KV + kh) * c.capacity + entry) * dh, dh, fk);
+    for (int row0 = 0; row0 < n * G; row0 += 32) {
+      const int mine = min(row0 + fr, n * G - 1);
+      floatx4 qf[4 * DT];
+      load_heads<T, DT>(qf, qkv + (size_t)(base + mine / G) * ld + (size_t)(kh * G + mine % G) * dh, dh, fk);
+      floatx16 s;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+      for (int g = 0; g < 4 * DT; ++g)
+        if (8 * g < dh) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_32x32x2f32(qf[g][u], kf[g][u], s, 0, 0, 0);
+        }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int r = row0 + 8 * (e >> 2) + 4 * fk + (e & 3);
+        if (r < n * G) {
+          const int node = r / G, head = kh * G + r % G;
+          const int64_t at = (int64_t)(base + node) * H + head;
+          const RowScore score{sc.scale, sc.cap, sc.slopes ? sc.slopes[head] : 0.f, sc.slopes ? positions[base + node] : 0};
+          const float m = ends[2 * at], l = ends[2 * at + 1];
+          if (l != 0.f) got += expf(score.logit(s[e], kpos) - m) / l;
+        }
+      }
+    }
+  }
+  got = xor32_sum(got);
+  if (fk == 0) part[wave][fr] = got;
+  __syncthreads();
+  if (threadIdx.x < 32 && e0 + (int)threadIdx.x < len)
+    c.mass[slot * c.capacity + e0 + threadIdx.x] += (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+}
+
+template <typename T>
+static hipError_t attention_tree_any(const CacheRef& c, const void* qkv, int H, const int32_t* positions, const int32_t* plan, size_t count,
+                                     const int32_t* d_plan, int B, int64_t T_, int max_len, bool has_parents, const ScoreArgs& sc,
+                                     bool add_mass, const TreeShape& shape, float* workspace, void* o, hipStream_t s) {
+  const int64_t TH = T_ * H, wgs = (int64_t)B * c.KV * shape.groups * shape.parts;
+  const int xblks = (max_len + 31) / 32;
+  if (wgs > INT32_MAX || (TH + 3) / 4 > INT32_MAX || (int64_t)B * xblks > INT32_MAX) return hipErrorInvalidValue;
+  float* ends = workspace;
+  float* tops = workspace + 2 * TH;
+  float* sums = tops + 2 * TH * shape.parts;
+  return with_plan(plan, count, d_plan, [&](auto p) {
+    typedef decltype(p) P;
+    return with_tiles(c.dh, [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      auto kern = attention_tree_f32_kernel<T, DT, P>;
+      const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
+      if (e != hipSuccess) return e;
+      kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>(c, (const T*)qkv, H, positions, p, B, has_parents, shape, sc, sums, tops,
+                                                                         add_mass ? ends : nullptr, TH, (T*)o);
+      if (shape.parts > 1)
+        attention_tree_join_kernel<T, P><<<dim3((unsigned)((TH + 3) / 4)), dim3(256), 0, s>>>(p, B, H, c.dh, shape, sums, tops,
+                                                                                             add_mass ? ends : nullptr, TH, (T*)o);
+      if (add_mass && max_len > 0)
+        attention_tree_mass_kernel<T, DT, P><<<dim3((unsigned)(B * xblks)), dim3(256), 0, s>>>(c, (const T*)qkv, H, positions, p, B, xblks, sc, ends);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t launch_attention_tree(int dtype, const CacheRef& c, const void* qkv, int H, const int32_t* positions, const int32_t* plan,
+                                 size_t count, const int32_t* d_plan, int B, int64_t T, int max_len, bool has_parents, const ScoreArgs& sc,
+                                 bool add_mass, const TreeShape& shape, float* workspace, void* o, hipStream_t s) {
+  if (T <= 0) return hipSuccess;
+  return dtype == 0 ? attention_tree_any<float>(c, qkv, H, positions, plan, count, d_plan, B, T, max_len, has_parents, sc, add_mass, shape, workspace, o, s)
+                    : attention_tree_any<bf16_t>(c, qkv, H, positions, plan, count, d_plan, B, T, max_len, has_parents, sc, add_mass, shape, workspace, o, s);
+}
+
+}  // namespace otas

@@ -21,9 +21,11 @@ FAMILIES = {
     "merge_plan": ("merge_plan_kernel", "merge_select_kernel"),
     "layer_norm": ("layer_norm_kernel",),
 }
-# The library's kernels outside those families: the ends of the model, small integer work, the clock and timing probes.
+# The library's kernels outside those families: the ends of the model, small integer work, the clock and timing probes, the
+# decoder's kernels around its cache (its attention counts as attention).
 REST = ("prepend_kernel", "deep_prompt_kernel", "patchify_kernel", "embed_finish_kernel", "task_head_kernel",
-        "fill_i32_kernel", "copy_i32_kernel", "spin_kernel", "clock_probe_kernel")
+        "fill_i32_kernel", "copy_i32_kernel", "spin_kernel", "clock_probe_kernel",
+        "rotary_kernel", "cache_append_kernel", "cache_evict_select_kernel", "cache_evict_move_kernel")
 DEFAULT_OUT = os.path.join(os.path.dirname(os.path.abspath(__file__)), "hbm_traffic.json")
 
 
