@@ -9,6 +9,19 @@
 
 namespace otas {
 
+// A call's host numbers in the kernel's arguments or, where they do not fit, on the device.
+struct PlanAny {
+  int32_t v[kArgInts];
+  const int32_t* p;
+  __device__ int32_t operator[](int i) const { return p ? p[i] : v[i]; }
+};
+inline PlanAny plan_any(const int32_t* plan, size_t count, const int32_t* d_plan) {
+  PlanAny a;
+  a.p = plan_in_args(count) ? nullptr : d_plan;
+  if (!a.p) std::memcpy(a.v, plan, count * sizeof(int32_t));
+  return a;
+}
+
 struct RowMask {
   int row, document, prefix, causal;
   __device__ bool sees(int j, int doc) const {

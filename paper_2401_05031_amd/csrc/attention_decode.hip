@@ -239,6 +239,7 @@ static hipError_t attention_masked_f32(const void* qkv, const int32_t* plan, siz
 hipError_t launch_attention_masked(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B,
                                    int max_n, int H, int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s) {
   if (max_n <= 0) return hipSuccess;
+  if (dtype != 0 && bf16_width(dh)) return launch_attention_masked_bf16(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, mk, o, s);
   return dtype == 0 ? attention_masked_f32<float>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, mk, o, s)
                     : attention_masked_f32<bf16_t>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, mk, o, s);
 }

@@ -1,0 +1,260 @@
+// otas_attention_masked in bf16: four waves have 128 rows of a head and walk the keys that any of them sees in tiles of 64, which
+// travel from global memory into the one LDS buffer while the other is worked on; one barrier a tile.
+#include "attention_tiles.h"
+
+namespace otas {
+
+namespace {
+constexpr int kRows = 128, kKeys = 64;
+
+// Which tiles of 64 keys a workgroup has to look at: one byte each, bit 0: some row may see some key, bit 1: every key has the one
+// document of all rows (or is a prefix key, seen by all).
+__device__ __forceinline__ int next_tile(const unsigned char* kinds, int t, int tiles, int lane) {   // wave-uniform
+  for (; t < tiles; t += 64) {
+    const uint64_t some = __ballot(t + lane < tiles && (kinds[min(t + lane, tiles - 1)] & 1));
+    if (some) return t + __ffsll((unsigned long long)some) - 1;
+  }
+  return tiles;
+}
+}  // namespace
+
+template <int DH> constexpr size_t masked_buffer() { return 2 * TileRows<DH>::bytes(kKeys) + value_slack<DH>() + 512; }
+template <int DH> constexpr size_t masked_lds(int max_n, bool documents) {
+  return 2 * masked_buffer<DH>() + 16 + (documents ? (size_t)(max_n + kKeys - 1) / kKeys + 64 : 0);
+}
+
+template <int DH, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf16_t* __restrict__ qkv, PlanAny plan, int B, int H, int KV, int xblks,
+                                                                       int by_xcd, ScoreArgs sc, MaskArgs mk, bf16_t* __restrict__ o) {
+  typedef TileRows<DH> R;
+  constexpr size_t KB = R::bytes(kKeys), BUF = masked_buffer<DH>();   // keys | values | slack | positions | documents
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  // Work in the order in which it is handed out: the last row blocks of all heads first (under a causal mask they have the most
+  // keys).  Where the heads divide among the eight XCDs each XCD has its own, whose keys then stay in its L2.
+  int id = (int)blockIdx.x, pair, xblk;
+  const int pairs = B * H;
+  if (by_xcd) {
+    const int mine = pairs >> 3, k = id >> 3;
+    pair = (id & 7) * mine + k % mine;
+    xblk = xblks - 1 - k / mine;
+  } else {
+    pair = id % pairs;
+    xblk = xblks - 1 - id / pairs;
+  }
+  const int h = pair % H, q = pair / H;
+  const int base = plan[q], n = plan[q + 1] - base, row0 = xblk * kRows, prefix = plan[B + 1 + q];
+  if (row0 >= n) return;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fk = lane >> 5;
+  const int wrow0 = row0 + wave * 32, row = min(wrow0 + fr, n - 1);
+  const bool active = wrow0 < n;
+  const size_t ld = (size_t)(H + 2 * KV) * DH;
+  const bf16_t* first = qkv + (size_t)base * ld;
+  const int kh = h / (H / KV);
+  const char* kbase = reinterpret_cast<const char*>(first + (size_t)(H + kh) * DH);
+  const char* vbase = reinterpret_cast<const char*>(first + (size_t)(H + KV + kh) * DH);
+  const int32_t* docs = mk.documents ? mk.documents + base : nullptr;
+  const int32_t* pos = BIAS && mk.positions ? mk.positions + base : nullptr;
+  const uint32_t ldb = (uint32_t)(ld * sizeof(bf16_t));
+
+  const int end = mk.causal ? max(min(row0 + kRows, n), prefix) : n, tiles = (end + kKeys - 1) / kKeys;
+  unsigned char* kinds = reinterpret_cast<unsigned char*>(lds + 2 * BUF + 16);
+  const int my_doc = docs ? docs[row] : 0;
+  if (docs) {
+    // the documents of the workgroup's rows: smallest and largest, padding aside
+    int lo = INT32_MAX, hi = -1;
+    bool padded = false;
+    for (int i = lane; i < min(kRows, n - row0); i += 64) {
+      const int d = docs[row0 + i];
+      padded |= d < 0;
+      if (d >= 0) { lo = min(lo, d); hi = max(hi, d); }
+    }
+#pragma unroll
+    for (int x = 32; x; x >>= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
+    const bool one = lo == hi && !__any(padded);
+    for (int t4 = wave * 4; t4 < tiles; t4 += 16) {   // a wave looks at four tiles, 16 lanes each
+      const int t = t4 + (lane >> 4);
+      bool some = false, all = one;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = t * kKeys + i * 16 + (lane & 15), d = j < n ? docs[j] : -1;
+        some |= hi >= 0 && d >= 0 && ((d >= lo && d <= hi) || j < prefix);
+        all &= d >= 0 && (d == lo || j < prefix);
+      }
+      const uint64_t s = __ballot(some), a = __ballot(all);
+      const int sh = lane & 48;
+      if ((lane & 15) == 0 && t < tiles) kinds[t] = (unsigned char)(((s >> sh & 0xFFFF) != 0 ? 1 : 0) | ((a >> sh & 0xFFFF) == 0xFFFF ? 2 : 0));
+    }
+    __syncthreads();
+  }
+
+  TileLoader<DH, kKeys, 4> loader;
+  loader.begin(wave, lane);
+  auto fetch = [&](int t, char* buf) {
+    const size_t at = (size_t)t * kKeys * ldb;
+    const int last = n - 1 - t * kKeys;
+    loader.load(kbase + at, vbase + at, ldb, last, buf, buf + KB);
+    if (BIAS && pos && wave == 0)
+      __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(pos + t * kKeys + min(lane, last)), OTAS_LDS(buf + 2 * KB + value_slack<DH>()), 4, 0, 0);
+    if (docs && wave == 1)
+      __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(docs + t * kKeys + min(lane, last)), OTAS_LDS(buf + 2 * KB + value_slack<DH>() + 256), 4, 0, 0);
+  };
+
+  const Score2 score = Score2::of(sc, BIAS ? sc.slopes[h] : 0.f, BIAS ? (pos ? pos[row] : row) : 0);
+  // A key below `limit` is seen (with documents: if it is a prefix key or of the row's document).
+  const int limit = my_doc < 0 ? 0 : max(mk.causal ? row + 1 : n, prefix);
+  const int own_prefix = my_doc < 0 ? 0 : prefix;
+  // Of the wave: below `sure` every row sees every key, from `none` on no row sees any.
+  const int sure = mk.causal ? max(min(wrow0 + 1, n), prefix) : n, none = mk.causal ? max(min(wrow0 + 32, n), prefix) : n;
+
+  // Of a tile that some row of the workgroup does not see all of, the values that are not finite are taken out and come back
+  // at the end, to the rows that see them.
+  const int wg_sure = mk.causal ? max(row0 + 1, prefix) : n;
+  auto partly = [&](int t) { return (t + 1) * kKeys > wg_sure || (docs && !(kinds[t] & 2)); };
+  int* not_finite = reinterpret_cast<int*>(lds + 2 * BUF);
+  if (tid == 0) *not_finite = 0;
+
+  WaveRows<DH> w;
+  int t = docs ? next_tile(kinds, 0, tiles, lane) : 0;
+  if (t < tiles) fetch(t, lds);
+  w.begin(first + (size_t)row * ld + (size_t)h * DH, fk, sc.scale < 0.f);
+  int side = 0;
+  while (t < tiles) {
+    const int next = docs ? next_tile(kinds, t + 1, tiles, lane) : t + 1;
+    wait_all_barrier();   // tile t is there, and nobody reads the other buffer any more
+    char* buf = lds + (side ? BUF : 0);
+    if (next < tiles) fetch(next, lds + (side ? 0 : BUF));
+    const int kb = t * kKeys;
+    if (partly(t)) {
+      const int* kd = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>() + 256);
+      const bool met = tile_make_finite<DH, kKeys, 256>(buf + KB, tid, [&](int r) { return kb + r < end && (!docs || kd[r] >= 0); });
+      if (met) *not_finite = 1;
+      wait_lds_barrier();
+    }
+    if (active && kb < none) {   // wave-uniform
+      floatx16 s[2];
+      tile_products<DH>(s[0], w, buf, 0, fr, fk);
+      tile_products<DH>(s[1], w, buf, 1, fr, fk);
+      if (CAP) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[b][e] = score.capped(s[b][e]);
+      }
+      if (BIAS) {
+        const int4* kp = reinterpret_cast<const int4*>(buf + 2 * KB + value_slack<DH>());
+        const float near = (float)(score.position - kb - 4 * fk);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            float d[4];
+            if (pos) {
+              const int4 p = kp[b * 8 + 2 * g + fk];
+              d[0] = (float)(score.position - p.x); d[1] = (float)(score.position - p.y);
+              d[2] = (float)(score.position - p.z); d[3] = (float)(score.position - p.w);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) d[e] = near - (float)(32 * b + 8 * g + e);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[b][4 * g + e] = fmaf(-score.slope2, fabsf(d[e]), CAP ? s[b][4 * g + e] : s[b][4 * g + e] * score.scale2);
+          }
+      }
+      const bool whole = kb + kKeys <= sure && (!docs || (kinds[t] & 2));
+      if (!whole && !docs) {
+        const int left = limit - kb - 4 * fk;   // keys of this half that the row sees, from the tile's first on
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bool see = 32 * b + 8 * (e >> 2) + (e & 3) < left;
+            s[b][e] = see ? s[b][e] : -INFINITY;
+          }
+        }
+      } else if (!whole) {
+        const int4* kd = reinterpret_cast<const int4*>(buf + 2 * KB + value_slack<DH>() + 256);
+        const int left = limit - kb - 4 * fk, early = own_prefix - kb - 4 * fk;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int4 d = kd[b * 8 + 2 * g + fk];
+            const int dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int j = 32 * b + 8 * g + e;
+              const bool see = (j < left) & (dd[e] >= 0) & ((j < early) | (dd[e] == my_doc));
+              s[b][4 * g + e] = see ? s[b][4 * g + e] : -INFINITY;
+            }
+          }
+        }
+      }
+      tile_weights<DH, 2>(w, s, CAP || BIAS ? 1.f : score.scale2);
+      tile_sums<DH, 2>(w, s, buf + KB, 0, lane);
+    }
+    t = next;
+    side ^= 1;
+  }
+  wait_lds_barrier();
+  if (*not_finite) {   // workgroup-uniform
+    for (int j = 0; j < end; ++j) {
+      if (!partly(j / kKeys)) continue;
+      const int d = docs ? docs[j] : 0;
+      const bool see = (j < limit) & (d >= 0) & ((j < own_prefix) | (d == my_doc));
+      const bf16_t* v = reinterpret_cast<const bf16_t*>(vbase + (size_t)j * ldb);
+#pragma unroll
+      for (int c = 0; c < WaveRows<DH>::DT; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          if (c * 32 + g * 8 < DH) add_not_finite(w.o[c], g, v + c * 32 + g * 8 + fk * 4, see);
+    }
+  }
+  const float l = xor32_sum(w.l);
+  if (wrow0 + fr >= n) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  bf16_t* orow = o + (size_t)(base + wrow0 + fr) * H * DH + (size_t)h * DH;
+#pragma unroll
+  for (int c = 0; c < WaveRows<DH>::DT; ++c)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = c * 32 + g * 8 + fk * 4;
+      if (d < DH) {
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (bf16_t)(l == 0.f ? 0.f : w.o[c][4 * g + e] * inv);
+        *reinterpret_cast<bf16x4*>(orow + d) = v;
+      }
+    }
+}
+
+hipError_t launch_attention_masked_bf16(const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H,
+                                        int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s) {
+  const int xblks = (max_n + kRows - 1) / kRows;
+  const int64_t wgs = (int64_t)xblks * H * B;
+  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  const PlanAny p = plan_any(plan, count, d_plan);
+  const int by_xcd = (int64_t)B * H % 8 == 0;
+  auto run = [&](auto width, auto cap, auto bias) {
+    constexpr int DH = decltype(width)::value;
+    auto kern = attention_masked_bf16_kernel<DH, decltype(cap)::value, decltype(bias)::value>;
+    const size_t lds = masked_lds<DH>(max_n, mk.documents != nullptr);
+    const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)masked_lds<DH>(1 << 20, true));
+    if (e != hipSuccess) return e;
+    kern<<<dim3((unsigned)wgs), dim3(256), lds, s>>>((const bf16_t*)qkv, p, B, H, KV, xblks, by_xcd, sc, mk, (bf16_t*)o);
+    return hipGetLastError();
+  };
+  auto pick = [&](auto width) {
+    const bool cap = sc.cap > 0.f, bias = sc.slopes != nullptr;
+    if (cap) return bias ? run(width, std::true_type{}, std::true_type{}) : run(width, std::true_type{}, std::false_type{});
+    return bias ? run(width, std::false_type{}, std::true_type{}) : run(width, std::false_type{}, std::false_type{});
+  };
+  switch (dh) {
+    case 64: return pick(std::integral_constant<int, 64>{});
+    case 80: return pick(std::integral_constant<int, 80>{});
+    case 96: return pick(std::integral_constant<int, 96>{});
+    case 128: return pick(std::integral_constant<int, 128>{});
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace otas

@@ -1,0 +1,236 @@
+// bf16 attention over tiles of keys that travel from global memory straight into LDS: what the masked and the tree kernels
+// share.  A wave owns 32 rows; both products are formed transposed (as in attention.hip),
+//   S^T[key, row] = K Q^T,   O^T[d, row] += V^T P^T    (v_mfma_f32_32x32x16_bf16)
+// so that lane (row = lane & 31, half = lane >> 5) holds, of 32 keys, the keys 8 (e / 4) + 4 half + (e & 3), e = 0 .. 15: maxima
+// and sums are over its own registers and one exchange with the other half, and the weights feed the second product as they lie.
+#pragma once
+#include "attention_decode.h"
+
+namespace otas {
+
+#define OTAS_GLOBAL(p) ((const __attribute__((address_space(1))) void*)(p))
+#define OTAS_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+
+// This wave's loads have landed and its LDS reads are back.
+__device__ __forceinline__ void wait_all() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(7 << 4);   // vmcnt(0) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+// LDS reads are back and writes done, of every wave of the workgroup; loads may be under way.
+__device__ __forceinline__ void wait_lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xF | (7 << 4) | (3 << 14));   // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// Loads and LDS, of every wave of the workgroup.
+__device__ __forceinline__ void wait_all_barrier() {
+  wait_all();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Where the 16-byte pieces of a tile's rows lie.  A load instruction fills 64 consecutive pieces of LDS, so that no padding comes
+// for free; in its place pieces change places within a row by a rule on the row.  Keys are read 16 bytes a lane from
+// 16 rows at a time, values 8 bytes a lane by the transposing read, 4 rows x 32 bytes per 16 lanes: the two rules put either
+// on all 64 banks once.  Widths of 80 and 96 have one spare piece a row instead (an odd number of pieces moves the rows apart).
+template <int DH> struct TileRows {
+  static constexpr int PIECES = DH / 8;
+  static constexpr int STRIDE = DH % 64 == 0 ? PIECES : PIECES + 1;   // pieces from row to row
+  static constexpr int ROW_BYTES = STRIDE * 16;
+  static constexpr size_t bytes(int rows) { return (size_t)rows * ROW_BYTES; }
+  static __device__ __forceinline__ int key_piece(int row, int c) { return DH == 128 ? c ^ (row & 15) : DH == 64 ? c ^ ((row >> 1) & 7) : c; }
+  static __device__ __forceinline__ int value_piece(int row, int c) { return DH == 128 ? c ^ 2 * (row & 7) : DH == 64 ? c ^ 2 * ((row >> 1) & 3) : c; }
+};
+
+// Loads of one wave's share (WAVES waves share the work) of ROWS keys and values into LDS.  The same lane loads the same
+// piece of every tile: its place within the row is formed once.
+template <int DH, int ROWS, int WAVES> struct TileLoader {
+  typedef TileRows<DH> R;
+  static constexpr int TOTAL = ROWS * R::STRIDE / 64;                  // load instructions a tile
+  static constexpr int OWN = (TOTAL + WAVES - 1) / WAVES;
+  static_assert(ROWS * R::STRIDE % 64 == 0, "whole instructions");
+  // Where a row's pieces are a power of two, a lane's share of every instruction is the same piece of a row STEP further on.
+  static constexpr bool EVEN = DH % 64 == 0;
+  static constexpr int PLACES = EVEN ? 1 : OWN, STEP = EVEN ? 64 * WAVES / R::STRIDE : 0;
+  int row[PLACES];
+  uint32_t kcol[PLACES], vcol[PLACES];   // bytes within the row
+  int wave;
+  __device__ __forceinline__ void begin(int wave_, int lane) {
+    wave = wave_;
+#pragma unroll
+    for (int i = 0; i < PLACES; ++i) {
+      const int at = (wave + i * WAVES) * 64 + lane, r = at / R::STRIDE, p = at - r * R::STRIDE;
+      row[i] = r;
+      kcol[i] = (uint32_t)min(R::key_piece(r, p), R::PIECES - 1) * 16u;
+      vcol[i] = (uint32_t)min(R::value_piece(r, p), R::PIECES - 1) * 16u;
+    }
+  }
+  // k, v: the tile's first row; ld: bytes from row to row; last: the last row that may be read (later ones repeat it).
+  __device__ __forceinline__ void load(const char* k, const char* v, uint32_t ld, int last, char* lds_k, char* lds_v) const {
+#pragma unroll
+    for (int i = 0; i < OWN; ++i)
+      if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {   // wave-uniform
+        const int x = EVEN ? 0 : i;
+        const uint32_t r = (uint32_t)min(EVEN ? row[0] + i * STEP : row[x], last) * ld;
+        __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(k + (r + kcol[x])), OTAS_LDS(lds_k + (wave + i * WAVES) * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(v + (r + vcol[x])), OTAS_LDS(lds_v + (wave + i * WAVES) * 1024), 16, 0, 0);
+      }
+  }
+};
+
+template <int DH> struct WaveRows {   // a wave's 32 rows
+  static constexpr int KS = DH / 16, DT = (DH + 31) / 32;
+  bf16x8 q[KS];
+  floatx16 o[DT];
+  float m, l;   // the largest logit that the sums are relative to, in units of ln 2; the weights' sum over the lane's keys
+  __device__ __forceinline__ void begin(const bf16_t* qrow, int fk, bool negative) {   // negative: of a negative scale, whose size alone is applied later
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      uint4 u = *reinterpret_cast<const uint4*>(qrow + ks * 16 + fk * 8);
+      if (negative) { u.x ^= 0x80008000u; u.y ^= 0x80008000u; u.z ^= 0x80008000u; u.w ^= 0x80008000u; }
+      __builtin_memcpy(&q[ks], &u, 16);
+    }
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+};
+
+// Products of the rows with keys 32 b .. 32 b + 31 of the tile.
+template <int DH>
+__device__ __forceinline__ void tile_products(floatx16& s, const WaveRows<DH>& w, const char* lds_k, int b, int fr, int fk) {
+  typedef TileRows<DH> R;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < WaveRows<DH>::KS; ++ks) {
+    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds_k + (b * 32 + fr) * R::ROW_BYTES + R::key_piece(fr, 2 * ks + fk) * 16);   // 32 b does not change the rule
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, w.q[ks], s, 0, 0, 0);
+  }
+}
+
+// V^T fragment of columns 32 t .. 32 t + 31 and keys 16 kk .. 16 kk + 15 of the tile (transposing reads: in every 16 lanes lane
+// s points at V[k0 + s / 4][4 (s & 3) ..] and lane i receives V[k0 .. k0 + 3][i]).
+template <int DH>
+__device__ __forceinline__ short8_t tile_values(const char* lds_v, int kk, int t, int lane) {
+  typedef TileRows<DH> R;
+  const int s16 = lane & 15, row = 4 * (lane >> 5) + (s16 >> 2), c = t * 4 + ((lane >> 4) & 1) * 2 + ((s16 & 3) >> 1);
+  const char* p = lds_v + (kk * 16 + row) * R::ROW_BYTES + R::value_piece(row, c) * 16 + (s16 & 1) * 8;   // 16 kk, 8: the rule's period
+  const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(p));
+  const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(p + 8 * R::ROW_BYTES));
+  return short8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+}
+template <int DH> constexpr int value_slack() { return 64; }   // bytes that the last columns' reads of the last row may run past a tile
+
+__device__ __forceinline__ bf16x8 as_bf16(short8_t v) {
+  bf16x8 f;
+  __builtin_memcpy(&f, &v, 16);
+  return f;
+}
+// o += V^T P^T over NB blocks of 32 keys; s holds the weights.  The weights are rounded to bf16 for the product: 2^-8 of each at
+// most, as much as the output's own rounding; their sum l takes them unrounded.
+template <int DH, int NB>
+__device__ __forceinline__ void tile_sums(WaveRows<DH>& w, const floatx16 (&s)[NB], const char* lds_v, int kk0, int lane) {
+#pragma unroll
+  for (int kk = 0; kk < 2 * NB; ++kk) {
+    bf16x8 pf;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pf[i] = (bf16_t)s[kk >> 1][8 * (kk & 1) + i];
+#pragma unroll
+    for (int t = 0; t < WaveRows<DH>::DT; ++t)
+      w.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(tile_values<DH>(lds_v, kk0 + kk, t, lane)), pf, w.o[t], 0, 0, 0);
+  }
+}
+
+// Values that are not finite, in a tile of which some row does not see some key: a weight of 0 would not keep them out of that
+// row.  All threads of the workgroup go over the tile's values and put 0 in their place; harmful(row) of the tile says whether some row sees
+// that key, and the answer whether any such was met: those are added at the end (add_not_finite).  Barriers before and after are the caller's.
+template <int DH, int ROWS, int THREADS, class F>
+__device__ __forceinline__ bool tile_make_finite(char* lds_v, int tid, F harmful) {
+  typedef TileRows<DH> R;
+  bool met = false;
+#pragma unroll
+  for (int i = 0; i < (ROWS * R::STRIDE + THREADS - 1) / THREADS; ++i) {
+    const int c = i * THREADS + tid;
+    if (ROWS * R::STRIDE % THREADS == 0 || c < ROWS * R::STRIDE) {
+      uint4 u = *reinterpret_cast<const uint4*>(lds_v + c * 16);
+      uint32_t* x = &u.x;
+      uint32_t odd[4];   // ones over the elements whose exponent is all ones, two at a time
+#pragma unroll
+      for (int k = 0; k < 4; ++k) odd[k] = ((((x[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;
+      if (odd[0] | odd[1] | odd[2] | odd[3]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] &= ~odd[k];
+        *reinterpret_cast<uint4*>(lds_v + c * 16) = u;
+        met |= harmful(c / R::STRIDE);
+      }
+    }
+  }
+  return met;
+}
+
+// Four consecutive values v of a key that the lane's row sees: what of them is not finite, added to its sums.
+__device__ __forceinline__ void add_not_finite(floatx16& o, int g, const bf16_t* v, bool sees) {
+  const Quad<bf16_t> x = *reinterpret_cast<const Quad<bf16_t>*>(v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float f = (float)x.x[e];
+    o[4 * g + e] += sees && !__builtin_isfinite(f) ? f : 0.f;
+  }
+}
+
+// Scores in units of ln 2: exp(s - m) is then one v_exp_f32.
+struct Score2 {
+  float scale2;    // scale log2 e; with a cap the factor of the exponent below
+  float cap2;      // cap log2 e
+  float slope2;    // the row's
+  int position;    // the row's
+  static __device__ __forceinline__ Score2 of(const ScoreArgs& sc, float slope, int position) {
+    constexpr float log2e = 1.44269504088896340736f;
+    const float scale = fabsf(sc.scale);   // the sign is in the rows
+    return Score2{sc.cap > 0.f ? 2.f * log2e * (scale / sc.cap) : scale * log2e, sc.cap * log2e, slope * log2e, position};
+  }
+  // cap tanh(s scale / cap) = cap - 2 cap / (1 + exp(2 s scale / cap)): off by 2^-23 cap at most near zero, where the two cancel.
+  __device__ __forceinline__ float capped(float s) const {
+    return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * scale2)), cap2);
+  }
+};
+
+// The tile's logits (times a positive factor; -inf where not seen) into weights, the running maximum and sum moved on.  The sums are
+// rescaled only when a maximum has grown by more than 8 (a weight may be up to 2^8 then: no accuracy is lost in a floating format).
+template <int DH, int NB>
+__device__ __forceinline__ void tile_weights(WaveRows<DH>& w, floatx16 (&s)[NB], float factor) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
+  mx = xor32_max(mx) * factor;
+  if (__any(mx > w.m + 8.f)) {
+    const float m_new = fmaxf(w.m, mx);
+    const float alpha = w.m == m_new ? 1.f : __builtin_amdgcn_exp2f(w.m - m_new);   // equal: also where both are -inf
+    w.m = m_new;
+    w.l *= alpha;
+#pragma unroll
+    for (int t = 0; t < WaveRows<DH>::DT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) w.o[t][e] *= alpha;
+  }
+  const float m = w.m == -INFINITY ? 0.f : w.m;   // nothing seen so far: all weights are 0
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[b][e] = __builtin_amdgcn_exp2f(fmaf(s[b][e], factor, -m));
+      w.l += s[b][e];
+    }
+}
+
+}  // namespace otas

@@ -40,6 +40,10 @@ struct MaskArgs {
 // plan: off [B+1] | prefix [B]
 hipError_t launch_attention_masked(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B,
                                    int max_n, int H, int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s);
+// Head widths of the bf16 kernels.
+inline bool bf16_width(int dh) { return dh == 64 || dh == 80 || dh == 96 || dh == 128; }
+hipError_t launch_attention_masked_bf16(const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H,
+                                        int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s);
 
 // How a call of the tree attention is cut up (pure host).  A workgroup has up to `rows` of the nodes x (H / KV) rows of a key
 // head, and `chunk` of the cache's entries; `parts` = most chunks of a query.
