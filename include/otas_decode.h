@@ -106,11 +106,12 @@ otas_status otas_cache_append(otas_ctx *ctx, const otas_kv_cache *cache, const v
  *   positions dev int32 [T] or NULL, read where score has slopes (then required); within +- 2^29, as the cache's
  *   slot, length host [B].  With add_mass the slots of a call differ from each other (EINVAL)
  *   add_mass != 0: entry j's mass grows by the weights it got, summed over the query's nodes and all heads (cache->mass required)
- *   workspace dev >= otas_attention_tree_workspace_bytes for the same offsets and length, 256-byte aligned
+ *   workspace dev >= otas_attention_tree_workspace_bytes for the same offsets, length and add_mass, 256-byte aligned.  The bytes
+ *   grow with the lengths; with add_mass there may be 4 for every row, head and entry among them
  *   o dev [T, D], no overlap.  A node without a key of weight is zero.   Host numbers: 3 B + 1, with parents T / 4 more.
  * The split of a long cache between workgroups, and with it the last bits of o, depends on the whole call's lengths. */
 size_t otas_attention_tree_workspace_bytes(const otas_ctx *ctx, int32_t kv_heads, const int32_t *offsets, const int32_t *length,
-                                           int32_t B);
+                                           int32_t B, int32_t add_mass);
 otas_status otas_attention_tree(otas_ctx *ctx, const otas_kv_cache *cache, const void *qkv, const int32_t *offsets,
                                 const int32_t *parents, const int32_t *positions, const int32_t *slot, const int32_t *length,
                                 int32_t B, const otas_score_desc *score, int32_t add_mass, void *workspace,

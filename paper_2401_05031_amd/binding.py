@@ -125,7 +125,7 @@ def load_library():
         "otas_rotary": (i32, [vp, vp, i64, i32, vp, C.POINTER(_RotaryDesc), vp]),
         "otas_attention_masked": (i32, [vp, vp, i32, _I32P, i32, i32, _I32P, vp, vp, C.POINTER(_ScoreDesc), vp]),
         "otas_cache_append": (i32, [vp, C.POINTER(_KVCache), vp, i64, _I32P, _I32P, vp, _I32P, _I32P, i32, _I32P]),
-        "otas_attention_tree_workspace_bytes": (sz, [vp, i32, _I32P, _I32P, i32]),
+        "otas_attention_tree_workspace_bytes": (sz, [vp, i32, _I32P, _I32P, i32, i32]),
         "otas_attention_tree": (i32, [vp, C.POINTER(_KVCache), vp, _I32P, _I32P, vp, _I32P, _I32P, i32, C.POINTER(_ScoreDesc), i32,
                                       vp, sz, vp]),
         "otas_cache_evict_workspace_bytes": (sz, [vp, _I32P, _I32P, i32]),
@@ -488,11 +488,12 @@ class Context:
                                            out.ctypes.data_as(_I32P)), "otas_cache_append")
         return out
 
-    def otas_attention_tree_workspace_bytes(self, kv_heads, offsets, lengths) -> int:
+    def otas_attention_tree_workspace_bytes(self, kv_heads, offsets, lengths, add_mass=True) -> int:
         oa, op = _i32(offsets)
         la, lp = _i32(lengths)
         self._need_lengths(len(offsets) - 1, lengths=lengths)
-        return int(self._lib.otas_attention_tree_workspace_bytes(self._h, int(kv_heads), op, lp, len(offsets) - 1))
+        return int(self._lib.otas_attention_tree_workspace_bytes(self._h, int(kv_heads), op, lp, len(offsets) - 1,
+                                                                 1 if add_mass else 0))
 
     def otas_attention_tree(self, cache, qkv, offsets, parents, positions, slots, lengths, workspace, o, score=None,
                             add_mass=False) -> None:

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libotas.so")
 SOURCES = ["api.hip", "elementwise.hip", "gemm.hip", "attention.hip", "merge.hip", "launch_util.hip", "sched.cpp",
-           "decode_api.hip", "rotary.hip", "attention_decode.hip", "attention_masked_bf16.hip", "evict.hip"]
+           "decode_api.hip", "rotary.hip", "attention_decode.hip", "attention_masked_bf16.hip",
+           "attention_tree_bf16.hip", "evict.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]

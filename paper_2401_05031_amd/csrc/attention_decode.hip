@@ -442,6 +442,8 @@ hipError_t launch_attention_tree(int dtype, const CacheRef& c, const void* qkv, 
                                  size_t count, const int32_t* d_plan, int B, int64_t T, int max_len, bool has_parents, const ScoreArgs& sc,
                                  bool add_mass, const TreeShape& shape, float* workspace, void* o, hipStream_t s) {
   if (T <= 0) return hipSuccess;
+  if (dtype != 0 && bf16_width(c.dh))
+    return launch_attention_tree_bf16(c, qkv, H, positions, plan, count, d_plan, B, T, max_len, has_parents, sc, add_mass, shape, workspace, o, s);
   return dtype == 0 ? attention_tree_any<float>(c, qkv, H, positions, plan, count, d_plan, B, T, max_len, has_parents, sc, add_mass, shape, workspace, o, s)
                     : attention_tree_any<bf16_t>(c, qkv, H, positions, plan, count, d_plan, B, T, max_len, has_parents, sc, add_mass, shape, workspace, o, s);
 }

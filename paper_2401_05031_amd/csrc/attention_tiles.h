@@ -176,6 +176,12 @@ __device__ __forceinline__ bool tile_make_finite(char* lds_v, int tid, F harmful
   return met;
 }
 
+// 0 in the place of the tile's values from row `valid` on.
+template <int DH, int ROWS, int THREADS>
+__device__ __forceinline__ void tile_zero_rows(char* lds_v, int tid, int valid) {
+  for (int c = valid * TileRows<DH>::STRIDE + tid; c < ROWS * TileRows<DH>::STRIDE; c += THREADS) *reinterpret_cast<uint4*>(lds_v + c * 16) = uint4{0, 0, 0, 0};
+}
+
 // Four consecutive values v of a key that the lane's row sees: what of them is not finite, added to its sums.
 __device__ __forceinline__ void add_not_finite(floatx16& o, int g, const bf16_t* v, bool sees) {
   const Quad<bf16_t> x = *reinterpret_cast<const Quad<bf16_t>*>(v);

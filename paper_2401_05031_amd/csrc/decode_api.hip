@@ -234,14 +234,19 @@ otas_status otas_cache_append(otas_ctx* c, const otas_kv_cache* cache, const voi
   });
 }
 
-size_t otas_attention_tree_workspace_bytes(const otas_ctx* c, int32_t kv_heads, const int32_t* offsets, const int32_t* length, int32_t B) {
+size_t otas_attention_tree_workspace_bytes(const otas_ctx* c, int32_t kv_heads, const int32_t* offsets, const int32_t* length, int32_t B,
+                                           int32_t add_mass) {
   return guarded_size([&]() -> size_t {
     if (!c || !offsets || !length || B <= 0 || !kv_heads_ok(c, kv_heads) || !offsets_ok(offsets, B)) return 0;
-    for (int q = 0; q < B; ++q)
+    int max_len = 0;
+    for (int q = 0; q < B; ++q) {
       if (length[q] < 0 || length[q] > OTAS_MAX_LONG_SEQ || offsets[q + 1] - offsets[q] > OTAS_MAX_TREE_NODES) return 0;
+      max_len = std::max(max_len, (int)length[q]);
+    }
     const int dh = c->desc.D / c->desc.H;
     const TreeShape t = tree_shape(c->desc.dtype, dh, c->desc.H, kv_heads, offsets, length, B);
-    return align_up(std::max<size_t>(1, tree_workspace_floats(t, offsets[B], c->desc.H, dh)) * sizeof(float), kAlign);
+    const size_t floats = tree_workspace_floats(t, c->desc.dtype, offsets[B], c->desc.H, dh, max_len, add_mass != 0);
+    return align_up(std::max<size_t>(1, floats) * sizeof(float), kAlign);
   });
 }
 
@@ -275,7 +280,7 @@ otas_status otas_attention_tree(otas_ctx* c, const otas_kv_cache* cache, const v
     }
     const int dh = c->desc.D / c->desc.H;
     const TreeShape shape = tree_shape(c->desc.dtype, dh, c->desc.H, cache->kv_heads, offsets, length, B);
-    const size_t floats = tree_workspace_floats(shape, T, c->desc.H, dh);
+    const size_t floats = tree_workspace_floats(shape, c->desc.dtype, T, c->desc.H, dh, max_len, add_mass != 0);
     if (workspace_bytes < floats * sizeof(float)) return OTAS_ENOMEM;
     const size_t in_bytes = qkv_bytes(c, T, cache->kv_heads), out_bytes = rows_bytes(c, T);
     if (overlap(qkv, in_bytes, o, out_bytes) || overlap(workspace, floats * sizeof(float), o, out_bytes) ||

@@ -51,14 +51,15 @@ struct TreeShape {
   int rows, groups, chunk, parts, room;   // room: what the workspace has place for; >= parts, and grows with the lengths
 };
 inline TreeShape tree_shape(int dtype, int dh, int H, int KV, const int32_t* off, const int32_t* length, int B) {
-  (void)dtype; (void)dh;
   TreeShape t{32, 1, 0, 1, 1};
   int most = 0, longest = 0;
   for (int q = 0; q < B; ++q) {
     most = std::max(most, off[q + 1] - off[q]);
     longest = std::max(longest, (int)length[q]);
   }
-  t.groups = std::max(1, (most * (H / KV) + t.rows - 1) / t.rows);
+  const int rows = most * (H / KV);
+  if (dtype != 0 && bf16_width(dh)) t.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  t.groups = std::max(1, (rows + t.rows - 1) / t.rows);
   const int64_t wgs = (int64_t)B * KV * t.groups;
   const int wanted = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / wgs, (longest + 255) / 256));
   t.chunk = std::max(128, ((longest + wanted - 1) / wanted + 127) & ~127);
@@ -66,15 +67,23 @@ inline TreeShape tree_shape(int dtype, int dh, int H, int KV, const int32_t* off
   t.room = wanted;
   return t;
 }
-// Floats of workspace: ends [T H][2] and, where there is room for more than one part, for each largest logits and weight sums
-// [T H][2] and sums [T H][dh].
-inline size_t tree_workspace_floats(const TreeShape& t, int64_t T, int H, int dh) {
-  return (size_t)T * H * ((t.room > 1 ? (size_t)t.room * (dh + 2) : 0) + 2);
+// Floats of workspace: ends [T H][2]; where there is room for more than one part, for each largest logits and weight sums [T H][2]
+// and sums [T H][dh]; where weights are added up over few rows (bf16), logits [T H][stride].
+inline int64_t tree_logit_stride(int max_len) { return (max_len + 3) / 4 * 4; }
+inline size_t tree_logits_at(const TreeShape& t, int64_t T, int H, int dh) {
+  return ((size_t)T * H * ((t.room > 1 ? (size_t)t.room * (dh + 2) : 0) + 2) + 3) / 4 * 4;
+}
+inline size_t tree_workspace_floats(const TreeShape& t, int dtype, int64_t T, int H, int dh, int max_len, bool add_mass) {
+  const bool logits = add_mass && dtype != 0 && bf16_width(dh) && t.rows == 32;
+  return tree_logits_at(t, T, H, dh) + (logits ? (size_t)T * H * tree_logit_stride(max_len) : 0);
 }
 // plan: off [B+1] | slot [B] | length [B] | parents, a byte each (has_parents)
 hipError_t launch_attention_tree(int dtype, const CacheRef& c, const void* qkv, int H, const int32_t* positions, const int32_t* plan,
                                  size_t count, const int32_t* d_plan, int B, int64_t T, int max_len, bool has_parents, const ScoreArgs& sc,
                                  bool add_mass, const TreeShape& shape, float* workspace, void* o, hipStream_t s);
+hipError_t launch_attention_tree_bf16(const CacheRef& c, const void* qkv, int H, const int32_t* positions, const int32_t* plan, size_t count,
+                                      const int32_t* d_plan, int B, int64_t T, int max_len, bool has_parents, const ScoreArgs& sc, bool add_mass,
+                                      const TreeShape& shape, float* workspace, void* o, hipStream_t s);
 
 // plan: slot [B] | length [B] | keep [B] | recent_from [B] | list offset [B].  lists: counts [B], then per query its places
 // and sources (2 x the bound of its moves).

@@ -126,7 +126,7 @@ int main() {
     IS(OTAS_OK, otas_cache_append(c, &no_mass, qkv, 8, roff, rows, pos, slot, len, 3, out));
 
     const int32_t parents[] = {-1, 0, 0, -1, 0, 1, 2, 3}, chain[] = {-1, 0, 1, -1, 0, 1, 2, 3};
-    size_t need = otas_attention_tree_workspace_bytes(c, 2, off, len, 3);
+    size_t need = otas_attention_tree_workspace_bytes(c, 2, off, len, 3, 1);
     CHECK(need > 0 && need % 256 == 0);
     IS(OTAS_OK, otas_attention_tree(c, &k, qkv, off, parents, pos, slot, len, 3, &s, 1, ws, need, o));
     IS(OTAS_OK, otas_attention_tree(c, &k, qkv, off, chain, nullptr, slot, len, 3, nullptr, 0, ws, need, o));
@@ -143,20 +143,22 @@ int main() {
     const int32_t self[] = {0, 0, 0, -1, 0, 1, 2, 3}, low[] = {-2, 0, 0, -1, 0, 1, 2, 3}, later[] = {-1, 0, 0, -1, 2, 1, 2, 3};
     for (const int32_t* p : {self, low, later}) IS(OTAS_EINVAL, otas_attention_tree(c, &k, qkv, off, p, pos, slot, len, 3, &s, 1, ws, need, o));
     const int32_t most[] = {0, 64}, more[] = {0, 65}, one_slot[] = {3}, one_len[] = {50};
-    need = otas_attention_tree_workspace_bytes(c, 2, most, one_len, 1);
+    need = otas_attention_tree_workspace_bytes(c, 2, most, one_len, 1, 1);
     IS(OTAS_OK, otas_attention_tree(c, &k, qkv, most, nullptr, pos, one_slot, one_len, 1, &s, 1, ws, need, o));
     IS(OTAS_EUNSUPPORTED, otas_attention_tree(c, &k, qkv, more, nullptr, pos, one_slot, one_len, 1, &s, 1, ws, (size_t)1 << 34, o));
-    CHECK(otas_attention_tree_workspace_bytes(c, 2, more, one_len, 1) == 0 && otas_attention_tree_workspace_bytes(nullptr, 2, most, one_len, 1) == 0);
+    CHECK(otas_attention_tree_workspace_bytes(c, 2, more, one_len, 1, 0) == 0 && otas_attention_tree_workspace_bytes(nullptr, 2, most, one_len, 1, 1) == 0);
     // a program that keeps one workspace asks for the longest lengths
     for (int B : {1, 5, 40}) {
       std::vector<int32_t> of(B + 1), ls(B);
       for (int q = 0; q <= B; ++q) of[q] = 3 * q;
-      size_t before = 0;
-      for (int l = 0; l < 100000; l = l * 5 / 4 + 1) {
-        std::fill(ls.begin(), ls.end(), l);
-        const size_t n = otas_attention_tree_workspace_bytes(c, 2, of.data(), ls.data(), B);
-        CHECK(n >= before);
-        before = n;
+      for (int mass : {0, 1}) {
+        size_t before = 0;
+        for (int l = 0; l < 100000; l = l * 5 / 4 + 1) {
+          std::fill(ls.begin(), ls.end(), l);
+          const size_t n = otas_attention_tree_workspace_bytes(c, 2, of.data(), ls.data(), B, mass);
+          CHECK(n >= before);
+          before = n;
+        }
       }
     }
 
