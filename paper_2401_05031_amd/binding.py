@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -122,14 +123,14 @@ def load_library():
         "otas_clock_probe_read": (i32, [vp, C.POINTER(C.c_float), i32, _I32P]),
         "otas_splitk_factor": (i32, [vp, C.c_int64, i32, i32, i32]),
         "otas_splitk_room": (i32, [vp, C.c_int64, C.c_int64]),
-        "otas_rotary": (i32, [vp, vp, i64, i32, vp, C.POINTER(_RotaryDesc), vp]),
-        "otas_attention_masked": (i32, [vp, vp, i32, _I32P, i32, i32, _I32P, vp, vp, C.POINTER(_ScoreDesc), vp]),
-        "otas_cache_append": (i32, [vp, C.POINTER(_KVCache), vp, i64, _I32P, _I32P, vp, _I32P, _I32P, i32, _I32P]),
-        "otas_attention_tree_workspace_bytes": (sz, [vp, i32, _I32P, _I32P, i32, i32]),
-        "otas_attention_tree": (i32, [vp, C.POINTER(_KVCache), vp, _I32P, _I32P, vp, _I32P, _I32P, i32, C.POINTER(_ScoreDesc), i32,
-                                      vp, sz, vp]),
-        "otas_cache_evict_workspace_bytes": (sz, [vp, _I32P, _I32P, i32]),
-        "otas_cache_evict": (i32, [vp, C.POINTER(_KVCache), _I32P, _I32P, _I32P, i32, i32, _I32P, vp, sz, _I32P]),
+        # host arrays of the decoder's calls go as addresses (_Ints)
+        "otas_rotary": (i32, [vp, vp, i64, i32, vp, vp, vp]),
+        "otas_attention_masked": (i32, [vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp]),
+        "otas_cache_append": (i32, [vp, vp, vp, i64, vp, vp, vp, vp, vp, i32, vp]),
+        "otas_attention_tree_workspace_bytes": (sz, [vp, i32, vp, vp, i32, i32]),
+        "otas_attention_tree": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, sz, vp]),
+        "otas_cache_evict_workspace_bytes": (sz, [vp, vp, vp, i32]),
+        "otas_cache_evict": (i32, [vp, vp, vp, vp, vp, i32, i32, vp, vp, sz, vp]),
         "otas_sched_create": (i32, [C.POINTER(_SchedParams), i32, _I32P, i32, _F64P, _F64P, i32, _F64P, _I32P,
                                     C.POINTER(vp)]),
         "otas_sched_destroy": (None, [vp]),
@@ -180,8 +181,30 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _opt_i32(values: Optional[Sequence[int]]):
-    return (None, None) if values is None else _i32(values)
+class _Ints:
+    """A host int32 array and its address.  Lists (what a scheduler has at hand) go through array.array: a microsecond less
+    per array than through NumPy, which for calls of a few microseconds on the GPU counts."""
+    __slots__ = ("n", "address", "_hold", "last")
+
+    def __init__(self, values, name: str, n: Optional[int] = None):
+        if values is None:
+            self.n = self.address = self._hold = self.last = None
+            return
+        if isinstance(values, (list, tuple)):
+            a = array("i", values)                 # OverflowError / TypeError for what is no int32
+            self.address = a.buffer_info()[0]
+        else:
+            a = np.asarray(values)
+            if a.dtype.kind not in "iu" or a.ndim != 1:
+                raise ValueError(f"{name}: want a list of integers")
+            if a.size and (a.min() < -2 ** 31 or a.max() >= 2 ** 31):
+                raise OverflowError(f"{name}: not 32-bit integers")
+            a = np.ascontiguousarray(a, dtype=np.int32)
+            self.address = a.ctypes.data
+        self._hold, self.n = a, len(a)
+        if n is not None and self.n != n:
+            raise ValueError(f"{name}: want {n} numbers, got {self.n}")
+        self.last = int(a[-1]) if self.n else None
 
 
 class Rotary:
@@ -192,6 +215,7 @@ class Rotary:
                  magnitude: float = 1.0, inverse: bool = False):
         self.desc = _RotaryDesc(int(rot_dim), int(layout), int(scaling), 1 if inverse else 0, base, factor, original_length,
                                 fast_turns, slow_turns, magnitude)
+        self.address = C.addressof(self.desc)
 
 
 class Score:
@@ -200,20 +224,31 @@ class Score:
     def __init__(self, scale: float = 0.0, cap: float = 0.0, slopes=None):
         self.slopes = slopes
         self.desc = _ScoreDesc(scale, cap, _ptr(slopes))
+        self.address = C.addressof(self.desc)
 
 
 class KVCache:
     """otas_kv_cache on tensors: k, v [slots, kv_heads, capacity, head width] of the model's dtype, positions int32 and mass
-    float32 (or None) [slots, capacity]."""
+    float32 (or None) [slots, capacity]; contiguous, on one GPU."""
 
     def __init__(self, k, v, positions, mass=None):
+        import torch
         if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
             raise ValueError("k and v must be [slots, kv_heads, capacity, head width] of one type")
-        if tuple(positions.shape) != (k.shape[0], k.shape[2]) or (mass is not None and mass.shape != positions.shape):
-            raise ValueError("positions and mass must be [slots, capacity]")
-        self.k, self.v, self.positions, self.mass = k, v, positions, mass
-        self.slots, self.kv_heads, self.capacity, self.head_width = (int(x) for x in k.shape)
-        self.desc = _KVCache(_ptr(k), _ptr(v), _ptr(positions), _ptr(mass), self.slots, self.kv_heads, self.capacity)
+        self.slots, self.kv_heads, self.capacity, self.head_width = k.shape
+        small = (self.slots, self.capacity)
+        if positions.shape != small or positions.dtype != torch.int32:
+            raise ValueError("positions must be int32 [slots, capacity]")
+        if mass is not None and (mass.shape != small or mass.dtype != torch.float32):
+            raise ValueError("mass must be float32 [slots, capacity]")
+        self.device_index = k.get_device()
+        for t in (k, v, positions) if mass is None else (k, v, positions, mass):
+            if t.get_device() != self.device_index or self.device_index < 0 or not t.is_contiguous():
+                raise ValueError("k, v, positions and mass must be contiguous tensors on one GPU")
+        self.k, self.v, self.positions, self.mass, self.dtype = k, v, positions, mass, k.dtype
+        self.desc = _KVCache(k.data_ptr(), v.data_ptr(), positions.data_ptr(), None if mass is None else mass.data_ptr(),
+                             self.slots, self.kv_heads, self.capacity)
+        self.address = C.addressof(self.desc)
 
 
 def otas_schedule(n0: int, P: int, r: int, n_lead: int, L: int) -> List[int]:
@@ -400,140 +435,114 @@ class Context:
         _check(self._lib.otas_attention(self._h, _ptr(qkv), _ptr(sizes), op, B, flags, _ptr(o)), "otas_attention")
 
     # -- a decoder's operators (include/otas_decode.h).  The C side sees addresses alone: what a tensor must be is checked here.
-    def _need(self, name: str, t, shape, dtype) -> None:
-        """t is a contiguous GPU tensor of this device, type and shape (None in the shape: any size), or ValueError."""
-        if t.dtype != dtype or t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)):
-            raise ValueError(f"{name}: want {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-        if not t.is_cuda or t.device.index != self.device_index or not t.is_contiguous():
+    def _need(self, name: str, t, shape, dtype) -> int:
+        """The address of t, a contiguous tensor of this type and shape on this context's GPU; else ValueError."""
+        if t.shape != shape or t.dtype != dtype:
+            raise ValueError(f"{name}: want {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if t.get_device() != self.device_index or not t.is_contiguous():
             raise ValueError(f"{name}: want a contiguous tensor on GPU {self.device_index}")
+        return t.data_ptr()
 
-    def _need_rows(self, qkv, kv_heads: int, out, width: int) -> int:
-        """T of qkv [T, (H + 2 kv_heads) d_h]; out [T, width]."""
-        W = (self.H + 2 * int(kv_heads)) * (self.D // self.H)
-        self._need("qkv", qkv, (None, W), self.torch_dtype)
-        T = int(qkv.shape[0])
-        self._need("out", out, (T, width or W), self.torch_dtype)
-        return T
+    def _need_rows(self, qkv, kv_heads: int) -> Tuple[int, int, int]:
+        """T, the row width and the address of qkv [T, (H + 2 kv_heads) d_h]."""
+        T, W = len(qkv), (self.H + 2 * kv_heads) * (self.D // self.H)
+        return T, W, self._need("qkv", qkv, (T, W), self.torch_dtype)
 
-    def _need_cache(self, cache) -> None:
-        import torch
-        shape = (cache.slots, cache.kv_heads, cache.capacity, self.D // self.H)
-        self._need("cache.k", cache.k, shape, self.torch_dtype)
-        self._need("cache.v", cache.v, shape, self.torch_dtype)
-        self._need("cache.positions", cache.positions, (cache.slots, cache.capacity), torch.int32)
-        if cache.mass is not None:
-            self._need("cache.mass", cache.mass, (cache.slots, cache.capacity), torch.float32)
+    def _need_cache(self, cache) -> int:
+        if cache.dtype != self.torch_dtype or cache.head_width != self.D // self.H or cache.device_index != self.device_index:
+            raise ValueError(f"cache: want {self.torch_dtype}, head width {self.D // self.H} on GPU {self.device_index}, got "
+                             f"{cache.dtype}, {cache.head_width} on GPU {cache.device_index}")
+        return cache.address
 
-    def _need_score(self, score):
+    def _need_score(self, score) -> Optional[int]:
         import torch
         if score is None:
             return None
         if score.slopes is not None:
             self._need("score.slopes", score.slopes, (self.H,), torch.float32)
-        return C.byref(score.desc)
+        return score.address
 
-    def _need_workspace(self, workspace) -> int:
+    def _need_workspace(self, workspace) -> Tuple[int, int]:
         import torch
-        self._need("workspace", workspace, (None,), torch.uint8)
-        return workspace.numel()
-
-    @staticmethod
-    def _need_lengths(B: int, **arrays) -> None:
-        for name, a in arrays.items():
-            if a is not None and len(a) != B:
-                raise ValueError(f"{name}: want {B} numbers, got {len(a)}")
+        n = workspace.numel()
+        return self._need("workspace", workspace, (n,), torch.uint8), n
 
     def otas_rotary(self, qkv, kv_heads, positions, rope, out) -> None:
         """Rotary positions (rope: Rotary) on the query and key heads of packed rows; out may be qkv."""
         import torch
-        T = self._need_rows(qkv, kv_heads, out, 0)
-        self._need("positions", positions, (T,), torch.int32)
-        _check(self._lib.otas_rotary(self._h, _ptr(qkv), T, int(kv_heads), _ptr(positions), C.byref(rope.desc), _ptr(out)),
+        T, W, at = self._need_rows(qkv, kv_heads)
+        to = at if out is qkv else self._need("out", out, (T, W), self.torch_dtype)
+        _check(self._lib.otas_rotary(self._h, at, T, kv_heads, self._need("positions", positions, (T,), torch.int32), rope.address, to),
                "otas_rotary")
 
     def otas_attention_masked(self, qkv, kv_heads, offsets, o, causal=True, prefix=None, documents=None, positions=None,
                               score=None) -> None:
         """Attention over packed rows with a causal, prefix and document mask; score: Score."""
         import torch
-        B = len(offsets) - 1
-        T = self._need_rows(qkv, kv_heads, o, self.D)
-        oa, op = _i32(offsets)
-        pa, pp = _opt_i32(prefix)
-        self._need_lengths(B, prefix=prefix)
-        if int(oa[-1]) != T:
-            raise ValueError(f"offsets end at {int(oa[-1])}, qkv has {T} rows")
-        for name, t in (("documents", documents), ("positions", positions)):
-            if t is not None:
-                self._need(name, t, (T,), torch.int32)
-        _check(self._lib.otas_attention_masked(self._h, _ptr(qkv), int(kv_heads), op, B, 1 if causal else 0, pp, _ptr(documents),
-                                               _ptr(positions), self._need_score(score), _ptr(o)), "otas_attention_masked")
+        T, _, at = self._need_rows(qkv, kv_heads)
+        off = _Ints(offsets, "offsets")
+        pre = _Ints(prefix, "prefix", off.n - 1)
+        if off.last != T:
+            raise ValueError(f"offsets end at {off.last}, qkv has {T} rows")
+        _check(self._lib.otas_attention_masked(
+            self._h, at, kv_heads, off.address, off.n - 1, 1 if causal else 0, pre.address,
+            None if documents is None else self._need("documents", documents, (T,), torch.int32),
+            None if positions is None else self._need("positions", positions, (T,), torch.int32), self._need_score(score),
+            self._need("o", o, (T, self.D), self.torch_dtype)), "otas_attention_masked")
 
     def otas_cache_append(self, cache, qkv, row_offsets, rows, positions, slots, lengths) -> np.ndarray:
         """Puts rows (None: all, in order) behind the entries of their queries' slots; returns the new lengths."""
         import torch
-        B = len(row_offsets) - 1
-        self._need_cache(cache)
-        self._need("qkv", qkv, (None, (self.H + 2 * cache.kv_heads) * (self.D // self.H)), self.torch_dtype)
-        T = int(qkv.shape[0])
-        self._need("positions", positions, (T,), torch.int32)
-        self._need_lengths(B, slots=slots, lengths=lengths)
-        oa, op = _i32(row_offsets)
-        ra, rp = _opt_i32(rows)
-        if rows is not None and len(rows) != int(oa[-1]):
-            raise ValueError(f"row_offsets end at {int(oa[-1])}, there are {len(rows)} rows")
-        sa, sp = _i32(slots)
-        la, lp = _i32(lengths)
-        out = np.zeros(B, dtype=np.int32)
-        _check(self._lib.otas_cache_append(self._h, C.byref(cache.desc), _ptr(qkv), T, op, rp, _ptr(positions), sp, lp, B,
-                                           out.ctypes.data_as(_I32P)), "otas_cache_append")
+        c = self._need_cache(cache)
+        T, _, at = self._need_rows(qkv, cache.kv_heads)
+        off = _Ints(row_offsets, "row_offsets")
+        B = off.n - 1
+        row, slot, length = _Ints(rows, "rows", off.last), _Ints(slots, "slots", B), _Ints(lengths, "lengths", B)
+        out = np.empty(max(B, 0), dtype=np.int32)
+        _check(self._lib.otas_cache_append(self._h, c, at, T, off.address, row.address,
+                                           self._need("positions", positions, (T,), torch.int32), slot.address, length.address, B,
+                                           out.ctypes.data), "otas_cache_append")
         return out
 
     def otas_attention_tree_workspace_bytes(self, kv_heads, offsets, lengths, add_mass=True) -> int:
-        oa, op = _i32(offsets)
-        la, lp = _i32(lengths)
-        self._need_lengths(len(offsets) - 1, lengths=lengths)
-        return int(self._lib.otas_attention_tree_workspace_bytes(self._h, int(kv_heads), op, lp, len(offsets) - 1,
+        off = _Ints(offsets, "offsets")
+        length = _Ints(lengths, "lengths", off.n - 1)
+        return int(self._lib.otas_attention_tree_workspace_bytes(self._h, kv_heads, off.address, length.address, off.n - 1,
                                                                  1 if add_mass else 0))
 
     def otas_attention_tree(self, cache, qkv, offsets, parents, positions, slots, lengths, workspace, o, score=None,
                             add_mass=False) -> None:
         """Attention of drafted nodes (parents None: chains) over their queries' cache slots and their own ancestors."""
         import torch
-        B = len(offsets) - 1
-        self._need_cache(cache)
-        T = self._need_rows(qkv, cache.kv_heads, o, self.D)
-        if positions is not None:
-            self._need("positions", positions, (T,), torch.int32)
-        self._need_lengths(B, slots=slots, lengths=lengths)
-        self._need_lengths(T, parents=parents)
-        oa, op = _i32(offsets)
-        if int(oa[-1]) != T:
-            raise ValueError(f"offsets end at {int(oa[-1])}, qkv has {T} rows")
-        pa, pp = _opt_i32(parents)
-        sa, sp = _i32(slots)
-        la, lp = _i32(lengths)
-        _check(self._lib.otas_attention_tree(self._h, C.byref(cache.desc), _ptr(qkv), op, pp, _ptr(positions), sp, lp, B,
-                                             self._need_score(score), 1 if add_mass else 0, _ptr(workspace),
-                                             self._need_workspace(workspace), _ptr(o)), "otas_attention_tree")
+        c = self._need_cache(cache)
+        T, _, at = self._need_rows(qkv, cache.kv_heads)
+        off = _Ints(offsets, "offsets")
+        B = off.n - 1
+        par, slot, length = _Ints(parents, "parents", T), _Ints(slots, "slots", B), _Ints(lengths, "lengths", B)
+        if off.last != T:
+            raise ValueError(f"offsets end at {off.last}, qkv has {T} rows")
+        ws, room = self._need_workspace(workspace)
+        _check(self._lib.otas_attention_tree(
+            self._h, c, at, off.address, par.address,
+            None if positions is None else self._need("positions", positions, (T,), torch.int32), slot.address, length.address, B,
+            self._need_score(score), 1 if add_mass else 0, ws, room, self._need("o", o, (T, self.D), self.torch_dtype)),
+            "otas_attention_tree")
 
     def otas_cache_evict_workspace_bytes(self, lengths, keep) -> int:
-        la, lp = _i32(lengths)
-        ka, kp = _i32(keep)
-        self._need_lengths(len(lengths), keep=keep)
-        return int(self._lib.otas_cache_evict_workspace_bytes(self._h, lp, kp, len(lengths)))
+        length = _Ints(lengths, "lengths")
+        kept = _Ints(keep, "keep", length.n)
+        return int(self._lib.otas_cache_evict_workspace_bytes(self._h, length.address, kept.address, length.n))
 
     def otas_cache_evict(self, cache, slots, lengths, keep, workspace, lead=0, recent_from=None) -> np.ndarray:
         """Cuts every query's slot down to its keep entries of most mass; returns the new lengths."""
-        B = len(slots)
-        self._need_cache(cache)
-        self._need_lengths(B, lengths=lengths, keep=keep, recent_from=recent_from)
-        sa, sp = _i32(slots)
-        la, lp = _i32(lengths)
-        ka, kp = _i32(keep)
-        ra, rp = _opt_i32(recent_from)
-        out = np.zeros(B, dtype=np.int32)
-        _check(self._lib.otas_cache_evict(self._h, C.byref(cache.desc), sp, lp, kp, B, int(lead), rp, _ptr(workspace),
-                                          self._need_workspace(workspace), out.ctypes.data_as(_I32P)), "otas_cache_evict")
+        c = self._need_cache(cache)
+        slot = _Ints(slots, "slots")
+        B = slot.n
+        length, kept, recent = _Ints(lengths, "lengths", B), _Ints(keep, "keep", B), _Ints(recent_from, "recent_from", B)
+        ws, room = self._need_workspace(workspace)
+        out = np.empty(B, dtype=np.int32)
+        _check(self._lib.otas_cache_evict(self._h, c, slot.address, length.address, kept.address, B, lead, recent.address, ws, room,
+                                          out.ctypes.data), "otas_cache_evict")
         return out
 
     def otas_timing_enable(self, on: bool) -> None:

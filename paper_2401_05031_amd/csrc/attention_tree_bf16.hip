@@ -229,6 +229,25 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
   }
 }
 
+// Largest logit and weight sum of a row from its parts' (stride TH): four at a time, so that the loads overlap.
+__device__ __forceinline__ float2 join_ends(const float* tops, int64_t TH, int64_t at, int parts) {
+  float m = -INFINITY, l = 0.f;
+  for (int p0 = 0; p0 < parts; p0 += 4) {
+    float2 e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = *reinterpret_cast<const float2*>(tops + 2 * (min(p0 + i, parts - 1) * TH + at));
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, e[i].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    l *= __builtin_amdgcn_exp2f(m - ref);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) l += p0 + i < parts ? e[i].y * __builtin_amdgcn_exp2f(e[i].x - ref) : 0.f;
+    m = top;
+  }
+  return make_float2(m, l);
+}
+
 // The chunks of every row joined, a wave a row (the first join_wgs workgroups), and beside it, where the logits are at hand, the
 // weights of 256 entries of a query added up over its rows (the others): mass_j += sum_i exp(s_ij - m_i) / l_i, rows in order.
 __global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef c, PlanAny plan, int B, int H, int dh, TreeShape shape, TreeBuffers in,
@@ -236,7 +255,7 @@ __global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef 
   extern __shared__ __attribute__((aligned(16))) float2 ends[];   // m, 1 / l of the query's rows
   const int tid = (int)threadIdx.x;
   if ((int)blockIdx.x < join_wgs) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + (tid >> 6);
+    const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63;
     if (at >= in.TH) return;
     const int row = (int)(at / H);
@@ -247,23 +266,33 @@ __global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef 
     }
     const int len = plan[2 * B + 1 + lo], parts = (len + shape.chunk - 1) / shape.chunk;
     if (parts <= 1) return;   // written already
-    float m = -INFINITY, l = 0.f;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, in.tops[2 * (p * in.TH + at)]);
-    float acc[2] = {0.f, 0.f};
-    for (int p = 0; p < parts; ++p) {
-      const float mp = in.tops[2 * (p * in.TH + at)];
-      const float k = mp == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mp - m);
-      if (k == 0.f) continue;   // wave-uniform
-      l += k * in.tops[2 * (p * in.TH + at) + 1];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (lane + 64 * i < dh) acc[i] += k * in.sums[(p * in.TH + at) * dh + lane + 64 * i];
+    // lane p has what part p (and p + 64, ..) is relative to, lane d columns 2 d and 2 d + 1
+    const float2 e = join_ends(in.tops, in.TH, at, parts);
+    const float ref = e.x == -INFINITY ? 0.f : e.x;
+    const bool mine = 2 * lane < dh;
+    float2 acc = {0.f, 0.f};
+    for (int p0 = 0; p0 < parts; p0 += 64) {
+      const int n = min(64, parts - p0);
+      const float k = lane < n ? __builtin_amdgcn_exp2f(in.tops[2 * ((p0 + lane) * in.TH + at)] - ref) : 0.f;
+      const float* sums = in.sums + (p0 * in.TH + at) * dh + 2 * (mine ? lane : 0);
+#pragma unroll 4
+      for (int p = 0; p < n; ++p) {
+        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k), p));
+        const float2 v = *reinterpret_cast<const float2*>(sums + (int64_t)p * in.TH * dh);
+        if (f != 0.f) {   // a part without a key of weight has sums of 0
+          acc.x += f * v.x;
+          acc.y += f * v.y;
+        }
+      }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (lane + 64 * i < dh) o[at * dh + lane + 64 * i] = (bf16_t)(l == 0.f ? 0.f : acc[i] * inv);
-    if (in.ends && lane == 0) { in.ends[2 * at] = m; in.ends[2 * at + 1] = l; }
+    const float inv = e.y == 0.f ? 0.f : 1.f / e.y;
+    if (mine) {
+      struct alignas(4) Pair { bf16_t x[2]; } out;
+      out.x[0] = (bf16_t)(e.y == 0.f ? 0.f : acc.x * inv);
+      out.x[1] = (bf16_t)(e.y == 0.f ? 0.f : acc.y * inv);
+      *reinterpret_cast<Pair*>(o + at * dh + 2 * lane) = out;
+    }
+    if (in.ends && lane == 0) { in.ends[2 * at] = e.x; in.ends[2 * at + 1] = e.y; }
     return;
   }
   const int id = (int)blockIdx.x - join_wgs, q = id / xblks, e0 = (id % xblks) * 256;
@@ -272,20 +301,8 @@ __global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef 
   if (e0 >= len || n == 0) return;   // workgroup-uniform
   for (int r = tid; r < n * H; r += 256) {
     const int64_t at = (int64_t)base * H + r;
-    float m, l;
-    if (parts <= 1) {
-      m = in.ends[2 * at];
-      l = in.ends[2 * at + 1];
-    } else {
-      m = -INFINITY;
-      l = 0.f;
-      for (int p = 0; p < parts; ++p) m = fmaxf(m, in.tops[2 * (p * in.TH + at)]);
-      for (int p = 0; p < parts; ++p) {
-        const float mp = in.tops[2 * (p * in.TH + at)];
-        if (mp != -INFINITY) l += __builtin_amdgcn_exp2f(mp - m) * in.tops[2 * (p * in.TH + at) + 1];
-      }
-    }
-    ends[r] = l == 0.f ? make_float2(0.f, 0.f) : make_float2(m, 1.f / l);
+    const float2 e = parts <= 1 ? make_float2(in.ends[2 * at], in.ends[2 * at + 1]) : join_ends(in.tops, in.TH, at, parts);
+    ends[r] = e.y == 0.f ? make_float2(0.f, 0.f) : make_float2(e.x, 1.f / e.y);
   }
   __syncthreads();
   const int j = e0 + tid;

@@ -136,7 +136,8 @@ extern "C" {
 otas_status otas_rotary(otas_ctx* c, const void* qkv, int64_t T, int32_t kv_heads, const int32_t* positions,
                         const otas_rotary_desc* rope, void* out) {
   return guarded([&]() -> otas_status {
-    if (!c || !qkv || !positions || !rope || !out || T < 0 || !kv_heads_ok(c, kv_heads)) return OTAS_EINVAL;
+    if (!c || !rope || T < 0 || !kv_heads_ok(c, kv_heads)) return OTAS_EINVAL;
+    if (T > 0 && (!qkv || !positions || !out)) return OTAS_EINVAL;   // no rows, no arrays
     const int dh = c->desc.D / c->desc.H;
     const otas_rotary_desc& d = *rope;
     if (d.rot_dim < 0 || d.rot_dim > dh || d.rot_dim % 2 != 0) return OTAS_EINVAL;
@@ -167,7 +168,8 @@ otas_status otas_attention_masked(otas_ctx* c, const void* qkv, int32_t kv_heads
                                   int32_t causal, const int32_t* prefix, const int32_t* documents, const int32_t* positions,
                                   const otas_score_desc* score, void* o) {
   return guarded([&]() -> otas_status {
-    if (!c || !qkv || !offsets || !o || B <= 0 || !kv_heads_ok(c, kv_heads) || !offsets_ok(offsets, B)) return OTAS_EINVAL;
+    if (!c || !offsets || B <= 0 || !kv_heads_ok(c, kv_heads) || !offsets_ok(offsets, B)) return OTAS_EINVAL;
+    if (offsets[B] > 0 && (!qkv || !o)) return OTAS_EINVAL;
     ScoreArgs sc;
     const otas_status st = score_ok(c, score, &sc);
     if (st != OTAS_OK) return st;
@@ -199,10 +201,11 @@ otas_status otas_cache_append(otas_ctx* c, const otas_kv_cache* cache, const voi
                               const int32_t* rows, const int32_t* positions, const int32_t* slot, const int32_t* length,
                               int32_t B, int32_t* length_out) {
   return guarded([&]() -> otas_status {
-    if (!c || !qkv || !row_offsets || !positions || !slot || !length || !length_out || B <= 0 || T < 0) return OTAS_EINVAL;
+    if (!c || !row_offsets || !slot || !length || !length_out || B <= 0 || T < 0) return OTAS_EINVAL;
     otas_status st = cache_ok(c, cache);
     if (st != OTAS_OK) return st;
     if (!aligned16(qkv) || !aligned4(positions) || !offsets_ok(row_offsets, B)) return OTAS_EINVAL;
+    if (row_offsets[B] > 0 && (!qkv || !positions)) return OTAS_EINVAL;
     st = slots_ok(cache, slot, length, B, true);
     if (st != OTAS_OK) return st;
     const int64_t N = row_offsets[B];
@@ -255,7 +258,8 @@ otas_status otas_attention_tree(otas_ctx* c, const otas_kv_cache* cache, const v
                                 int32_t B, const otas_score_desc* score, int32_t add_mass, void* workspace,
                                 size_t workspace_bytes, void* o) {
   return guarded([&]() -> otas_status {
-    if (!c || !qkv || !offsets || !slot || !length || !workspace || !o || B <= 0 || !offsets_ok(offsets, B)) return OTAS_EINVAL;
+    if (!c || !offsets || !slot || !length || B <= 0 || !offsets_ok(offsets, B)) return OTAS_EINVAL;
+    if (offsets[B] > 0 && (!qkv || !workspace || !o)) return OTAS_EINVAL;
     otas_status st = cache_ok(c, cache);
     if (st != OTAS_OK) return st;
     ScoreArgs sc;
@@ -281,7 +285,7 @@ otas_status otas_attention_tree(otas_ctx* c, const otas_kv_cache* cache, const v
     const int dh = c->desc.D / c->desc.H;
     const TreeShape shape = tree_shape(c->desc.dtype, dh, c->desc.H, cache->kv_heads, offsets, length, B);
     const size_t floats = tree_workspace_floats(shape, c->desc.dtype, T, c->desc.H, dh, max_len, add_mass != 0);
-    if (workspace_bytes < floats * sizeof(float)) return OTAS_ENOMEM;
+    if (T > 0 && workspace_bytes < floats * sizeof(float)) return OTAS_ENOMEM;
     const size_t in_bytes = qkv_bytes(c, T, cache->kv_heads), out_bytes = rows_bytes(c, T);
     if (overlap(qkv, in_bytes, o, out_bytes) || overlap(workspace, floats * sizeof(float), o, out_bytes) ||
         overlap(workspace, floats * sizeof(float), qkv, in_bytes))

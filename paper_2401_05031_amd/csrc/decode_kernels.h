@@ -61,7 +61,8 @@ inline TreeShape tree_shape(int dtype, int dh, int H, int KV, const int32_t* off
   if (dtype != 0 && bf16_width(dh)) t.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   t.groups = std::max(1, (rows + t.rows - 1) / t.rows);
   const int64_t wgs = (int64_t)B * KV * t.groups;
-  const int wanted = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / wgs, (longest + 255) / 256));
+  const int target = t.rows > 32 ? 512 : 1024;
+  const int wanted = (int)std::max<int64_t>(1, std::min<int64_t>(target / wgs, (longest + 127) / 128));
   t.chunk = std::max(128, ((longest + wanted - 1) / wanted + 127) & ~127);
   t.parts = std::max(1, (longest + t.chunk - 1) / t.chunk);
   t.room = wanted;
