@@ -266,24 +266,32 @@ __global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef 
     }
     const int len = plan[2 * B + 1 + lo], parts = (len + shape.chunk - 1) / shape.chunk;
     if (parts <= 1) return;   // written already
-    // lane p has what part p (and p + 64, ..) is relative to, lane d columns 2 d and 2 d + 1
-    const float2 e = join_ends(in.tops, in.TH, at, parts);
-    const float ref = e.x == -INFINITY ? 0.f : e.x;
+    // lane d has columns 2 d and 2 d + 1; eight parts at a time, so that their loads overlap
     const bool mine = 2 * lane < dh;
-    float2 acc = {0.f, 0.f};
-    for (int p0 = 0; p0 < parts; p0 += 64) {
-      const int n = min(64, parts - p0);
-      const float k = lane < n ? __builtin_amdgcn_exp2f(in.tops[2 * ((p0 + lane) * in.TH + at)] - ref) : 0.f;
-      const float* sums = in.sums + (p0 * in.TH + at) * dh + 2 * (mine ? lane : 0);
-#pragma unroll 4
-      for (int p = 0; p < n; ++p) {
-        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k), p));
-        const float2 v = *reinterpret_cast<const float2*>(sums + (int64_t)p * in.TH * dh);
-        if (f != 0.f) {   // a part without a key of weight has sums of 0
-          acc.x += f * v.x;
-          acc.y += f * v.y;
+    float2 acc = {0.f, 0.f}, e = {-INFINITY, 0.f};   // e: largest logit, weight sum
+    for (int p0 = 0; p0 < parts; p0 += 8) {
+      float2 t[8], v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t p = min(p0 + i, parts - 1) * in.TH + at;
+        t[i] = *reinterpret_cast<const float2*>(in.tops + 2 * p);
+        v[i] = *reinterpret_cast<const float2*>(in.sums + p * dh + (mine ? 2 * lane : 0));
+      }
+      float top = e.x;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, t[i].x);
+      const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(e.x - ref);
+      acc.x *= f; acc.y *= f; e.y *= f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float k = p0 + i < parts ? __builtin_amdgcn_exp2f(t[i].x - ref) : 0.f;
+        if (k != 0.f) {   // wave-uniform
+          e.y += k * t[i].y;
+          acc.x += k * v[i].x;
+          acc.y += k * v[i].y;
         }
       }
+      e.x = top;
     }
     const float inv = e.y == 0.f ? 0.f : 1.f / e.y;
     if (mine) {

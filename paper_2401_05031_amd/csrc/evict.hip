@@ -6,78 +6,81 @@
 namespace otas {
 
 // ------------------------------------------------------------------------------------------------- which entries stay
-// Scores become unsigned numbers in the same order (NaN lowest, protected entries highest); the keep-th largest of them is found by
-// its four bytes, highest first: a histogram of the byte over the entries that agree with the bytes found so far, counted
-// per wave in LDS (integer counts: any order gives the same), and a walk from its top.  Of the entries equal to it the lowest stay.
-// Then every wave goes through a run of its own of the entries twice, counting and writing the places below keep that fall
-// free and the entries above that move there, in rising order.  A few passes over 8 n bytes that sit in the L2: latency.
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
+// Scores become unsigned numbers in the same order (NaN lowest, protected entries highest), which stay in LDS up to 32768 entries
+// (beyond that they are formed again in every pass).  The keep-th largest of them is found by 11, 11 and 10 bits, highest first: a
+// histogram of the bits over the entries that agree with those found so far (integer counts: any order gives the same), and a
+// scan from its top.  Bytes would take a fourth pass, and the highest of them is little but the exponent: weights of one
+// order of magnitude would all meet in one counter.  Of the entries equal to the keep-th the lowest stay.  Then every wave goes
+// through a run of its own of the entries twice, counting and writing the places below keep that fall free and the entries above
+// that move there, in rising order.
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64, kEvictBins = 2048, kEvictInLds = 32768;
 
 struct EvictQuery {
   const float* mass;
   const int32_t* positions;
   int n, keep, lead, recent_from;
   bool has_recent;
-  __device__ uint32_t rank(int j) const {
-    if (j < lead || (has_recent && positions[j] >= recent_from)) return 0xFFFFFFFFu;
-    const float m = mass[j] + 0.f;   // -0 and 0 are equal
-    if (m != m) return 0u;
-    const uint32_t b = __float_as_uint(m);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;   // -inf: 0x007FFFFF, inf: 0xFF800000
+  __device__ uint32_t rank(int j) const {   // both loads at once, no branch
+    const float m = mass[j] + 0.f;          // -0 and 0 are equal
+    const int p = positions[j];
+    const uint32_t b = __float_as_uint(m), sign = (uint32_t)((int)b >> 31);
+    const uint32_t r = m != m ? 0u : b ^ (sign | 0x80000000u);   // -inf: 0x007FFFFF, inf: 0xFF800000
+    return (j < lead) | (has_recent & (p >= recent_from)) ? 0xFFFFFFFFu : r;
   }
 };
 
-template <typename P>
+template <bool IN_LDS, typename P>
 __global__ __launch_bounds__(kEvictThreads) void cache_evict_select_kernel(CacheRef c, P plan, int B, int lead, bool has_recent,
                                                                            int32_t* __restrict__ lists) {
-  __shared__ int hist[kEvictWaves][256];
-  __shared__ int total[256];
+  extern __shared__ __attribute__((aligned(16))) uint32_t ranks[];   // [n] where they fit
+  __shared__ int hist[kEvictBins];
   __shared__ uint32_t found;
   __shared__ int above;
   __shared__ int sums[3][kEvictWaves];
   const int q = (int)blockIdx.x, tid = (int)threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int64_t slot = plan[q];
   const int n = plan[B + q], keep = plan[2 * B + q];
-  if (keep >= n) {   // workgroup-uniform
-    if (tid == 0) lists[q] = 0;
-    return;
-  }
-  if (keep == 0) {
+  if (keep >= n || keep == 0) {   // workgroup-uniform
     if (tid == 0) lists[q] = 0;
     return;
   }
   const EvictQuery eq{c.mass + slot * c.capacity, c.positions + slot * c.capacity, n, keep, lead, plan[3 * B + q], has_recent};
+  if (IN_LDS) {
+#pragma unroll 4
+    for (int j = tid; j < n; j += kEvictThreads) ranks[j] = eq.rank(j);
+  }
+  auto rank = [&](int j) { return IN_LDS ? ranks[j] : eq.rank(j); };
   if (tid == 0) { found = 0; above = 0; }
-  for (int byte = 3; byte >= 0; --byte) {
-    for (int i = tid; i < kEvictWaves * 256; i += kEvictThreads) (&hist[0][0])[i] = 0;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+    const uint32_t agree = pass == 0 ? 0u : pass == 1 ? ~0u << 21 : ~0u << 10;
+    for (int i = tid; i < bins; i += kEvictThreads) hist[i] = 0;
     __syncthreads();
-    const uint32_t prefix = found, mask = byte == 3 ? 0u : ~0u << (8 * (byte + 1));
+    const uint32_t prefix = found;
+    const int had = above;
+#pragma unroll 4
     for (int j = tid; j < n; j += kEvictThreads) {
-      const uint32_t r = eq.rank(j);
-      if ((r & mask) == prefix) atomicAdd(&hist[wave][(r >> (8 * byte)) & 255], 1);
+      const uint32_t r = rank(j);
+      if ((r & agree) == prefix) atomicAdd(&hist[(r >> shift) & (bins - 1)], 1);
     }
     __syncthreads();
-    if (tid < 256) {
-      int v = 0;
-      for (int w = 0; w < kEvictWaves; ++w) v += hist[w][tid];
-      total[tid] = v;
+    // The bin of the keep-th largest: as many as possible above it, fewer than keep.  Thread t has the two bins 2 t from the top.
+    const bool has = 2 * tid < bins;
+    const int hi = has ? hist[bins - 1 - 2 * tid] : 0, lo = has ? hist[bins - 2 - 2 * tid] : 0;
+    int upto = hi + lo;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int x = __shfl_up(upto, d);
+      if (lane >= d) upto += x;
     }
+    if (lane == 63) sums[0][wave] = upto;
     __syncthreads();
-    if (wave == 0) {   // the byte of the keep-th largest: as many as possible above it, fewer than keep
-      int v[4], sum = 0;
-      for (int i = 0; i < 4; ++i) sum += v[i] = total[255 - 4 * lane - i];   // lane 0 has the highest four
-      int upto = sum;
-      for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-      }
-      int a = above + upto - sum;
-      if (a < keep && above + upto >= keep) {   // one lane: all entries that agree so far are more than are still wanted
-        int i = 0;
-        while (a + v[i] < keep) a += v[i++];
-        above = a;
-        found = prefix | ((uint32_t)(255 - 4 * lane - i) << (8 * byte));
-      }
+    for (int w = 0; w < wave; ++w) upto += sums[0][w];
+    const int before = had + upto - hi - lo;
+    if (has && before < keep && had + upto >= keep) {   // one thread
+      const bool low = before + hi < keep;
+      above = low ? before + hi : before;
+      found = prefix | ((uint32_t)(bins - 1 - 2 * tid - (low ? 1 : 0)) << shift);
     }
     __syncthreads();
   }
@@ -89,7 +92,7 @@ __global__ __launch_bounds__(kEvictThreads) void cache_evict_select_kernel(Cache
   int eqs = 0;
   for (int b = b0; b < b1; ++b) {
     const int j = b * 64 + lane;
-    eqs += __popcll(__ballot(j < n && eq.rank(j) == edge));
+    eqs += __popcll(__ballot(j < n && rank(j) == edge));
   }
   if (lane == 0) sums[0][wave] = eqs;
   __syncthreads();
@@ -103,7 +106,7 @@ __global__ __launch_bounds__(kEvictThreads) void cache_evict_select_kernel(Cache
     int eqr = eq_before;
     for (int b = b0; b < b1; ++b) {
       const int j = b * 64 + lane;
-      const uint32_t r = j < n ? eq.rank(j) : 0u;
+      const uint32_t r = j < n ? rank(j) : 0u;
       const bool same = j < n && r == edge;
       const uint64_t ties = __ballot(same), below = (1ull << lane) - 1;
       const bool stays = j < n && (r > edge || (same && eqr + __popcll(ties & below) < equal_kept));
@@ -158,11 +161,16 @@ __global__ __launch_bounds__(256) void cache_evict_move_kernel(CacheRef c, P pla
 
 hipError_t launch_cache_evict(int dtype, const CacheRef& c, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_len,
                               int max_moves, int lead, bool has_recent, int32_t* lists, hipStream_t s) {
-  (void)max_len;
   if (max_moves <= 0) return hipSuccess;   // nothing is to go, or nothing stays
   return with_plan(plan, count, d_plan, [&](auto p) {
     typedef decltype(p) P;
-    cache_evict_select_kernel<P><<<dim3(B), dim3(kEvictThreads), 0, s>>>(c, p, B, lead, has_recent, lists);
+    if (max_len <= kEvictInLds) {
+      const hipError_t e = set_max_dynamic_lds((const void*)cache_evict_select_kernel<true, P>, kEvictInLds * (int)sizeof(uint32_t));
+      if (e != hipSuccess) return e;
+      cache_evict_select_kernel<true, P><<<dim3(B), dim3(kEvictThreads), (size_t)max_len * sizeof(uint32_t), s>>>(c, p, B, lead, has_recent, lists);
+    } else {
+      cache_evict_select_kernel<false, P><<<dim3(B), dim3(kEvictThreads), 0, s>>>(c, p, B, lead, has_recent, lists);
+    }
     const dim3 grid((max_moves + kMovesPerGroup - 1) / kMovesPerGroup, B), block(256);
     if (dtype == 0) cache_evict_move_kernel<float, 4, P><<<grid, block, 0, s>>>(c, p, B, lists);
     else if (c.dh % 8 == 0) cache_evict_move_kernel<bf16_t, 8, P><<<grid, block, 0, s>>>(c, p, B, lists);

@@ -385,7 +385,7 @@ def test_queries_that_share_a_slot(lib):
     ("f32", 3, 64, [100, 7, 0], [60, 7, 5], 4, 30, "random"), ("bf16", 2, 80, [1000, 999, 1], [10, 0, 1], 0, None, "random"),
     ("bf16", 1, 12, [300, 65], [299, 64], 1, 10, "ties"), ("bf16", 1, 128, [5000, 40], [3000, 1], 2, 100, "odd"),
     ("f32", 1, 20, [2000], [1999], 0, None, "ties"), ("f32", 1, 4, [20000], [9000], 4, 500, "odd"), ("bf16", 1, 64, [64] * 250, [40] * 250, 1, 3, "random"),
-    ("bf16", 1, 64, [130], [20], 64, None, "random")])
+    ("bf16", 1, 64, [130], [20], 64, None, "random"), ("bf16", 1, 12, [40000, 3], [30000, 2], 3, 70, "odd"), ("bf16", 1, 12, [32768, 32767], [1, 32766], 0, None, "ties")])
 def test_cache_evict(lib, dtype, KV, dh, lengths, keep, lead, recent, kind):
     import torch
     H = 2 if KV < 3 else 3
