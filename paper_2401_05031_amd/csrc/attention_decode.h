@@ -14,6 +14,9 @@ struct PlanAny {
   int32_t v[kArgInts];
   const int32_t* p;
   __device__ int32_t operator[](int i) const { return p ? p[i] : v[i]; }
+  // For an index that the wave shares: the compiler cannot tell that what comes of either place is the same in all lanes, and without that
+  // every address formed from it would be a vector's.
+  __device__ int32_t at(int i) const { return __builtin_amdgcn_readfirstlane((*this)[i]); }
 };
 inline PlanAny plan_any(const int32_t* plan, size_t count, const int32_t* d_plan) {
   PlanAny a;

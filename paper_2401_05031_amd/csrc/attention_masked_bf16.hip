@@ -25,7 +25,7 @@ template <int DH> constexpr size_t masked_lds(int max_n, bool documents) {
 
 template <int DH, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf16_t* __restrict__ qkv, PlanAny plan, int B, int H, int KV, int xblks,
-                                                                       int by_xcd, ScoreArgs sc, MaskArgs mk, bf16_t* __restrict__ o) {
+                                                                       int by_xcd, ScoreArgs sc, CapArgs cap, MaskArgs mk, bf16_t* __restrict__ o) {
   typedef TileRows<DH> R;
   constexpr size_t KB = R::bytes(kKeys), BUF = masked_buffer<DH>();   // keys | values | slack | positions | documents
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
     xblk = xblks - 1 - id / pairs;
   }
   const int h = pair % H, q = pair / H;
-  const int base = plan[q], n = plan[q + 1] - base, row0 = xblk * kRows, prefix = plan[B + 1 + q];
+  const int base = plan.at(q), n = plan.at(q + 1) - base, row0 = xblk * kRows, prefix = plan.at(B + 1 + q);
   if (row0 >= n) return;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fk = lane >> 5;
   const int wrow0 = row0 + wave * 32, row = min(wrow0 + fr, n - 1);
@@ -63,26 +63,36 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
     // the documents of the workgroup's rows: smallest and largest, padding aside
     int lo = INT32_MAX, hi = -1;
     bool padded = false;
-    for (int i = lane; i < min(kRows, n - row0); i += 64) {
-      const int d = docs[row0 + i];
+#pragma unroll
+    for (int i = 0; i < kRows / 64; ++i) {
+      const int d = docs[min(row0 + i * 64 + lane, n - 1)];
       padded |= d < 0;
       if (d >= 0) { lo = min(lo, d); hi = max(hi, d); }
     }
 #pragma unroll
     for (int x = 32; x; x >>= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
     const bool one = lo == hi && !__any(padded);
-    for (int t4 = wave * 4; t4 < tiles; t4 += 16) {   // a wave looks at four tiles, 16 lanes each
-      const int t = t4 + (lane >> 4);
-      bool some = false, all = one;
+    for (int t0 = wave * 4; t0 < tiles; t0 += 64) {   // a wave looks at 4 x 4 tiles at a time, 16 lanes each, all loads at once
+      int d[4][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = t * kKeys + i * 16 + (lane & 15), d = j < n ? docs[j] : -1;
-        some |= hi >= 0 && d >= 0 && ((d >= lo && d <= hi) || j < prefix);
-        all &= d >= 0 && (d == lo || j < prefix);
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[u][i] = docs[min((t0 + 16 * u + (lane >> 4)) * kKeys + i * 16 + (lane & 15), n - 1)];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = t0 + 16 * u + (lane >> 4);
+        bool some = false, all = one;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = t * kKeys + i * 16 + (lane & 15);
+          const bool in = (d[u][i] >= lo) & (d[u][i] <= hi), here = (j < n) & (d[u][i] >= 0);
+          some |= (hi >= 0) & here & (in | (j < prefix));
+          all &= here & ((d[u][i] == lo) | (j < prefix));
+        }
+        const uint64_t s = __ballot(some), a = __ballot(all);
+        const int sh = lane & 48;
+        if ((lane & 15) == 0 && t < tiles) kinds[t] = (unsigned char)(((s >> sh & 0xFFFF) != 0 ? 1 : 0) | ((a >> sh & 0xFFFF) == 0xFFFF ? 2 : 0));
       }
-      const uint64_t s = __ballot(some), a = __ballot(all);
-      const int sh = lane & 48;
-      if ((lane & 15) == 0 && t < tiles) kinds[t] = (unsigned char)(((s >> sh & 0xFFFF) != 0 ? 1 : 0) | ((a >> sh & 0xFFFF) == 0xFFFF ? 2 : 0));
     }
     __syncthreads();
   }
@@ -134,7 +144,10 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
       floatx16 s[2];
       tile_products<DH>(s[0], w, buf, 0, fr, fk);
       tile_products<DH>(s[1], w, buf, 1, fr, fk);
-      if (CAP) {
+      const bool whole = kb + kKeys <= sure && (!docs || (kinds[t] & 2));
+      bool done = false;
+      if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);
+      if (CAP && !done) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -160,7 +173,6 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
             for (int e = 0; e < 4; ++e) s[b][4 * g + e] = fmaf(-score.slope2, fabsf(d[e]), CAP ? s[b][4 * g + e] : s[b][4 * g + e] * score.scale2);
           }
       }
-      const bool whole = kb + kKeys <= sure && (!docs || (kinds[t] & 2));
       if (!whole && !docs) {
         const int left = limit - kb - 4 * fk;   // keys of this half that the row sees, from the tile's first on
 #pragma unroll
@@ -189,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
           }
         }
       }
-      tile_weights<DH, 2>(w, s, CAP || BIAS ? 1.f : score.scale2);
+      if (!done) tile_weights<DH, 2>(w, s, CAP || BIAS ? 1.f : score.scale2);
       tile_sums<DH, 2>(w, s, buf + KB, 0, lane);
     }
     t = next;
@@ -240,7 +252,7 @@ hipError_t launch_attention_masked_bf16(const void* qkv, const int32_t* plan, si
     const size_t lds = masked_lds<DH>(max_n, mk.documents != nullptr);
     const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)masked_lds<DH>(1 << 20, true));
     if (e != hipSuccess) return e;
-    kern<<<dim3((unsigned)wgs), dim3(256), lds, s>>>((const bf16_t*)qkv, p, B, H, KV, xblks, by_xcd, sc, mk, (bf16_t*)o);
+    kern<<<dim3((unsigned)wgs), dim3(256), lds, s>>>((const bf16_t*)qkv, p, B, H, KV, xblks, by_xcd, sc, CapArgs::of(sc), mk, (bf16_t*)o);
     return hipGetLastError();
   };
   auto pick = [&](auto width) {

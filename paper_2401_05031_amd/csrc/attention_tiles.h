@@ -69,16 +69,32 @@ template <int DH, int ROWS, int WAVES> struct TileLoader {
       vcol[i] = (uint32_t)min(R::value_piece(r, p), R::PIECES - 1) * 16u;
     }
   }
-  // k, v: the tile's first row; ld: bytes from row to row; last: the last row that may be read (later ones repeat it).
+  // k, v: the tile's first row; ld: bytes from row to row; last: the last row that may be read (later ones repeat it).  All but
+  // the lanes' places are the wave's: a tile that is all there costs an addition or two per instruction.
   __device__ __forceinline__ void load(const char* k, const char* v, uint32_t ld, int last, char* lds_k, char* lds_v) const {
+    if (last >= ROWS - 1) {
 #pragma unroll
-    for (int i = 0; i < OWN; ++i)
-      if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {   // wave-uniform
-        const int x = EVEN ? 0 : i;
-        const uint32_t r = (uint32_t)min(EVEN ? row[0] + i * STEP : row[x], last) * ld;
-        __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(k + (r + kcol[x])), OTAS_LDS(lds_k + (wave + i * WAVES) * 1024), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(v + (r + vcol[x])), OTAS_LDS(lds_v + (wave + i * WAVES) * 1024), 16, 0, 0);
-      }
+      for (int i = 0; i < OWN; ++i)
+        if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {
+          const int x = EVEN ? 0 : i;
+          const uint32_t r = __umul24((uint32_t)row[x], ld);
+          const size_t step = (size_t)(EVEN ? i * STEP : 0) * ld;
+          one(k + step, r + kcol[x], lds_k + (wave + i * WAVES) * 1024);
+          one(v + step, r + vcol[x], lds_v + (wave + i * WAVES) * 1024);
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < OWN; ++i)
+        if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {
+          const int x = EVEN ? 0 : i;
+          const uint32_t r = __umul24((uint32_t)min(EVEN ? row[0] + i * STEP : row[x], last), ld);
+          one(k, r + kcol[x], lds_k + (wave + i * WAVES) * 1024);
+          one(v, r + vcol[x], lds_v + (wave + i * WAVES) * 1024);
+        }
+    }
+  }
+  static __device__ __forceinline__ void one(const char* base, uint32_t at, char* lds) {
+    __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(base + at), OTAS_LDS(lds), 16, 0, 0);
   }
 };
 
@@ -209,16 +225,33 @@ struct Score2 {
   }
 };
 
-// The tile's logits (times a positive factor; -inf where not seen) into weights, the running maximum and sum moved on.  The sums are
-// rescaled only when a maximum has grown by more than 8 (a weight may be up to 2^8 then: no accuracy is lost in a floating format).
-template <int DH, int NB>
-__device__ __forceinline__ void tile_weights(WaveRows<DH>& w, floatx16 (&s)[NB], float factor) {
-  float mx = -INFINITY;
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
-  mx = xor32_max(mx) * factor;
+// cap tanh(s scale / cap) for products that stay below three eighths of the cap, as they mostly do: an odd polynomial of degree 5
+// (least squares on a fine grid, re-weighted until the error is flat: 8e-7 of the cap) takes three full-rate instructions and no
+// more for the exponent, where exponential and reciprocal are two at quarter rate and four more; these kernels are bound by
+// the vector ALU there.  limit < 0: scale / cap is too far from 1 for its powers.
+struct CapArgs {
+  float a0, a1, a2, limit;   // logits in units of ln 2 = s (a0 + a1 s^2 + a2 s^4) while |s| <= limit
+  static CapArgs of(const ScoreArgs& sc) {
+    CapArgs r = {0.f, 0.f, 0.f, -1.f};
+    if (!(sc.cap > 0.f)) return r;
+    const double x = fabs((double)sc.scale) / sc.cap, k = sc.cap * 1.4426950408889634 * x;
+    if (x < 1.0 / 65536 || x > 65536.0 || sc.cap > 1e6f) return r;
+    r.a0 = (float)(0.9999854 * k);
+    r.a1 = (float)(-0.33248851 * k * x * x);
+    r.a2 = (float)(0.120988494 * k * x * x * x * x);
+    r.limit = (float)(0.375 / x);
+    return r;
+  }
+  __device__ __forceinline__ float slope(float s) const {   // logit / s
+    const float y = s * s;
+    return fmaf(fmaf(a2, y, a1), y, a0);
+  }
+};
+
+// The sums are rescaled only when a maximum has grown by more than 8 (a weight may be up to 2^8 then: no accuracy is lost in a
+// floating format).
+template <int DH>
+__device__ __forceinline__ void raise_top(WaveRows<DH>& w, float mx) {
   if (__any(mx > w.m + 8.f)) {
     const float m_new = fmaxf(w.m, mx);
     const float alpha = w.m == m_new ? 1.f : __builtin_amdgcn_exp2f(w.m - m_new);   // equal: also where both are -inf
@@ -229,6 +262,42 @@ __device__ __forceinline__ void tile_weights(WaveRows<DH>& w, floatx16 (&s)[NB],
 #pragma unroll
       for (int e = 0; e < 16; ++e) w.o[t][e] *= alpha;
   }
+}
+
+// Products of a tile that every row sees all of into weights, if they are small enough for the polynomial (wave-uniform; else nothing
+// is done).  tanh grows with its argument: the largest product gives the largest logit.
+template <int DH, int NB>
+__device__ __forceinline__ bool tile_weights_capped(WaveRows<DH>& w, floatx16 (&s)[NB], const CapArgs& cap) {
+  float hi = -INFINITY, lo = INFINITY;   // NaN is passed over here and stays one in either form
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      hi = fmaxf(fmaxf(hi, s[b][e]), s[b][e + 1]);
+      lo = fminf(fminf(lo, s[b][e]), s[b][e + 1]);
+    }
+  if (!__all(fmaxf(hi, -lo) <= cap.limit)) return false;
+  hi = xor32_max(hi);
+  raise_top<DH>(w, hi * cap.slope(hi));
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[b][e] = __builtin_amdgcn_exp2f(fmaf(s[b][e], cap.slope(s[b][e]), -w.m));
+      w.l += s[b][e];
+    }
+  return true;
+}
+
+// The tile's logits (times a positive factor; -inf where not seen) into weights, the running maximum and sum moved on.
+template <int DH, int NB>
+__device__ __forceinline__ void tile_weights(WaveRows<DH>& w, floatx16 (&s)[NB], float factor) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[b][e]), s[b][e + 1]);
+  raise_top<DH>(w, xor32_max(mx) * factor);
   const float m = w.m == -INFINITY ? 0.f : w.m;   // nothing seen so far: all weights are 0
 #pragma unroll
   for (int b = 0; b < NB; ++b)

@@ -25,7 +25,7 @@ template <int DH, int RW> struct TreeTile {
 template <int DH, int RW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tree_bf16_kernel(CacheRef c, const bf16_t* __restrict__ qkv, int H,
                                                                                               const int32_t* __restrict__ positions, PlanAny plan, int B,
-                                                                                              bool has_parents, TreeShape shape, ScoreArgs sc,
+                                                                                              bool has_parents, TreeShape shape, ScoreArgs sc, CapArgs cap,
                                                                                               TreeBuffers out, bf16_t* __restrict__ o) {
   typedef TreeTile<DH, RW> S;
   typedef TileRows<DH> R;
@@ -45,8 +45,8 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
     unit = eights + id % (units - eights);
   }
   const int part = unit % shape.parts, kh = unit / shape.parts % c.KV, q = unit / shape.parts / c.KV, G = H / c.KV;
-  const int base = plan[q], n = plan[q + 1] - base, len = plan[2 * B + 1 + q], rows = n * G, group0 = group * 32 * RW;
-  const int64_t slot = plan[B + 1 + q];
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G, group0 = group * 32 * RW;
+  const int64_t slot = plan.at(B + 1 + q);
   if (group0 >= rows || (part > 0 && part * shape.chunk >= len)) return;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fk = lane >> 5;
   const int rw = wave % RW, kg = wave / RW, row0 = group0 + rw * 32;
@@ -102,7 +102,10 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
       floatx16 s[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b) tile_products<DH>(s[b], w, buf, kg * NB + b, fr, fk);
-      if (CAP) {
+      const bool whole = cached && k0 + 32 * NB <= valid;
+      bool done = false;
+      if (CAP && !BIAS && whole && !(RW == 1 && out.logits)) done = tile_weights_capped<DH, NB>(w, s, cap);
+      if (CAP && !done) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -121,15 +124,17 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
           }
       }
       constexpr bool SCALED = CAP || BIAS;
-      if (!cached || k0 + 32 * NB > valid) {
-        const uint64_t sees = cached ? ~0ull : line >> k0;
+      if (!whole) {
+        // of this half's keys, from the wave's first on: how many are left, and which of the nodes the row sees
         const int left = valid - k0 - 4 * fk;
+        const uint64_t mine = cached ? ~0ull : line >> (k0 + 4 * fk);
+        const uint32_t sees[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int j = 32 * b + 8 * (e >> 2) + (e & 3);
-            const bool see = (j < left) & (k0 + j < 64 ? (int)(sees >> (j + 4 * fk) & 1) : (int)cached);
+            const int j = 8 * (e >> 2) + (e & 3);
+            const bool see = (32 * b + j < left) & (int)(sees[b] >> j & 1);
             s[b][e] = see ? s[b][e] : -INFINITY;
           }
       }
@@ -144,7 +149,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
               *reinterpret_cast<floatx4*>(to + 32 * b + 8 * g) = floatx4{s[b][4 * g] * f, s[b][4 * g + 1] * f, s[b][4 * g + 2] * f, s[b][4 * g + 3] * f};
             }
       }
-      tile_weights<DH, NB>(w, s, SCALED ? 1.f : score.scale2);
+      if (!done) tile_weights<DH, NB>(w, s, SCALED ? 1.f : score.scale2);
       tile_sums<DH, NB>(w, s, buf + S::KB, 2 * kg * NB, lane);
     }
   }
@@ -262,9 +267,9 @@ __global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef 
     int lo = 0, hi = B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (plan[mid] <= row) lo = mid; else hi = mid;
+      if (plan.at(mid) <= row) lo = mid; else hi = mid;
     }
-    const int len = plan[2 * B + 1 + lo], parts = (len + shape.chunk - 1) / shape.chunk;
+    const int len = plan.at(2 * B + 1 + lo), parts = (len + shape.chunk - 1) / shape.chunk;
     if (parts <= 1) return;   // written already
     // lane d has columns 2 d and 2 d + 1; eight parts at a time, so that their loads overlap
     const bool mine = 2 * lane < dh;
@@ -304,8 +309,8 @@ __global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef 
     return;
   }
   const int id = (int)blockIdx.x - join_wgs, q = id / xblks, e0 = (id % xblks) * 256;
-  const int base = plan[q], n = plan[q + 1] - base, len = plan[2 * B + 1 + q], parts = (len + shape.chunk - 1) / shape.chunk;
-  const int64_t slot = plan[B + 1 + q];
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), parts = (len + shape.chunk - 1) / shape.chunk;
+  const int64_t slot = plan.at(B + 1 + q);
   if (e0 >= len || n == 0) return;   // workgroup-uniform
   for (int r = tid; r < n * H; r += 256) {
     const int64_t at = (int64_t)base * H + r;
@@ -333,8 +338,8 @@ __global__ __launch_bounds__(256, 2) void attention_tree_mass_bf16_kernel(CacheR
                                                                           PlanAny plan, int B, int xblks, ScoreArgs sc, const float* __restrict__ ends) {
   __shared__ float part[4][32];
   const int id = (int)blockIdx.x, q = id / xblks, e0 = (id % xblks) * 32, G = H / c.KV;
-  const int base = plan[q], n = plan[q + 1] - base, len = plan[2 * B + 1 + q], rows = n * G;
-  const int64_t slot = plan[B + 1 + q];
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G;
+  const int64_t slot = plan.at(B + 1 + q);
   if (e0 >= len || n == 0) return;
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;
   const size_t ld = (size_t)(H + 2 * c.KV) * DH;
@@ -401,7 +406,7 @@ hipError_t launch_attention_tree_bf16(const CacheRef& c, const void* qkv, int H,
     auto kern = attention_tree_bf16_kernel<DH, RW, decltype(cap)::value, decltype(bias)::value>;
     hipError_t e = set_max_dynamic_lds((const void*)kern, (int)TreeTile<DH, RW>::LDS);
     if (e != hipSuccess) return e;
-    kern<<<dim3((unsigned)wgs), dim3(256), TreeTile<DH, RW>::LDS, s>>>(c, (const bf16_t*)qkv, H, positions, p, B, has_parents, shape, sc, buf, (bf16_t*)o);
+    kern<<<dim3((unsigned)wgs), dim3(256), TreeTile<DH, RW>::LDS, s>>>(c, (const bf16_t*)qkv, H, positions, p, B, has_parents, shape, sc, CapArgs::of(sc), buf, (bf16_t*)o);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t second = join_wgs + (by_logits ? (int64_t)B * xblks : 0);

@@ -50,8 +50,8 @@ def rotary(qkv, H, KV, positions, rot, interleaved, freqs, magnitude=1.0, invers
 def attend(q, k, v, visible, dtype, scale, cap=0.0, slope=0.0, distance=None):
     """One head: q [m, dh], k, v [n, dh], visible [m, n] -> (o, bound of o, weights, bound of the weights), 64 bits.
 
-    Logits: dh products and sums, scale, cap (tanh good to 4 half steps, times cap), slope and distance, each rounded in
-    float32.  Weights of a logit that is off by d are off by d of themselves and by the mean of d over the row; exponential,
+    Logits: dh products and sums, scale, cap (tanh good to 4 half steps, in bfloat16 to 2^-20, times cap), slope and distance,
+    each rounded in float32.  Weights of a logit that is off by d are off by d of themselves and by the mean of d over the row; exponential,
     running sum and its factors add 16 half steps.  In bfloat16 the weight is rounded once before it meets the value, and the output
     once."""
     q, k, v = q.double(), k.double(), v.double()
@@ -66,7 +66,7 @@ def attend(q, k, v, visible, dtype, scale, cap=0.0, slope=0.0, distance=None):
     off = F32 * ((dh + 4) * abs(scale) * (q.abs() @ k.abs().T.contiguous()) + 2 * s.abs())
     if cap:
         s = cap * torch.tanh(s / cap)
-        off = off + 8 * F32 * cap
+        off = off + (8 * F32 if dtype == torch.float32 else 2.0 ** -20) * cap
     if slope:
         s = s - slope * distance.abs()
         off = off + F32 * (2 * slope * distance.abs() + s.abs())
