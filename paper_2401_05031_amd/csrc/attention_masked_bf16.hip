@@ -97,12 +97,15 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
     __syncthreads();
   }
 
-  TileLoader<DH, kKeys, 4> loader;
-  loader.begin(wave, lane);
+  TileLoader<DH, kKeys, 4, false> key_loader;
+  TileLoader<DH, kKeys, 4, true> value_loader;
+  key_loader.begin(wave, lane);
+  value_loader.begin(wave, lane);
   auto fetch = [&](int t, char* buf) {
     const size_t at = (size_t)t * kKeys * ldb;
     const int last = n - 1 - t * kKeys;
-    loader.load(kbase + at, vbase + at, ldb, last, buf, buf + KB);
+    key_loader.load(kbase + at, ldb, last, buf);
+    value_loader.load(vbase + at, ldb, last, buf + KB);
     if (BIAS && pos && wave == 0)
       __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(pos + t * kKeys + min(lane, last)), OTAS_LDS(buf + 2 * KB + value_slack<DH>()), 4, 0, 0);
     if (docs && wave == 1)

@@ -34,21 +34,27 @@ __device__ __forceinline__ void wait_all_barrier() {
 }
 
 // Where the 16-byte pieces of a tile's rows lie.  A load instruction fills 64 consecutive pieces of LDS, so that no padding comes
-// for free; in its place pieces change places within a row by a rule on the row.  Keys are read 16 bytes a lane from
-// 16 rows at a time, values 8 bytes a lane by the transposing read, 4 rows x 32 bytes per 16 lanes: the two rules put either
-// on all 64 banks once.  Widths of 80 and 96 have one spare piece a row instead (an odd number of pieces moves the rows apart).
+// for free; in its place pieces change places within a row by a rule on the row.  Keys are read 16 bytes a lane from 16 rows at
+// a time, values 8 bytes a lane by the transposing read, 4 rows x 64 bytes per 32 lanes: the rules put either on all 64 banks
+// once.  Rows of 80 and 96 elements take 12 pieces, turned by a place every four rows.
 template <int DH> struct TileRows {
   static constexpr int PIECES = DH / 8;
-  static constexpr int STRIDE = DH % 64 == 0 ? PIECES : PIECES + 1;   // pieces from row to row
+  static constexpr int STRIDE = DH % 64 == 0 ? PIECES : 12;   // pieces from row to row
+  static_assert(PIECES <= STRIDE, "widths of 64, 80, 96 and 128");
   static constexpr int ROW_BYTES = STRIDE * 16;
   static constexpr size_t bytes(int rows) { return (size_t)rows * ROW_BYTES; }
-  static __device__ __forceinline__ int key_piece(int row, int c) { return DH == 128 ? c ^ (row & 15) : DH == 64 ? c ^ ((row >> 1) & 7) : c; }
-  static __device__ __forceinline__ int value_piece(int row, int c) { return DH == 128 ? c ^ 2 * (row & 7) : DH == 64 ? c ^ 2 * ((row >> 1) & 3) : c; }
+  static __device__ __forceinline__ int turned(int row, int c) { const int p = c + ((row >> 2) & 3); return p >= 12 ? p - 12 : p; }
+  static __device__ __forceinline__ int unturned(int row, int p) { const int c = p - ((row >> 2) & 3); return c < 0 ? c + 12 : c; }
+  static __device__ __forceinline__ int key_piece(int row, int c) { return DH == 128 ? c ^ (row & 15) : DH == 64 ? c ^ ((row >> 1) & 7) : turned(row, c); }
+  static __device__ __forceinline__ int value_piece(int row, int c) { return DH == 128 ? c ^ 4 * (row & 3) : DH == 64 ? c ^ 4 * ((row >> 1) & 1) : turned(row, c); }
+  // the piece of a row that lies at place p
+  static __device__ __forceinline__ int key_at(int row, int p) { return DH % 64 == 0 ? key_piece(row, p) : unturned(row, p); }
+  static __device__ __forceinline__ int value_at(int row, int p) { return DH % 64 == 0 ? value_piece(row, p) : unturned(row, p); }
 };
 
-// Loads of one wave's share (WAVES waves share the work) of ROWS keys and values into LDS.  The same lane loads the same
-// piece of every tile: its place within the row is formed once.
-template <int DH, int ROWS, int WAVES> struct TileLoader {
+// Loads of one wave's share (WAVES waves share the work) of ROWS rows of keys (VALUES: of values) into LDS.  The same lane loads
+// the same piece of every tile: its place within the row is formed once.
+template <int DH, int ROWS, int WAVES, bool VALUES> struct TileLoader {
   typedef TileRows<DH> R;
   static constexpr int TOTAL = ROWS * R::STRIDE / 64;                  // load instructions a tile
   static constexpr int OWN = (TOTAL + WAVES - 1) / WAVES;
@@ -57,44 +63,36 @@ template <int DH, int ROWS, int WAVES> struct TileLoader {
   static constexpr bool EVEN = DH % 64 == 0;
   static constexpr int PLACES = EVEN ? 1 : OWN, STEP = EVEN ? 64 * WAVES / R::STRIDE : 0;
   int row[PLACES];
-  uint32_t kcol[PLACES], vcol[PLACES];   // bytes within the row
+  uint32_t col[PLACES];   // bytes within the row
   int wave;
   __device__ __forceinline__ void begin(int wave_, int lane) {
-    wave = wave_;
+    wave = VALUES ? WAVES - 1 - wave_ : wave_;   // where the instructions do not divide, the waves with one fewer of keys have one more of values
 #pragma unroll
     for (int i = 0; i < PLACES; ++i) {
       const int at = (wave + i * WAVES) * 64 + lane, r = at / R::STRIDE, p = at - r * R::STRIDE;
       row[i] = r;
-      kcol[i] = (uint32_t)min(R::key_piece(r, p), R::PIECES - 1) * 16u;
-      vcol[i] = (uint32_t)min(R::value_piece(r, p), R::PIECES - 1) * 16u;
+      col[i] = (uint32_t)min(VALUES ? R::value_at(r, p) : R::key_at(r, p), R::PIECES - 1) * 16u;
     }
   }
-  // k, v: the tile's first row; ld: bytes from row to row; last: the last row that may be read (later ones repeat it).  All but
+  // from: the tile's first row; ld: bytes from row to row; last: the last row that may be read (later ones repeat it).  All but
   // the lanes' places are the wave's: a tile that is all there costs an addition or two per instruction.
-  __device__ __forceinline__ void load(const char* k, const char* v, uint32_t ld, int last, char* lds_k, char* lds_v) const {
+  __device__ __forceinline__ void load(const char* from, uint32_t ld, int last, char* lds) const {
     if (last >= ROWS - 1) {
 #pragma unroll
       for (int i = 0; i < OWN; ++i)
         if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {
-          const int x = EVEN ? 0 : i;
-          const uint32_t r = __umul24((uint32_t)row[x], ld);
           const size_t step = (size_t)(EVEN ? i * STEP : 0) * ld;
-          one(k + step, r + kcol[x], lds_k + (wave + i * WAVES) * 1024);
-          one(v + step, r + vcol[x], lds_v + (wave + i * WAVES) * 1024);
+          one(from + step, __umul24((uint32_t)row[EVEN ? 0 : i], ld) + col[EVEN ? 0 : i], lds + (wave + i * WAVES) * 1024);
         }
     } else {
 #pragma unroll
       for (int i = 0; i < OWN; ++i)
-        if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {
-          const int x = EVEN ? 0 : i;
-          const uint32_t r = __umul24((uint32_t)min(EVEN ? row[0] + i * STEP : row[x], last), ld);
-          one(k, r + kcol[x], lds_k + (wave + i * WAVES) * 1024);
-          one(v, r + vcol[x], lds_v + (wave + i * WAVES) * 1024);
-        }
+        if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL)
+          one(from, __umul24((uint32_t)min(EVEN ? row[0] + i * STEP : row[EVEN ? 0 : i], last), ld) + col[EVEN ? 0 : i], lds + (wave + i * WAVES) * 1024);
     }
   }
-  static __device__ __forceinline__ void one(const char* base, uint32_t at, char* lds) {
-    __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(base + at), OTAS_LDS(lds), 16, 0, 0);
+  static __device__ __forceinline__ void one(const char* from, uint32_t at, char* lds) {
+    __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(from + at), OTAS_LDS(lds), 16, 0, 0);
   }
 };
 
@@ -138,9 +136,9 @@ template <int DH>
 __device__ __forceinline__ short8_t tile_values(const char* lds_v, int kk, int t, int lane) {
   typedef TileRows<DH> R;
   const int s16 = lane & 15, row = 4 * (lane >> 5) + (s16 >> 2), c = t * 4 + ((lane >> 4) & 1) * 2 + ((s16 & 3) >> 1);
-  const char* p = lds_v + (kk * 16 + row) * R::ROW_BYTES + R::value_piece(row, c) * 16 + (s16 & 1) * 8;   // 16 kk, 8: the rule's period
-  const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(p));
-  const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(p + 8 * R::ROW_BYTES));
+  const char* p = lds_v + (kk * 16 + row) * R::ROW_BYTES + (s16 & 1) * 8;   // 16 rows: the rules' period
+  const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(p + R::value_piece(row, c) * 16));
+  const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(p + 8 * R::ROW_BYTES + R::value_piece(row + 8, c) * 16));
   return short8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
 template <int DH> constexpr int value_slack() { return 64; }   // bytes that the last columns' reads of the last row may run past a tile

@@ -62,14 +62,17 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
   const int32_t* cached_pos = c.positions + slot * c.capacity + begin;
   const int cached_tiles = (max(0, end - begin) + KEYS - 1) / KEYS, steps = cached_tiles + (part == 0 ? 1 : 0);   // the nodes themselves last
 
-  TileLoader<DH, KEYS, 4> loader;
-  loader.begin(wave, lane);
+  TileLoader<DH, KEYS, 4, false> key_loader;
+  TileLoader<DH, KEYS, 4, true> value_loader;
+  key_loader.begin(wave, lane);
+  value_loader.begin(wave, lane);
   auto fetch = [&](int i, char* buf) {
     const bool cached = i < cached_tiles;   // wave-uniform
     const int last = cached ? end - begin - 1 - i * KEYS : n - 1;
     const size_t at = cached ? (size_t)i * KEYS * (DH * sizeof(bf16_t)) : 0;
-    loader.load((cached ? cached_k : draft_k) + at, (cached ? cached_v : draft_v) + at, cached ? (uint32_t)(DH * sizeof(bf16_t)) : (uint32_t)(ld * sizeof(bf16_t)),
-                last, buf, buf + S::KB);
+    const uint32_t stride = cached ? (uint32_t)(DH * sizeof(bf16_t)) : (uint32_t)(ld * sizeof(bf16_t));
+    key_loader.load((cached ? cached_k : draft_k) + at, stride, last, buf);
+    value_loader.load((cached ? cached_v : draft_v) + at, stride, last, buf + S::KB);
     if (BIAS && wave < KEYS / 64) {
       const int32_t* p = cached ? cached_pos + i * KEYS : positions + base;
       __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(p + min(wave * 64 + lane, last)), OTAS_LDS(buf + 2 * S::KB + value_slack<DH>() + wave * 256), 4, 0, 0);
