@@ -145,8 +145,9 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
     }
     if (active && kb < none) {   // wave-uniform
       floatx16 s[2];
-      tile_products<DH>(s[0], w, buf, 0, fr, fk);
-      tile_products<DH>(s[1], w, buf, 1, fr, fk);
+      tile_products<DH, 2>(s, w, buf, 0, fr, fk);
+      short8_t v[WaveRows<DH>::DT];
+      first_values<DH>(v, buf + KB, 0, lane);
       const bool whole = kb + kKeys <= sure && (!docs || (kinds[t] & 2));
       bool done = false;
       if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
           for (int e = 0; e < 16; ++e) s[b][e] = score.capped(s[b][e]);
       }
       if (BIAS) {
-        const int4* kp = reinterpret_cast<const int4*>(buf + 2 * KB + value_slack<DH>());
+        const int* kp = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>());
         const float near = (float)(score.position - kb - 4 * fk);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
           for (int g = 0; g < 4; ++g) {
             float d[4];
             if (pos) {
-              const int4 p = kp[b * 8 + 2 * g + fk];
+              const int4 p = read_four(kp, b * 8 + 2 * g + fk);
               d[0] = (float)(score.position - p.x); d[1] = (float)(score.position - p.y);
               d[2] = (float)(score.position - p.z); d[3] = (float)(score.position - p.w);
             } else {
@@ -187,13 +188,13 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
           }
         }
       } else if (!whole) {
-        const int4* kd = reinterpret_cast<const int4*>(buf + 2 * KB + value_slack<DH>() + 256);
+        const int* kd = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>() + 256);
         const int left = limit - kb - 4 * fk, early = own_prefix - kb - 4 * fk;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const int4 d = kd[b * 8 + 2 * g + fk];
+            const int4 d = read_four(kd, b * 8 + 2 * g + fk);
             const int dd[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
         }
       }
       if (!done) tile_weights<DH, 2>(w, s, CAP || BIAS ? 1.f : score.scale2);
-      tile_sums<DH, 2>(w, s, buf + KB, 0, lane);
+      tile_sums<DH, 2>(w, s, v, buf + KB, 0, lane);
     }
     t = next;
     side ^= 1;

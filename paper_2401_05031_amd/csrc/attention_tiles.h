@@ -52,6 +52,10 @@ template <int DH> struct TileRows {
   static __device__ __forceinline__ int value_at(int row, int p) { return DH % 64 == 0 ? value_piece(row, p) : unturned(row, p); }
 };
 
+// LDS is read and written through restricted pointers below: unless the compiler can tell that a read is not of a place that a load
+// straight into LDS is still on its way to, it waits for all such loads before the read, the next tile's among them.
+__device__ __forceinline__ int4 read_four(const int* __restrict__ p, int i) { return *reinterpret_cast<const int4*>(p + 4 * i); }
+
 // Loads of one wave's share (WAVES waves share the work) of ROWS rows of keys (VALUES: of values) into LDS.  The same lane loads
 // the same piece of every tile: its place within the row is formed once.
 template <int DH, int ROWS, int WAVES, bool VALUES> struct TileLoader {
@@ -91,7 +95,7 @@ template <int DH, int ROWS, int WAVES, bool VALUES> struct TileLoader {
           one(from, __umul24((uint32_t)min(EVEN ? row[0] + i * STEP : row[EVEN ? 0 : i], last), ld) + col[EVEN ? 0 : i], lds + (wave + i * WAVES) * 1024);
     }
   }
-  static __device__ __forceinline__ void one(const char* from, uint32_t at, char* lds) {
+  static __device__ __forceinline__ void one(const char* __restrict__ from, uint32_t at, char* __restrict__ lds) {
     __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(from + at), OTAS_LDS(lds), 16, 0, 0);
   }
 };
@@ -117,23 +121,36 @@ template <int DH> struct WaveRows {   // a wave's 32 rows
   }
 };
 
-// Products of the rows with keys 32 b .. 32 b + 31 of the tile.
-template <int DH>
-__device__ __forceinline__ void tile_products(floatx16& s, const WaveRows<DH>& w, const char* lds_k, int b, int fr, int fk) {
+// Products of the rows with NB blocks of 32 keys of the tile, from block b0 on.  The keys of a block are read while the products of
+// the one before it run (left alone the compiler reads each piece just before its product, and waits for it there).
+template <int DH, int NB>
+__device__ __forceinline__ void tile_products(floatx16 (&s)[NB], const WaveRows<DH>& w, const char* __restrict__ lds_k, int b0, int fr, int fk) {
   typedef TileRows<DH> R;
+  constexpr int KS = WaveRows<DH>::KS;
+  auto piece = [&](int b, int ks) {   // 32 b does not change the rule
+    return *reinterpret_cast<const bf16x8*>(lds_k + ((b0 + b) * 32 + fr) * R::ROW_BYTES + R::key_piece(fr, 2 * ks + fk) * 16);
+  };
+  bf16x8 kf[2][KS];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) s[e] = 0.f;
+  for (int ks = 0; ks < KS; ++ks) kf[0][ks] = piece(0, ks);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int ks = 0; ks < WaveRows<DH>::KS; ++ks) {
-    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(lds_k + (b * 32 + fr) * R::ROW_BYTES + R::key_piece(fr, 2 * ks + fk) * 16);   // 32 b does not change the rule
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, w.q[ks], s, 0, 0, 0);
+  for (int b = 0; b < NB; ++b) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b & 1][ks], w.q[ks], s[b], 0, 0, 0);
+      if (b + 1 < NB) kf[(b + 1) & 1][ks] = piece(b + 1, ks);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 }
 
 // V^T fragment of columns 32 t .. 32 t + 31 and keys 16 kk .. 16 kk + 15 of the tile (transposing reads: in every 16 lanes lane
 // s points at V[k0 + s / 4][4 (s & 3) ..] and lane i receives V[k0 .. k0 + 3][i]).
 template <int DH>
-__device__ __forceinline__ short8_t tile_values(const char* lds_v, int kk, int t, int lane) {
+__device__ __forceinline__ short8_t tile_values(const char* __restrict__ lds_v, int kk, int t, int lane) {
   typedef TileRows<DH> R;
   const int s16 = lane & 15, row = 4 * (lane >> 5) + (s16 >> 2), c = t * 4 + ((lane >> 4) & 1) * 2 + ((s16 & 3) >> 1);
   const char* p = lds_v + (kk * 16 + row) * R::ROW_BYTES + (s16 & 1) * 8;   // 16 rows: the rules' period
@@ -148,18 +165,32 @@ __device__ __forceinline__ bf16x8 as_bf16(short8_t v) {
   __builtin_memcpy(&f, &v, 16);
   return f;
 }
-// o += V^T P^T over NB blocks of 32 keys; s holds the weights.  The weights are rounded to bf16 for the product: 2^-8 of each at
-// most, as much as the output's own rounding; their sum l takes them unrounded.
+// The tile's first values, read ahead of the exponentials that come before their products.
+template <int DH>
+__device__ __forceinline__ void first_values(short8_t (&v)[WaveRows<DH>::DT], const char* lds_v, int kk0, int lane) {
+#pragma unroll
+  for (int t = 0; t < WaveRows<DH>::DT; ++t) v[t] = tile_values<DH>(lds_v, kk0, t, lane);
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// o += V^T P^T over NB blocks of 32 keys; s holds the weights, v the first 16 keys' values; the next 16 keys' are read beneath the
+// products.  The weights are rounded to bf16 for the product: 2^-8 of each at most, as much as the output's own rounding; their
+// sum l takes them unrounded.
 template <int DH, int NB>
-__device__ __forceinline__ void tile_sums(WaveRows<DH>& w, const floatx16 (&s)[NB], const char* lds_v, int kk0, int lane) {
+__device__ __forceinline__ void tile_sums(WaveRows<DH>& w, const floatx16 (&s)[NB], short8_t (&v)[WaveRows<DH>::DT], const char* lds_v, int kk0, int lane) {
+  constexpr int DT = WaveRows<DH>::DT;
+  short8_t u[DT];
 #pragma unroll
   for (int kk = 0; kk < 2 * NB; ++kk) {
     bf16x8 pf;
 #pragma unroll
     for (int i = 0; i < 8; ++i) pf[i] = (bf16_t)s[kk >> 1][8 * (kk & 1) + i];
 #pragma unroll
-    for (int t = 0; t < WaveRows<DH>::DT; ++t)
-      w.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(tile_values<DH>(lds_v, kk0 + kk, t, lane)), pf, w.o[t], 0, 0, 0);
+    for (int t = 0; t < DT; ++t) {
+      w.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(kk & 1 ? u[t] : v[t]), pf, w.o[t], 0, 0, 0);
+      if (kk + 1 < 2 * NB) (kk & 1 ? v[t] : u[t]) = tile_values<DH>(lds_v, kk0 + kk + 1, t, lane);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 }
 
@@ -167,7 +198,7 @@ __device__ __forceinline__ void tile_sums(WaveRows<DH>& w, const floatx16 (&s)[N
 // row.  All threads of the workgroup go over the tile's values and put 0 in their place; harmful(row) of the tile says whether some row sees
 // that key, and the answer whether any such was met: those are added at the end (add_not_finite).  Barriers before and after are the caller's.
 template <int DH, int ROWS, int THREADS, class F>
-__device__ __forceinline__ bool tile_make_finite(char* lds_v, int tid, F harmful) {
+__device__ __forceinline__ bool tile_make_finite(char* __restrict__ lds_v, int tid, F harmful) {
   typedef TileRows<DH> R;
   bool met = false;
 #pragma unroll
@@ -192,7 +223,7 @@ __device__ __forceinline__ bool tile_make_finite(char* lds_v, int tid, F harmful
 
 // 0 in the place of the tile's values from row `valid` on.
 template <int DH, int ROWS, int THREADS>
-__device__ __forceinline__ void tile_zero_rows(char* lds_v, int tid, int valid) {
+__device__ __forceinline__ void tile_zero_rows(char* __restrict__ lds_v, int tid, int valid) {
   for (int c = valid * TileRows<DH>::STRIDE + tid; c < ROWS * TileRows<DH>::STRIDE; c += THREADS) *reinterpret_cast<uint4*>(lds_v + c * 16) = uint4{0, 0, 0, 0};
 }
 

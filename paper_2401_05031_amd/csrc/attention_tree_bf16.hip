@@ -103,8 +103,9 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
     const int k0 = kg * 32 * NB;
     if (active && k0 < valid) {   // wave-uniform
       floatx16 s[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) tile_products<DH>(s[b], w, buf, kg * NB + b, fr, fk);
+      tile_products<DH, NB>(s, w, buf, kg * NB, fr, fk);
+      short8_t v[WaveRows<DH>::DT];
+      first_values<DH>(v, buf + S::KB, 2 * kg * NB, lane);
       const bool whole = cached && k0 + 32 * NB <= valid;
       bool done = false;
       if (CAP && !BIAS && whole && !(RW == 1 && out.logits)) done = tile_weights_capped<DH, NB>(w, s, cap);
@@ -115,12 +116,12 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
           for (int e = 0; e < 16; ++e) s[b][e] = score.capped(s[b][e]);
       }
       if (BIAS) {
-        const int4* kp = reinterpret_cast<const int4*>(buf + 2 * S::KB + value_slack<DH>()) + k0 / 4;
+        const int* kp = reinterpret_cast<const int*>(buf + 2 * S::KB + value_slack<DH>()) + k0;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const int4 p = kp[b * 8 + 2 * g + fk];
+            const int4 p = read_four(kp, b * 8 + 2 * g + fk);
             const float d[4] = {(float)(score.position - p.x), (float)(score.position - p.y), (float)(score.position - p.z), (float)(score.position - p.w)};
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[b][4 * g + e] = fmaf(-score.slope2, fabsf(d[e]), CAP ? s[b][4 * g + e] : s[b][4 * g + e] * score.scale2);
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
             }
       }
       if (!done) tile_weights<DH, NB>(w, s, SCALED ? 1.f : score.scale2);
-      tile_sums<DH, NB>(w, s, buf + S::KB, 2 * kg * NB, lane);
+      tile_sums<DH, NB>(w, s, v, buf + S::KB, 2 * kg * NB, lane);
     }
   }
   wait_lds_barrier();
