@@ -32,14 +32,30 @@ struct RowMask {
   }
 };
 
+// Logits of the fp32 kernels, in units of ln 2: exp(s - m) is then one v_exp_f32 (good to a unit in the last place).
 struct RowScore {
-  float scale, cap, slope;
+  float scale, cap, cap2, slope2;
   int position;
+  bool sloped;
+  static __device__ RowScore of(const ScoreArgs& sc, int head, int position) {
+    constexpr float log2e = 1.44269504088896340736f;
+    const bool capped = sc.cap > 0.f, sloped = sc.slopes != nullptr;
+    return RowScore{capped ? sc.scale / sc.cap : sc.scale * log2e, sc.cap, sc.cap * log2e, sloped ? sc.slopes[head] * log2e : 0.f, position, sloped};
+  }
+  __device__ float scaled(float s) const { return cap > 0.f ? cap2 * tanhf(s * scale) : s * scale; }
+  __device__ float with_distance(float s, int key_position) const { return s - slope2 * fabsf((float)(position - key_position)); }
   __device__ float logit(float s, int key_position) const {
-    s *= scale;
-    if (cap > 0.f) s = cap * tanhf(s / cap);
-    if (slope != 0.f) s -= slope * fabsf((float)(position - key_position));
-    return s;
+    s = scaled(s);
+    return sloped ? with_distance(s, key_position) : s;
+  }
+  __device__ void capped(floatx16& s) const {
+    if (cap > 0.f) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = cap2 * tanhf(s[e] * scale);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] *= scale;
+    }
   }
 };
 

@@ -35,14 +35,29 @@ __device__ __forceinline__ void rows_begin(FloatRows<T, DT>& r, const T* q, int 
   r.l = 0.f;
 }
 
-// keys: k(j), v(j) addresses of key j's head (any j: those past the end give a row that may be read), logit(s, j) of the
-// lane's row (-inf where it does not see j), sees(j), partial(b) whether block b has a pair that does not see each other.
+// keys: k(j), v(j) addresses of key j's head (any j: those past the end give a row that may be read); logits(s, kb), in place, of the
+// products of a block (in units of ln 2, -inf where the lane's row does not see the key); sees(j); partial(kb) whether block kb
+// has a pair that does not see each other.  Values are asked for when the first products are under way: one set of registers does
+// for keys and values, and two waves fit a SIMD at widths up to 64.
 template <typename T, int DT, class Keys>
 __device__ __forceinline__ void rows_stream(FloatRows<T, DT>& r, const Keys& keys, int dh, int b0, int b1, int step, int fr, int fk) {
+  bool odd = false;   // whether values that are not finite were left out where some row does not see some key
   for (int b = b0; b < b1; b += step) {
     const int kb = b * 32;
-    floatx4 kf[4 * DT];
-    load_heads<T, DT>(kf, keys.k(kb + fr), dh, fk);
+    floatx16 s;
+    {
+      floatx4 kf[4 * DT];
+      load_heads<T, DT>(kf, keys.k(kb + fr), dh, fk);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+      for (int g = 0; g < 4 * DT; ++g)
+        if (8 * g < dh) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[g][u], r.q[g][u], s, 0, 0, 0);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
     float vf[DT][16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -50,68 +65,60 @@ __device__ __forceinline__ void rows_stream(FloatRows<T, DT>& r, const Keys& key
 #pragma unroll
       for (int t = 0; t < DT; ++t) vf[t][e] = to_float(pv[min(32 * t + fr, dh - 1)]);   // sums past the width are not stored
     }
-    floatx16 s;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-    for (int g = 0; g < 4 * DT; ++g)
-      if (8 * g < dh) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[g][u], r.q[g][u], s, 0, 0, 0);
-      }
+    __builtin_amdgcn_sched_barrier(0);
+    keys.logits(s, kb);
     float mx = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[e] = keys.logit(s[e], kb + 8 * (e >> 2) + 4 * fk + (e & 3));
-      mx = fmaxf(mx, s[e]);
-    }
-    const float m_new = fmaxf(r.m, xor32_max(mx));
-    const float m_ref = m_new == -INFINITY ? 0.f : m_new;   // nothing seen so far: all weights 0
-    const float alpha = expf(r.m - m_ref);
-    r.m = m_new;
-    r.l *= alpha;
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) r.o[t][e] *= alpha;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[e] = expf(s[e] - m_ref);
-      r.l += s[e];
-    }
-    if (keys.partial(kb)) {   // wave-uniform
-      bool bad = false;
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    mx = xor32_max(mx);
+    if (__any(mx > r.m)) {   // some row's maximum moved: rescale what there is
+      const float m_new = fmaxf(r.m, mx);
+      const float alpha = r.m == m_new ? 1.f : __builtin_amdgcn_exp2f(r.m - m_new);   // equal: also where both are -inf
+      r.m = m_new;
+      r.l *= alpha;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) bad |= !__builtin_isfinite(vf[t][e]);
-      if (__any(bad)) {   // a weight of 0 does not keep an infinite value out: add those that are seen, and them alone, by counting
+        for (int e = 0; e < 16; ++e) r.o[t][e] *= alpha;
+    }
+    const float m = r.m == -INFINITY ? 0.f : r.m;   // nothing seen so far: all weights 0
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
-          floatx16 nan, pos, neg;
+    for (int e = 0; e < 16; ++e) {
+      s[e] = __builtin_amdgcn_exp2f(s[e] - m);
+      r.l += s[e];
+    }
+    if (keys.partial(kb)) {   // wave-uniform: a weight of 0 does not keep an infinite value out
 #pragma unroll
-          for (int e = 0; e < 16; ++e) nan[e] = pos[e] = neg[e] = 0.f;
+      for (int t = 0; t < DT; ++t)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float sees = keys.sees(kb + 8 * (e >> 2) + 4 * fk + (e & 3)) ? 1.f : 0.f, v = vf[t][e];
-            nan = __builtin_amdgcn_mfma_f32_32x32x2f32(v != v ? 1.f : 0.f, sees, nan, 0, 0, 0);
-            pos = __builtin_amdgcn_mfma_f32_32x32x2f32(v == INFINITY ? 1.f : 0.f, sees, pos, 0, 0, 0);
-            neg = __builtin_amdgcn_mfma_f32_32x32x2f32(v == -INFINITY ? 1.f : 0.f, sees, neg, 0, 0, 0);
-            vf[t][e] = __builtin_isfinite(v) ? v : 0.f;
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            if (nan[e] > 0.f) r.o[t][e] += NAN;
-            if (pos[e] > 0.f) r.o[t][e] += INFINITY;
-            if (neg[e] > 0.f) r.o[t][e] -= INFINITY;
-          }
+        for (int e = 0; e < 16; ++e) {
+          odd |= !__builtin_isfinite(vf[t][e]);
+          vf[t][e] = __builtin_isfinite(vf[t][e]) ? vf[t][e] : 0.f;
         }
-      }
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e)
 #pragma unroll
       for (int t = 0; t < DT; ++t) r.o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[t][e], s[e], r.o[t], 0, 0, 0);
+  }
+  if (!__any(odd)) return;
+  for (int b = b0; b < b1; b += step) {   // they go to the rows that see them
+    if (!keys.partial(b * 32)) continue;
+    for (int j = b * 32; j < b * 32 + 32; ++j) {
+      const bool sees = keys.sees(j);
+      const T* v = keys.v(j);
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int d = 32 * t + 8 * g + 4 * fk;
+          if (d < dh) {
+            const floatx4 x = load4<T>(v + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.o[t][4 * g + e] += sees && !__builtin_isfinite(x[e]) ? x[e] : 0.f;
+          }
+        }
+    }
   }
 }
 
@@ -133,7 +140,7 @@ __device__ __forceinline__ void rows_join(const FloatRows<T, DT>& r, int dh, flo
   float m_all = -INFINITY;
 #pragma unroll
   for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, ml[w * 64 + fr]);
-  const float k = r.m == -INFINITY ? 0.f : expf(r.m - m_all);
+  const float k = r.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r.m - m_all);
   float* mine = osh + (wave * 32 + fr) * LDO;
 #pragma unroll
   for (int t = 0; t < DT; ++t)
@@ -148,7 +155,7 @@ __device__ __forceinline__ void rows_join(const FloatRows<T, DT>& r, int dh, flo
   for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + row]);
 #pragma unroll
   for (int w = 0; w < 4; ++w)
-    if (ml[w * 64 + row] != -INFINITY) l += ml[w * 64 + 32 + row] * expf(ml[w * 64 + row] - m);
+    if (ml[w * 64 + row] != -INFINITY) l += ml[w * 64 + 32 + row] * __builtin_amdgcn_exp2f(ml[w * 64 + row] - m);
   for (int d = (tid & 7) * 4; d < dh; d += 32) {
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -173,20 +180,34 @@ template <typename T> struct PackedKeys {
   RowMask mask;
   RowScore score;
   const int32_t *documents, *positions;   // the query's, or NULL
-  int full;                               // keys below this are seen by every row of the wave
+  int full, fk;                           // keys below `full` are seen by every row of the wave; the lane's half
   __device__ const T* k(int j) const { return kp + (size_t)min(j, n - 1) * ld; }
   __device__ const T* v(int j) const { return vp + (size_t)min(j, n - 1) * ld; }
   __device__ bool sees(int j) const { return j < n && mask.sees(j, documents ? documents[j] : 0); }
-  __device__ float logit(float s, int j) const {
-    const int at = min(j, n - 1);
-    return sees(j) ? score.logit(s, positions ? positions[at] : at) : -INFINITY;
+  __device__ void logits(floatx16& s, int kb) const {
+    score.capped(s);
+    if (score.sloped) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = min(kb + 8 * (e >> 2) + 4 * fk + (e & 3), n - 1);
+        s[e] = score.with_distance(s[e], positions ? positions[j] : j);
+      }
+    }
+    if (documents) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = sees(kb + 8 * (e >> 2) + 4 * fk + (e & 3)) ? s[e] : -INFINITY;
+    } else if (kb + 32 > full) {
+      const int left = min(n, max(mask.prefix, mask.causal ? mask.row + 1 : n)) - kb - 4 * fk;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) < left ? s[e] : -INFINITY;
+    }
   }
   __device__ bool partial(int kb) const { return documents || kb + 32 > full; }
 };
 
 // Four waves have 32 rows of a head between them and take the key blocks in turn.
 template <typename T, int DT, typename P>
-__global__ __launch_bounds__(256) void attention_masked_f32_kernel(const T* __restrict__ qkv, P plan, int B, int H, int KV, int dh, int xblks,
+__global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_masked_f32_kernel(const T* __restrict__ qkv, P plan, int B, int H, int KV, int dh, int xblks,
                                                                    ScoreArgs sc, MaskArgs mk, T* __restrict__ o) {
   extern __shared__ __attribute__((aligned(16))) float f32_lds[];
   int id = (int)blockIdx.x;
@@ -204,8 +225,7 @@ __global__ __launch_bounds__(256) void attention_masked_f32_kernel(const T* __re
   const int32_t* pos = mk.positions ? mk.positions + base : nullptr;
   const PackedKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + KV + kh) * dh, ld, n,
                            RowMask{row, docs ? docs[row] : 0, prefix, mk.causal},
-                           RowScore{sc.scale, sc.cap, sc.slopes ? sc.slopes[h] : 0.f, pos ? pos[row] : row}, docs, pos,
-                           mk.causal ? max(min(row0 + 1, n), prefix) : n};
+                           RowScore::of(sc, h, pos ? pos[row] : row), docs, pos, mk.causal ? max(min(row0 + 1, n), prefix) : n, fk};
   const int end = mk.causal ? max(min(row0 + 32, n), prefix) : n;
   FloatRows<T, DT> r;
   rows_begin<T, DT>(r, first + (size_t)row * ld + (size_t)h * dh, dh, fk);
@@ -247,33 +267,51 @@ hipError_t launch_attention_masked(int dtype, const void* qkv, const int32_t* pl
 // ------------------------------------------------------------------------------------------------ a tree over the cache
 template <typename T> struct CachedKeys {
   const T *kp, *vp;   // the slot's key head
-  int dh, end;        // entries
+  int dh, end, fk;    // entries; the lane's half
   RowScore score;
   const int32_t* positions;   // of the slot, read where there are slopes
   __device__ const T* k(int j) const { return kp + (size_t)min(j, end - 1) * dh; }
   __device__ const T* v(int j) const { return vp + (size_t)min(j, end - 1) * dh; }
   __device__ bool sees(int j) const { return j < end; }
-  __device__ float logit(float s, int j) const { return j < end ? score.logit(s, score.slope != 0.f ? positions[min(j, end - 1)] : 0) : -INFINITY; }
+  __device__ void logits(floatx16& s, int kb) const {
+    score.capped(s);
+    if (score.sloped) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = score.with_distance(s[e], positions[min(kb + 8 * (e >> 2) + 4 * fk + (e & 3), end - 1)]);
+    }
+    if (partial(kb)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = sees(kb + 8 * (e >> 2) + 4 * fk + (e & 3)) ? s[e] : -INFINITY;
+    }
+  }
   __device__ bool partial(int kb) const { return kb + 32 > end; }
 };
 template <typename T> struct DraftKeys {
   const T *kp, *vp;
   size_t ld;
-  int n;
+  int n, fk;
   uint64_t line;   // the nodes that the lane's node sees
   RowScore score;
   const int32_t* positions;
   __device__ const T* k(int j) const { return kp + (size_t)min(j, n - 1) * ld; }
   __device__ const T* v(int j) const { return vp + (size_t)min(j, n - 1) * ld; }
   __device__ bool sees(int j) const { return j < n && (line >> (j & 63) & 1); }
-  __device__ float logit(float s, int j) const { return sees(j) ? score.logit(s, score.slope != 0.f ? positions[j] : 0) : -INFINITY; }
+  __device__ void logits(floatx16& s, int kb) const {
+    score.capped(s);
+    if (score.sloped) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = score.with_distance(s[e], positions[min(kb + 8 * (e >> 2) + 4 * fk + (e & 3), n - 1)]);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = sees(kb + 8 * (e >> 2) + 4 * fk + (e & 3)) ? s[e] : -INFINITY;
+  }
   __device__ bool partial(int) const { return true; }
 };
 
 // A workgroup has 32 rows (nodes x heads that share a key head) and one chunk of the cache; the first chunk's also the nodes
 // themselves.  With one chunk the rows are done, else the sums go to the workspace for the join.
 template <typename T, int DT, typename P>
-__global__ __launch_bounds__(256) void attention_tree_f32_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
+__global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_tree_f32_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
                                                                  P plan, int B, bool has_parents, TreeShape shape, ScoreArgs sc,
                                                                  float* __restrict__ sums, float* __restrict__ tops, float* __restrict__ ends, int64_t TH,
                                                                  T* __restrict__ o) {
@@ -291,19 +329,19 @@ __global__ __launch_bounds__(256) void attention_tree_f32_kernel(CacheRef c, con
   const int row = min(row0 + fr, n * G - 1), node = row / G, head = kh * G + row % G;
   const size_t ld = (size_t)(H + 2 * c.KV) * dh;
   const T* first = qkv + (size_t)base * ld;
-  const RowScore score{sc.scale, sc.cap, sc.slopes ? sc.slopes[head] : 0.f, sc.slopes ? positions[base + node] : 0};
+  const RowScore score = RowScore::of(sc, head, sc.slopes ? positions[base + node] : 0);
   FloatRows<T, DT> r;
   rows_begin<T, DT>(r, first + (size_t)node * ld + (size_t)head * dh, dh, fk);
   const int begin = part * shape.chunk, end = min(len, begin + shape.chunk);   // chunks are whole blocks
   if (begin < end) {
     const T* heads_k = (const T*)c.k + (slot * c.KV + kh) * c.capacity * dh;
     const T* heads_v = (const T*)c.v + (slot * c.KV + kh) * c.capacity * dh;
-    const CachedKeys<T> keys{heads_k, heads_v, dh, end, score, c.positions + slot * c.capacity};
+    const CachedKeys<T> keys{heads_k, heads_v, dh, end, fk, score, c.positions + slot * c.capacity};
     rows_stream<T, DT>(r, keys, dh, (begin >> 5) + wave, (end + 31) >> 5, 4, fr, fk);
   }
   if (part == 0) {
     const uint64_t line = tree_lines(plan, 3 * B + 1, base, n, has_parents, lane);
-    const DraftKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + c.KV + kh) * dh, ld, n, lane_value(line, node), score, positions + base};
+    const DraftKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + c.KV + kh) * dh, ld, n, fk, lane_value(line, node), score, positions + base};
     rows_stream<T, DT>(r, keys, dh, wave, (n + 31) >> 5, 4, fr, fk);
   }
   const bool only = len <= shape.chunk;   // the rows' one chunk
@@ -343,7 +381,7 @@ __global__ __launch_bounds__(256) void attention_tree_join_kernel(P plan, int B,
   for (int p = 0; p < parts; ++p) {
     const float mp = tops[2 * (p * TH + at)];
     if (mp == -INFINITY) continue;
-    const float k = expf(mp - m);
+    const float k = __builtin_amdgcn_exp2f(mp - m);
     l += k * tops[2 * (p * TH + at) + 1];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -395,9 +433,9 @@ __global__ __launch_bounds__(256) void attention_tree_mass_kernel(CacheRef c, co
         if (r < n * G) {
           const int node = r / G, head = kh * G + r % G;
           const int64_t at = (int64_t)(base + node) * H + head;
-          const RowScore score{sc.scale, sc.cap, sc.slopes ? sc.slopes[head] : 0.f, sc.slopes ? positions[base + node] : 0};
+          const RowScore score = RowScore::of(sc, head, sc.slopes ? positions[base + node] : 0);
           const float m = ends[2 * at], l = ends[2 * at + 1];
-          if (l != 0.f) got += expf(score.logit(s[e], kpos) - m) / l;
+          if (l != 0.f) got += __builtin_amdgcn_exp2f(score.logit(s[e], kpos) - m) / l;
         }
       }
     }
