@@ -4,6 +4,7 @@
 // in one pass over the keys with the running maximum and sum of the softmax.  All arithmetic is fp32, on
 // v_mfma_f32_32x32x2_f32 for both products; bf16 operands are widened.
 #include "attention_decode.h"
+#include "attention_tree_join.h"
 
 namespace otas {
 
@@ -358,42 +359,6 @@ __global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_tree_f32_kerne
   });
 }
 
-// The chunks of every row into one, a wave a row.  ends (wanted where the cache's weights are added up): the row's largest logit
-// and sum.
-template <typename T, typename P>
-__global__ __launch_bounds__(256) void attention_tree_join_kernel(P plan, int B, int H, int dh, TreeShape shape, const float* __restrict__ sums,
-                                                                  const float* __restrict__ tops, float* __restrict__ ends, int64_t TH,
-                                                                  T* __restrict__ o) {
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = (int)threadIdx.x & 63;
-  if (at >= TH) return;
-  const int row = (int)(at / H);
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (plan[mid] <= row) lo = mid; else hi = mid;
-  }
-  const int len = plan[2 * B + 1 + lo], parts = (len + shape.chunk - 1) / shape.chunk;
-  if (parts <= 1) return;   // written already
-  float m = -INFINITY, l = 0.f;
-  for (int p = 0; p < parts; ++p) m = fmaxf(m, tops[2 * (p * TH + at)]);
-  float acc[2] = {0.f, 0.f};
-  for (int p = 0; p < parts; ++p) {
-    const float mp = tops[2 * (p * TH + at)];
-    if (mp == -INFINITY) continue;
-    const float k = __builtin_amdgcn_exp2f(mp - m);
-    l += k * tops[2 * (p * TH + at) + 1];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (lane + 64 * i < dh) acc[i] += k * sums[(p * TH + at) * dh + lane + 64 * i];
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (lane + 64 * i < dh) o[at * dh + lane + 64 * i] = from_float<T>(l == 0.f ? 0.f : acc[i] * inv);
-  if (ends && lane == 0) { ends[2 * at] = m; ends[2 * at + 1] = l; }
-}
-
 // mass_j += sum over rows and heads of exp(s_ij - m_i) / l_i, with the logits formed again (the weights of one pass are
 // relative to maxima that the next chunk may change, and keeping them all would be 4 bytes a row and key).  A workgroup has 32
 // entries; its waves share out the key heads, whose keys a lane holds while it goes through the rows 32 at a time: here a lane owns
@@ -466,9 +431,11 @@ static hipError_t attention_tree_any(const CacheRef& c, const void* qkv, int H, 
       if (e != hipSuccess) return e;
       kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>(c, (const T*)qkv, H, positions, p, B, has_parents, shape, sc, sums, tops,
                                                                          add_mass ? ends : nullptr, TH, (T*)o);
-      if (shape.parts > 1)
-        attention_tree_join_kernel<T, P><<<dim3((unsigned)((TH + 3) / 4)), dim3(256), 0, s>>>(p, B, H, c.dh, shape, sums, tops,
-                                                                                             add_mass ? ends : nullptr, TH, (T*)o);
+      if (shape.parts > 1) {
+        const TreeBuffers buf{sums, tops, add_mass ? ends : nullptr, nullptr, TH, 0};
+        const hipError_t j = launch_attention_tree_join<T>(c, plan_any(plan, count, d_plan), B, H, shape, buf, (TH + 3) / 4, 0, o, s);
+        if (j != hipSuccess) return j;
+      }
       if (add_mass && max_len > 0)
         attention_tree_mass_kernel<T, DT, P><<<dim3((unsigned)(B * xblks)), dim3(256), 0, s>>>(c, (const T*)qkv, H, positions, p, B, xblks, sc, ends);
       return hipGetLastError();

@@ -4,13 +4,9 @@
 // single token has few rows, and then all four waves work on keys.  What bounds few rows is the cache's own bytes; what bounds
 // many is the matrix cores and the exponentials, as in otas_attention_masked.
 #include "attention_tiles.h"
+#include "attention_tree_join.h"
 
 namespace otas {
-
-struct TreeBuffers {
-  float *sums, *tops, *ends, *logits;   // logits, ends: or NULL (see below)
-  int64_t TH, stride;
-};
 
 template <int DH, int RW> struct TreeTile {
   static constexpr int KG = 4 / RW, NB = RW == 4 ? 2 : 1, KEYS = 32 * KG * NB;   // waves that share rows, blocks of 32 keys a wave and tile
@@ -238,103 +234,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
   }
 }
 
-// Largest logit and weight sum of a row from its parts' (stride TH): four at a time, so that the loads overlap.
-__device__ __forceinline__ float2 join_ends(const float* tops, int64_t TH, int64_t at, int parts) {
-  float m = -INFINITY, l = 0.f;
-  for (int p0 = 0; p0 < parts; p0 += 4) {
-    float2 e[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = *reinterpret_cast<const float2*>(tops + 2 * (min(p0 + i, parts - 1) * TH + at));
-    float top = m;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, e[i].x);
-    const float ref = top == -INFINITY ? 0.f : top;
-    l *= __builtin_amdgcn_exp2f(m - ref);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) l += p0 + i < parts ? e[i].y * __builtin_amdgcn_exp2f(e[i].x - ref) : 0.f;
-    m = top;
-  }
-  return make_float2(m, l);
-}
-
-// The chunks of every row joined, a wave a row (the first join_wgs workgroups), and beside it, where the logits are at hand, the
-// weights of 256 entries of a query added up over its rows (the others): mass_j += sum_i exp(s_ij - m_i) / l_i, rows in order.
-__global__ __launch_bounds__(256) void attention_tree_join_bf16_kernel(CacheRef c, PlanAny plan, int B, int H, int dh, TreeShape shape, TreeBuffers in,
-                                                                       int join_wgs, int xblks, bf16_t* __restrict__ o) {
-  extern __shared__ __attribute__((aligned(16))) float2 ends[];   // m, 1 / l of the query's rows
-  const int tid = (int)threadIdx.x;
-  if ((int)blockIdx.x < join_wgs) {
-    const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int lane = tid & 63;
-    if (at >= in.TH) return;
-    const int row = (int)(at / H);
-    int lo = 0, hi = B;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (plan.at(mid) <= row) lo = mid; else hi = mid;
-    }
-    const int len = plan.at(2 * B + 1 + lo), parts = (len + shape.chunk - 1) / shape.chunk;
-    if (parts <= 1) return;   // written already
-    // lane d has columns 2 d and 2 d + 1; eight parts at a time, so that their loads overlap
-    const bool mine = 2 * lane < dh;
-    float2 acc = {0.f, 0.f}, e = {-INFINITY, 0.f};   // e: largest logit, weight sum
-    for (int p0 = 0; p0 < parts; p0 += 8) {
-      float2 t[8], v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t p = min(p0 + i, parts - 1) * in.TH + at;
-        t[i] = *reinterpret_cast<const float2*>(in.tops + 2 * p);
-        v[i] = *reinterpret_cast<const float2*>(in.sums + p * dh + (mine ? 2 * lane : 0));
-      }
-      float top = e.x;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, t[i].x);
-      const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(e.x - ref);
-      acc.x *= f; acc.y *= f; e.y *= f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float k = p0 + i < parts ? __builtin_amdgcn_exp2f(t[i].x - ref) : 0.f;
-        if (k != 0.f) {   // wave-uniform
-          e.y += k * t[i].y;
-          acc.x += k * v[i].x;
-          acc.y += k * v[i].y;
-        }
-      }
-      e.x = top;
-    }
-    const float inv = e.y == 0.f ? 0.f : 1.f / e.y;
-    if (mine) {
-      struct alignas(4) Pair { bf16_t x[2]; } out;
-      out.x[0] = (bf16_t)(e.y == 0.f ? 0.f : acc.x * inv);
-      out.x[1] = (bf16_t)(e.y == 0.f ? 0.f : acc.y * inv);
-      *reinterpret_cast<Pair*>(o + at * dh + 2 * lane) = out;
-    }
-    if (in.ends && lane == 0) { in.ends[2 * at] = e.x; in.ends[2 * at + 1] = e.y; }
-    return;
-  }
-  const int id = (int)blockIdx.x - join_wgs, q = id / xblks, e0 = (id % xblks) * 256;
-  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), parts = (len + shape.chunk - 1) / shape.chunk;
-  const int64_t slot = plan.at(B + 1 + q);
-  if (e0 >= len || n == 0) return;   // workgroup-uniform
-  for (int r = tid; r < n * H; r += 256) {
-    const int64_t at = (int64_t)base * H + r;
-    const float2 e = parts <= 1 ? make_float2(in.ends[2 * at], in.ends[2 * at + 1]) : join_ends(in.tops, in.TH, at, parts);
-    ends[r] = e.y == 0.f ? make_float2(0.f, 0.f) : make_float2(e.x, 1.f / e.y);
-  }
-  __syncthreads();
-  const int j = e0 + tid;
-  if (j >= len) return;
-  const float* s = in.logits + (int64_t)base * H * in.stride + j;
-  float got = 0.f;
-#pragma unroll 8
-  for (int r = 0; r < n * H; ++r) {
-    const float2 e = ends[r];
-    got += e.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(s[(int64_t)r * in.stride] - e.x) * e.y;
-  }
-  c.mass[slot * c.capacity + j] += got;
-}
-
-// The same sums with the logits formed again, for many rows.  A workgroup has 32 entries; its waves share out the key heads,
+// mass_j += sum_i exp(s_ij - m_i) / l_i with the logits formed again, for many rows.  A workgroup has 32 entries; its waves share out the key heads,
 // whose keys a lane holds while it goes through the rows 32 at a time: here a lane owns a key, so that the sum over rows is one
 // over its own registers.  Waves are added in order.
 template <int DH, bool CAP, bool BIAS>
@@ -415,9 +315,7 @@ hipError_t launch_attention_tree_bf16(const CacheRef& c, const void* qkv, int H,
     if (e != hipSuccess) return e;
     const int64_t second = join_wgs + (by_logits ? (int64_t)B * xblks : 0);
     if (second > 0) {
-      const size_t lds = by_logits ? 32 * (size_t)c.KV * sizeof(float2) : 0;   // rows of 32 a key head at most
-      attention_tree_join_bf16_kernel<<<dim3((unsigned)second), dim3(256), lds, s>>>(c, p, B, H, c.dh, shape, buf, (int)join_wgs, xblks, (bf16_t*)o);
-      e = hipGetLastError();
+      e = launch_attention_tree_join<bf16_t>(c, p, B, H, shape, buf, join_wgs, by_logits ? xblks : 0, o, s);
       if (e != hipSuccess) return e;
     }
     if (add_mass && !by_logits && max_len > 0) {

@@ -78,6 +78,10 @@ inline size_t tree_workspace_floats(const TreeShape& t, int dtype, int64_t T, in
   const bool logits = add_mass && dtype != 0 && bf16_width(dh) && t.rows == 32;
   return tree_logits_at(t, T, H, dh) + (logits ? (size_t)T * H * tree_logit_stride(max_len) : 0);
 }
+struct TreeBuffers {
+  float *sums, *tops, *ends, *logits;   // ends, logits: or NULL
+  int64_t TH, stride;
+};
 // plan: off [B+1] | slot [B] | length [B] | parents, a byte each (has_parents)
 hipError_t launch_attention_tree(int dtype, const CacheRef& c, const void* qkv, int H, const int32_t* positions, const int32_t* plan,
                                  size_t count, const int32_t* d_plan, int B, int64_t T, int max_len, bool has_parents, const ScoreArgs& sc,
