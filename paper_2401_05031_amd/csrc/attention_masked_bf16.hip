@@ -122,7 +122,8 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
   // Of a tile that some row of the workgroup does not see all of, the values that are not finite are taken out and come back
   // at the end, to the rows that see them.
   const int wg_sure = mk.causal ? max(row0 + 1, prefix) : n;
-  auto partly = [&](int t) { return (t + 1) * kKeys > wg_sure || (docs && !(kinds[t] & 2)); };
+  auto one_document = [&](int t) { return !docs || (__builtin_amdgcn_readfirstlane(kinds[t]) & 2) != 0; };
+  auto partly = [&](int t, bool one) { return (t + 1) * kKeys > wg_sure || !one; };
   int* not_finite = reinterpret_cast<int*>(lds + 2 * BUF);
   if (tid == 0) *not_finite = 0;
 
@@ -137,19 +138,21 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
     char* buf = lds + (side ? BUF : 0);
     if (next < tiles) fetch(next, lds + (side ? 0 : BUF));
     const int kb = t * kKeys;
-    if (partly(t)) {
+    const bool one = one_document(t);
+    if (partly(t, one)) {
       const int* kd = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>() + 256);
       const bool met = tile_make_finite<DH, kKeys, 256>(buf + KB, tid, [&](int r) { return kb + r < end && (!docs || kd[r] >= 0); });
       if (met) *not_finite = 1;
       wait_lds_barrier();
     }
     if (active && kb < none) {   // wave-uniform
+      __builtin_amdgcn_s_setprio(0);
       floatx16 s[2];
       tile_products<DH, 2>(s, w, buf, 0, fr, fk);
       short8_t v[WaveRows<DH>::DT];
       first_values<DH>(v, buf + KB, 0, lane);
-      __builtin_amdgcn_s_setprio(1);   // the vector ALU is what bounds this: a wave that needs it goes before one at its products (358 -> 335 us, 8192 capped rows)
-      const bool whole = kb + kKeys <= sure && (!docs || (kinds[t] & 2));
+      __builtin_amdgcn_s_setprio(1);   // the vector ALU is the bound: a wave that needs it goes before one at its products (358 -> 335 us, 8192 capped rows)
+      const bool whole = kb + kKeys <= sure && one;
       bool done = false;
       if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);
       if (CAP && !done) {
@@ -178,21 +181,17 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
             for (int e = 0; e < 4; ++e) s[b][4 * g + e] = fmaf(-score.slope2, fabsf(d[e]), CAP ? s[b][4 * g + e] : s[b][4 * g + e] * score.scale2);
           }
       }
-      if (!whole && !docs) {
+      if (!whole && one) {   // of documents, all keys are the rows' (or prefix keys): as without
         const int left = limit - kb - 4 * fk;   // keys of this half that the row sees, from the tile's first on
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const bool see = 32 * b + 8 * (e >> 2) + (e & 3) < left;
-            s[b][e] = see ? s[b][e] : -INFINITY;
-          }
-        }
+          for (int e = 0; e < 16; ++e) s[b][e] = 32 * b + 8 * (e >> 2) + (e & 3) < left ? s[b][e] : -INFINITY;
       } else if (!whole) {
         const int* kd = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>() + 256);
         const int left = limit - kb - 4 * fk, early = own_prefix - kb - 4 * fk;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int4 d = read_four(kd, b * 8 + 2 * g + fk);
@@ -204,12 +203,10 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
               s[b][4 * g + e] = see ? s[b][4 * g + e] : -INFINITY;
             }
           }
-        }
       }
       if (!done) tile_weights<DH, 2>(w, s, CAP || BIAS ? 1.f : score.scale2);
       __builtin_amdgcn_s_setprio(0);
       tile_sums<DH, 2>(w, s, v, buf + KB, 0, lane);
-      __builtin_amdgcn_s_setprio(1);   // the vector ALU is the bound: a wave that needs it goes before one at its products
     }
     t = next;
     side ^= 1;
@@ -217,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
   wait_lds_barrier();
   if (*not_finite) {   // workgroup-uniform
     for (int j = 0; j < end; ++j) {
-      if (!partly(j / kKeys)) continue;
+      if (!partly(j / kKeys, one_document(j / kKeys))) continue;
       const int d = docs ? docs[j] : 0;
       const bool see = (j < limit) & (d >= 0) & ((j < own_prefix) | (d == my_doc));
       const bf16_t* v = reinterpret_cast<const bf16_t*>(vbase + (size_t)j * ldb);
