@@ -25,6 +25,13 @@ inline PlanAny plan_any(const int32_t* plan, size_t count, const int32_t* d_plan
   return a;
 }
 
+// Head i of XCD x where the heads of all queries, counted through, divide among the eight.
+__device__ inline int xcd_head(int x, int i, int H) {
+  if (H % 8) return i * 8 + x;
+  const int each = H >> 3, q = i / each;
+  return q * H + x * each + i - q * each;
+}
+
 struct RowMask {
   int row, document, prefix, causal;
   __device__ bool sees(int j, int doc) const {

@@ -211,10 +211,18 @@ template <typename T, int DT, typename P>
 __global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_masked_f32_kernel(const T* __restrict__ qkv, P plan, int B, int H, int KV, int dh, int xblks,
                                                                    ScoreArgs sc, MaskArgs mk, T* __restrict__ o) {
   extern __shared__ __attribute__((aligned(16))) float f32_lds[];
-  int id = (int)blockIdx.x;
-  const int xblk = xblks - 1 - id % xblks;   // under a causal mask the last rows have the most keys: first
-  id /= xblks;
-  const int h = id % H, q = id / H;
+  // The last rows first (under a causal mask they have the most keys); the row blocks of a head on one XCD where heads divide so.
+  const int id = (int)blockIdx.x, pairs = B * H;
+  int pair, xblk;
+  if (pairs % 8 == 0) {
+    const int mine = pairs >> 3, k = id >> 3;
+    pair = xcd_head(id & 7, k % mine, H);
+    xblk = xblks - 1 - k / mine;
+  } else {
+    pair = id % pairs;
+    xblk = xblks - 1 - id / pairs;
+  }
+  const int h = pair % H, q = pair / H;
   const int base = plan[q], n = plan[q + 1] - base, row0 = xblk * 32;
   if (row0 >= n) return;
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;

@@ -30,12 +30,14 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
   constexpr size_t KB = R::bytes(kKeys), BUF = masked_buffer<DH>();   // keys | values | slack | positions | documents
   extern __shared__ __attribute__((aligned(16))) char lds[];
   // Work in the order in which it is handed out: the last row blocks of all heads first (under a causal mask they have the most
-  // keys).  Where the heads divide among the eight XCDs each XCD has its own, whose keys then stay in its L2.
+  // keys).  Where the heads divide among the eight XCDs each XCD has its own, whose keys then stay in its L2: of every query as many
+  // as of any other (a query's heads on one XCD would leave a long query of a ragged batch to it alone), side by side where a
+  // query has eights of them (heads that share keys).
   int id = (int)blockIdx.x, pair, xblk;
   const int pairs = B * H;
   if (by_xcd) {
     const int mine = pairs >> 3, k = id >> 3;
-    pair = (id & 7) * mine + k % mine;
+    pair = xcd_head(id & 7, k % mine, H);
     xblk = xblks - 1 - k / mine;
   } else {
     pair = id % pairs;
