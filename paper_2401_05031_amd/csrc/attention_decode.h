@@ -35,7 +35,7 @@ __device__ inline int xcd_head(int x, int i, int H) {
 struct RowMask {
   int row, document, prefix, causal;
   __device__ bool sees(int j, int doc) const {
-    return (document | doc) >= 0 && (j < prefix || (doc == document && (!causal || j <= row)));
+    return ((document | doc) >= 0) & ((j < prefix) | ((doc == document) & (!causal | (j <= row))));
   }
 };
 
@@ -66,14 +66,16 @@ struct RowScore {
   }
 };
 
-// f(integral_constant<int, tiles of 32 columns>).
+// f(integral_constant<int, tiles of 32 columns>, bool_constant whether the tiles are whole): the checks of columns of a width that
+// is no multiple of 32 take branches and registers that 32, 64, 96 and 128 do without.
 template <typename F>
 inline hipError_t with_tiles(int dh, F f) {
+  auto tiles = [&](auto dt) { return dh % 32 ? f(dt, std::false_type{}) : f(dt, std::true_type{}); };
   switch ((dh + 31) / 32) {
-    case 1: return f(std::integral_constant<int, 1>{});
-    case 2: return f(std::integral_constant<int, 2>{});
-    case 3: return f(std::integral_constant<int, 3>{});
-    case 4: return f(std::integral_constant<int, 4>{});
+    case 1: return tiles(std::integral_constant<int, 1>{});
+    case 2: return tiles(std::integral_constant<int, 2>{});
+    case 3: return tiles(std::integral_constant<int, 3>{});
+    case 4: return tiles(std::integral_constant<int, 4>{});
   }
   return hipErrorInvalidValue;
 }

@@ -36,19 +36,30 @@ __device__ __forceinline__ void rows_begin(FloatRows<T, DT>& r, const T* q, int 
   r.l = 0.f;
 }
 
-// keys: k(j), v(j) addresses of key j's head (any j: those past the end give a row that may be read); logits(s, kb), in place, of the
+// No instruction: a value that the compiler then forms where it is used.  From offsets that it knows to be the same in every
+// iteration it forms the 64-bit addresses of all loads ahead of the loop, 60 registers a lane.
+__device__ __forceinline__ void keep_here(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
+// keys: kp, vp the first key's head, ld elements between keys, end their number; logits(s, kb), in place, of the
 // products of a block (in units of ln 2, -inf where the lane's row does not see the key); sees(j); partial(kb) whether block kb
 // has a pair that does not see each other.  Values are asked for when the first products are under way: one set of registers does
-// for keys and values, and two waves fit a SIMD at widths up to 64.
+// for keys and values.  Three waves fit a SIMD at widths up to 64 and two beyond, which is what the loop lives on: it waits for L2, then
+// for the matrix cores (fp32, 2 queries of 1500 with 12 heads of 64: 94 -> 83 us from two waves to three; 16 heads of 128: 269 ->
+// 215 us from one to two, 76 of 153 TFLOP/s).
 template <typename T, int DT, class Keys>
 __device__ __forceinline__ void rows_stream(FloatRows<T, DT>& r, const Keys& keys, int dh, int b0, int b1, int step, int fr, int fk) {
   bool odd = false;   // whether values that are not finite were left out where some row does not see some key
   for (int b = b0; b < b1; b += step) {
-    const int kb = b * 32;
+    const int kb = b * 32, last = keys.end - 1 - kb;   // rows past the last one are the last one again
     floatx16 s;
     {
       floatx4 kf[4 * DT];
-      load_heads<T, DT>(kf, keys.k(kb + fr), dh, fk);
+      const char* kp = reinterpret_cast<const char*>(keys.kp + (size_t)kb * keys.ld);
+      uint32_t mine = (uint32_t)(min(fr, last) * keys.ld + 4 * fk) * (uint32_t)sizeof(T);
+      keep_here(mine);
+#pragma unroll
+      for (int g = 0; g < 4 * DT; ++g)
+        kf[g] = 8 * g + 4 * fk < dh ? load4<T>(reinterpret_cast<const T*>(kp + (mine + 8 * g * (uint32_t)sizeof(T)))) : floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
@@ -60,11 +71,24 @@ __device__ __forceinline__ void rows_stream(FloatRows<T, DT>& r, const Keys& key
     }
     __builtin_amdgcn_sched_barrier(0);
     float vf[DT][16];
+    const char* vb = reinterpret_cast<const char*>(keys.vp + (size_t)kb * keys.ld);
+    const uint32_t row = (uint32_t)keys.ld * (uint32_t)sizeof(T);
+    const bool full = last >= 31;   // wave-uniform: the rows' offsets within a lane half are scalars
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const T* pv = keys.v(kb + 8 * (e >> 2) + 4 * fk + (e & 3));
+    for (int t = 0; t < DT; ++t) {
+      uint32_t column = (uint32_t)min(32 * t + fr, dh - 1) * (uint32_t)sizeof(T);   // sums past the width are not stored
+      if (full) {
+        uint32_t at = 4 * fk * row + column;
+        keep_here(at);
 #pragma unroll
-      for (int t = 0; t < DT; ++t) vf[t][e] = to_float(pv[min(32 * t + fr, dh - 1)]);   // sums past the width are not stored
+        for (int e = 0; e < 16; ++e)
+          vf[t][e] = to_float(*reinterpret_cast<const T*>(vb + (size_t)((8 * (e >> 2) + (e & 3)) * row) + at));
+      } else {
+        keep_here(column);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          vf[t][e] = to_float(*reinterpret_cast<const T*>(vb + ((uint32_t)min(8 * (e >> 2) + 4 * fk + (e & 3), last) * row + column)));
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
     keys.logits(s, kb);
@@ -105,9 +129,9 @@ __device__ __forceinline__ void rows_stream(FloatRows<T, DT>& r, const Keys& key
   if (!__any(odd)) return;
   for (int b = b0; b < b1; b += step) {   // they go to the rows that see them
     if (!keys.partial(b * 32)) continue;
-    for (int j = b * 32; j < b * 32 + 32; ++j) {
+    for (int j = b * 32; j < min(b * 32 + 32, keys.end); ++j) {
       const bool sees = keys.sees(j);
-      const T* v = keys.v(j);
+      const T* v = keys.vp + (size_t)j * keys.ld;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -176,29 +200,35 @@ template <typename T> __device__ __forceinline__ void store_row4(T* p, floatx4 v
 // --------------------------------------------------------------------------------------------------------- packed rows
 template <typename T> struct PackedKeys {
   const T *kp, *vp;
-  size_t ld;
-  int n;
+  int ld, end;                            // keys from `end` on are seen by no row of the workgroup
   RowMask mask;
   RowScore score;
   const int32_t *documents, *positions;   // the query's, or NULL
   int full, fk;                           // keys below `full` are seen by every row of the wave; the lane's half
-  __device__ const T* k(int j) const { return kp + (size_t)min(j, n - 1) * ld; }
-  __device__ const T* v(int j) const { return vp + (size_t)min(j, n - 1) * ld; }
-  __device__ bool sees(int j) const { return j < n && mask.sees(j, documents ? documents[j] : 0); }
+  __device__ bool sees(int j) const { return j < end && mask.sees(j, documents ? documents[j] : 0); }
   __device__ void logits(floatx16& s, int kb) const {
     score.capped(s);
     if (score.sloped) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int j = min(kb + 8 * (e >> 2) + 4 * fk + (e & 3), n - 1);
+        const int j = min(kb + 8 * (e >> 2) + 4 * fk + (e & 3), end - 1);
         s[e] = score.with_distance(s[e], positions ? positions[j] : j);
       }
     }
     if (documents) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = sees(kb + 8 * (e >> 2) + 4 * fk + (e & 3)) ? s[e] : -INFINITY;
+      for (int g = 0; g < 4; ++g) {
+        int d[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[e] = documents[min(kb + 8 * g + 4 * fk + e, end - 1)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = kb + 8 * g + 4 * fk + e;
+          s[4 * g + e] = (j < end) & mask.sees(j, d[e]) ? s[4 * g + e] : -INFINITY;
+        }
+      }
     } else if (kb + 32 > full) {
-      const int left = min(n, max(mask.prefix, mask.causal ? mask.row + 1 : n)) - kb - 4 * fk;
+      const int left = min(end, max(mask.prefix, mask.causal ? mask.row + 1 : end)) - kb - 4 * fk;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + (e & 3) < left ? s[e] : -INFINITY;
     }
@@ -207,8 +237,8 @@ template <typename T> struct PackedKeys {
 };
 
 // Four waves have 32 rows of a head between them and take the key blocks in turn.
-template <typename T, int DT, typename P>
-__global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_masked_f32_kernel(const T* __restrict__ qkv, P plan, int B, int H, int KV, int dh, int xblks,
+template <typename T, int DT, bool WHOLE>
+__global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_masked_f32_kernel(const T* __restrict__ qkv, PlanAny plan, int B, int H, int KV, int width, int xblks,
                                                                    ScoreArgs sc, MaskArgs mk, T* __restrict__ o) {
   extern __shared__ __attribute__((aligned(16))) float f32_lds[];
   // The last rows first (under a causal mask they have the most keys); the row blocks of a head on one XCD where heads divide so.
@@ -222,20 +252,20 @@ __global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_masked_f32_ker
     pair = id % pairs;
     xblk = xblks - 1 - id / pairs;
   }
-  const int h = pair % H, q = pair / H;
-  const int base = plan[q], n = plan[q + 1] - base, row0 = xblk * 32;
+  const int h = pair % H, q = pair / H, dh = WHOLE ? 32 * DT : width;
+  const int base = plan.at(q), n = plan.at(q + 1) - base, row0 = xblk * 32;
   if (row0 >= n) return;
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;
-  const int row = min(row0 + fr, n - 1), prefix = plan[B + 1 + q];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), fr = lane & 31, fk = lane >> 5;
+  const int row = min(row0 + fr, n - 1), prefix = plan.at(B + 1 + q);
   const size_t ld = (size_t)(H + 2 * KV) * dh;
   const T* first = qkv + (size_t)base * ld;
   const int kh = h / (H / KV);
   const int32_t* docs = mk.documents ? mk.documents + base : nullptr;
   const int32_t* pos = mk.positions ? mk.positions + base : nullptr;
-  const PackedKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + KV + kh) * dh, ld, n,
+  const int end = mk.causal ? max(min(row0 + 32, n), prefix) : n;
+  const PackedKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + KV + kh) * dh, (int)ld, end,
                            RowMask{row, docs ? docs[row] : 0, prefix, mk.causal},
                            RowScore::of(sc, h, pos ? pos[row] : row), docs, pos, mk.causal ? max(min(row0 + 1, n), prefix) : n, fk};
-  const int end = mk.causal ? max(min(row0 + 32, n), prefix) : n;
   FloatRows<T, DT> r;
   rows_begin<T, DT>(r, first + (size_t)row * ld + (size_t)h * dh, dh, fk);
   rows_stream<T, DT>(r, keys, dh, wave, (end + 31) >> 5, 4, fr, fk);
@@ -251,17 +281,14 @@ static hipError_t attention_masked_f32(const void* qkv, const int32_t* plan, siz
   const int xblks = (max_n + 31) / 32;
   const int64_t wgs = (int64_t)xblks * H * B;
   if (wgs > INT32_MAX) return hipErrorInvalidValue;
-  return with_plan(plan, count, d_plan, [&](auto p) {
-    typedef decltype(p) P;
-    auto run = [&](auto dt) {
-      constexpr int DT = decltype(dt)::value;
-      auto kern = attention_masked_f32_kernel<T, DT, P>;
-      const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
-      if (e != hipSuccess) return e;
-      kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>((const T*)qkv, p, B, H, KV, dh, xblks, sc, mk, (T*)o);
-      return hipGetLastError();
-    };
-    return with_tiles(dh, run);
+  const PlanAny p = plan_any(plan, count, d_plan);
+  return with_tiles(dh, [&](auto dt, auto whole) {
+    constexpr int DT = decltype(dt)::value;
+    auto kern = attention_masked_f32_kernel<T, DT, decltype(whole)::value>;
+    const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
+    if (e != hipSuccess) return e;
+    kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>((const T*)qkv, p, B, H, KV, dh, xblks, sc, mk, (T*)o);
+    return hipGetLastError();
   });
 }
 
@@ -276,11 +303,9 @@ hipError_t launch_attention_masked(int dtype, const void* qkv, const int32_t* pl
 // ------------------------------------------------------------------------------------------------ a tree over the cache
 template <typename T> struct CachedKeys {
   const T *kp, *vp;   // the slot's key head
-  int dh, end, fk;    // entries; the lane's half
+  int ld, end, fk;    // entries; the lane's half
   RowScore score;
   const int32_t* positions;   // of the slot, read where there are slopes
-  __device__ const T* k(int j) const { return kp + (size_t)min(j, end - 1) * dh; }
-  __device__ const T* v(int j) const { return vp + (size_t)min(j, end - 1) * dh; }
   __device__ bool sees(int j) const { return j < end; }
   __device__ void logits(floatx16& s, int kb) const {
     score.capped(s);
@@ -297,19 +322,16 @@ template <typename T> struct CachedKeys {
 };
 template <typename T> struct DraftKeys {
   const T *kp, *vp;
-  size_t ld;
-  int n, fk;
+  int ld, end, fk;
   uint64_t line;   // the nodes that the lane's node sees
   RowScore score;
   const int32_t* positions;
-  __device__ const T* k(int j) const { return kp + (size_t)min(j, n - 1) * ld; }
-  __device__ const T* v(int j) const { return vp + (size_t)min(j, n - 1) * ld; }
-  __device__ bool sees(int j) const { return j < n && (line >> (j & 63) & 1); }
+  __device__ bool sees(int j) const { return j < end && (line >> (j & 63) & 1); }
   __device__ void logits(floatx16& s, int kb) const {
     score.capped(s);
     if (score.sloped) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = score.with_distance(s[e], positions[min(kb + 8 * (e >> 2) + 4 * fk + (e & 3), n - 1)]);
+      for (int e = 0; e < 16; ++e) s[e] = score.with_distance(s[e], positions[min(kb + 8 * (e >> 2) + 4 * fk + (e & 3), end - 1)]);
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = sees(kb + 8 * (e >> 2) + 4 * fk + (e & 3)) ? s[e] : -INFINITY;
@@ -319,9 +341,9 @@ template <typename T> struct DraftKeys {
 
 // A workgroup has 32 rows (nodes x heads that share a key head) and one chunk of the cache; the first chunk's also the nodes
 // themselves.  With one chunk the rows are done, else the sums go to the workspace for the join.
-template <typename T, int DT, typename P>
-__global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_tree_f32_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
-                                                                 P plan, int B, bool has_parents, TreeShape shape, ScoreArgs sc,
+template <typename T, int DT, bool WHOLE>
+__global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_tree_f32_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
+                                                                 PlanAny plan, int B, bool has_parents, TreeShape shape, ScoreArgs sc,
                                                                  float* __restrict__ sums, float* __restrict__ tops, float* __restrict__ ends, int64_t TH,
                                                                  T* __restrict__ o) {
   extern __shared__ __attribute__((aligned(16))) float f32_lds[];
@@ -330,11 +352,11 @@ __global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_tree_f32_kerne
   id /= shape.parts;
   const int group = id % shape.groups;
   id /= shape.groups;
-  const int kh = id % c.KV, q = id / c.KV, dh = c.dh, G = H / c.KV;
-  const int base = plan[q], n = plan[q + 1] - base, len = plan[2 * B + 1 + q], row0 = group * 32;
-  const int64_t slot = plan[B + 1 + q];
+  const int kh = id % c.KV, q = id / c.KV, dh = WHOLE ? 32 * DT : c.dh, G = H / c.KV;
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), row0 = group * 32;
+  const int64_t slot = plan.at(B + 1 + q);
   if (row0 >= n * G || (part > 0 && part * shape.chunk >= len)) return;
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), fr = lane & 31, fk = lane >> 5;
   const int row = min(row0 + fr, n * G - 1), node = row / G, head = kh * G + row % G;
   const size_t ld = (size_t)(H + 2 * c.KV) * dh;
   const T* first = qkv + (size_t)base * ld;
@@ -350,7 +372,7 @@ __global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_tree_f32_kerne
   }
   if (part == 0) {
     const uint64_t line = tree_lines(plan, 3 * B + 1, base, n, has_parents, lane);
-    const DraftKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + c.KV + kh) * dh, ld, n, fk, lane_value(line, node), score, positions + base};
+    const DraftKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + c.KV + kh) * dh, (int)ld, n, fk, lane_value(line, node), score, positions + base};
     rows_stream<T, DT>(r, keys, dh, wave, (n + 31) >> 5, 4, fr, fk);
   }
   const bool only = len <= shape.chunk;   // the rows' one chunk
@@ -371,13 +393,13 @@ __global__ __launch_bounds__(256, DT <= 2 ? 2 : 1) void attention_tree_f32_kerne
 // relative to maxima that the next chunk may change, and keeping them all would be 4 bytes a row and key).  A workgroup has 32
 // entries; its waves share out the key heads, whose keys a lane holds while it goes through the rows 32 at a time: here a lane owns
 // a key, so that the sum over rows is one over its own registers.  Waves are added in order.
-template <typename T, int DT, typename P>
+template <typename T, int DT, bool WHOLE>
 __global__ __launch_bounds__(256) void attention_tree_mass_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
-                                                                  P plan, int B, int xblks, ScoreArgs sc, const float* __restrict__ ends) {
+                                                                  PlanAny plan, int B, int xblks, ScoreArgs sc, const float* __restrict__ ends) {
   __shared__ float part[4][32];
-  const int id = (int)blockIdx.x, q = id / xblks, e0 = (id % xblks) * 32, dh = c.dh, G = H / c.KV;
-  const int base = plan[q], n = plan[q + 1] - base, len = plan[2 * B + 1 + q];
-  const int64_t slot = plan[B + 1 + q];
+  const int id = (int)blockIdx.x, q = id / xblks, e0 = (id % xblks) * 32, dh = WHOLE ? 32 * DT : c.dh, G = H / c.KV;
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q);
+  const int64_t slot = plan.at(B + 1 + q);
   if (e0 >= len || n == 0) return;
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, fr = lane & 31, fk = lane >> 5;
   const size_t ld = (size_t)(H + 2 * c.KV) * dh;
@@ -430,24 +452,23 @@ static hipError_t attention_tree_any(const CacheRef& c, const void* qkv, int H, 
   float* ends = workspace;
   float* tops = workspace + 2 * TH;
   float* sums = tops + 2 * TH * shape.parts;
-  return with_plan(plan, count, d_plan, [&](auto p) {
-    typedef decltype(p) P;
-    return with_tiles(c.dh, [&](auto dt) {
-      constexpr int DT = decltype(dt)::value;
-      auto kern = attention_tree_f32_kernel<T, DT, P>;
-      const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
-      if (e != hipSuccess) return e;
-      kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>(c, (const T*)qkv, H, positions, p, B, has_parents, shape, sc, sums, tops,
-                                                                         add_mass ? ends : nullptr, TH, (T*)o);
-      if (shape.parts > 1) {
-        const TreeBuffers buf{sums, tops, add_mass ? ends : nullptr, nullptr, TH, 0};
-        const hipError_t j = launch_attention_tree_join<T>(c, plan_any(plan, count, d_plan), B, H, shape, buf, (TH + 3) / 4, 0, o, s);
-        if (j != hipSuccess) return j;
-      }
-      if (add_mass && max_len > 0)
-        attention_tree_mass_kernel<T, DT, P><<<dim3((unsigned)(B * xblks)), dim3(256), 0, s>>>(c, (const T*)qkv, H, positions, p, B, xblks, sc, ends);
-      return hipGetLastError();
-    });
+  const PlanAny p = plan_any(plan, count, d_plan);
+  return with_tiles(c.dh, [&](auto dt, auto whole) {
+    constexpr int DT = decltype(dt)::value;
+    constexpr bool WHOLE = decltype(whole)::value;
+    auto kern = attention_tree_f32_kernel<T, DT, WHOLE>;
+    const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
+    if (e != hipSuccess) return e;
+    kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>(c, (const T*)qkv, H, positions, p, B, has_parents, shape, sc, sums, tops,
+                                                                       add_mass ? ends : nullptr, TH, (T*)o);
+    if (shape.parts > 1) {
+      const TreeBuffers buf{sums, tops, add_mass ? ends : nullptr, nullptr, TH, 0};
+      const hipError_t j = launch_attention_tree_join<T>(c, p, B, H, shape, buf, (TH + 3) / 4, 0, o, s);
+      if (j != hipSuccess) return j;
+    }
+    if (add_mass && max_len > 0)
+      attention_tree_mass_kernel<T, DT, WHOLE><<<dim3((unsigned)(B * xblks)), dim3(256), 0, s>>>(c, (const T*)qkv, H, positions, p, B, xblks, sc, ends);
+    return hipGetLastError();
   });
 }
 
