@@ -224,7 +224,7 @@ template <typename T> struct PackedKeys {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int j = kb + 8 * g + 4 * fk + e;
-          s[4 * g + e] = (j < end) & mask.sees(j, d[e]) ? s[4 * g + e] : -INFINITY;
+          s[4 * g + e] = ((j < end) & mask.sees(j, d[e])) ? s[4 * g + e] : -INFINITY;
         }
       }
     } else if (kb + 32 > full) {

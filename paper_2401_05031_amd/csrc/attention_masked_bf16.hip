@@ -61,25 +61,32 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
   const int end = mk.causal ? max(min(row0 + kRows, n), prefix) : n, tiles = (end + kKeys - 1) / kKeys;
   unsigned char* kinds = reinterpret_cast<unsigned char*>(lds + 2 * BUF + 16);
   const int my_doc = docs ? docs[row] : 0;
+  WaveRows<DH> w;
   if (docs) {
+    // A wave looks at 4 x 4 tiles at a time, 16 lanes each.  All that it needs for that and its queries are asked for together.
+    int d[4][4], rows_doc[kRows / 64];
+    auto ask = [&](int t0) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[u][i] = docs[min((t0 + 16 * u + (lane >> 4)) * kKeys + i * 16 + (lane & 15), n - 1)];
+    };
+#pragma unroll
+    for (int i = 0; i < kRows / 64; ++i) rows_doc[i] = docs[min(row0 + i * 64 + lane, n - 1)];
+    ask(wave * 4);
+    w.begin(first + (size_t)row * ld + (size_t)h * DH, fk, sc.scale < 0.f);
     // the documents of the workgroup's rows: smallest and largest, padding aside
     int lo = INT32_MAX, hi = -1;
     bool padded = false;
 #pragma unroll
     for (int i = 0; i < kRows / 64; ++i) {
-      const int d = docs[min(row0 + i * 64 + lane, n - 1)];
-      padded |= d < 0;
-      if (d >= 0) { lo = min(lo, d); hi = max(hi, d); }
+      padded |= rows_doc[i] < 0;
+      if (rows_doc[i] >= 0) { lo = min(lo, rows_doc[i]); hi = max(hi, rows_doc[i]); }
     }
 #pragma unroll
     for (int x = 32; x; x >>= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
     const bool one = lo == hi && !__any(padded);
-    for (int t0 = wave * 4; t0 < tiles; t0 += 64) {   // a wave looks at 4 x 4 tiles at a time, 16 lanes each, all loads at once
-      int d[4][4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[u][i] = docs[min((t0 + 16 * u + (lane >> 4)) * kKeys + i * 16 + (lane & 15), n - 1)];
+    for (int t0 = wave * 4; t0 < tiles; t0 += 64) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int t = t0 + 16 * u + (lane >> 4);
@@ -95,6 +102,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
         const int sh = lane & 48;
         if ((lane & 15) == 0 && t < tiles) kinds[t] = (unsigned char)(((s >> sh & 0xFFFF) != 0 ? 1 : 0) | ((a >> sh & 0xFFFF) == 0xFFFF ? 2 : 0));
       }
+      if (t0 + 64 < tiles) ask(t0 + 64);
     }
     __syncthreads();
   }
@@ -129,10 +137,9 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
   int* not_finite = reinterpret_cast<int*>(lds + 2 * BUF);
   if (tid == 0) *not_finite = 0;
 
-  WaveRows<DH> w;
   int t = docs ? next_tile(kinds, 0, tiles, lane) : 0;
   if (t < tiles) fetch(t, lds);
-  w.begin(first + (size_t)row * ld + (size_t)h * DH, fk, sc.scale < 0.f);
+  if (!docs) w.begin(first + (size_t)row * ld + (size_t)h * DH, fk, sc.scale < 0.f);
   int side = 0;
   while (t < tiles) {
     const int next = docs ? next_tile(kinds, t + 1, tiles, lane) : t + 1;
