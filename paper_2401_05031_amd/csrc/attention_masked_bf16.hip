@@ -7,14 +7,25 @@ namespace otas {
 namespace {
 constexpr int kRows = 128, kKeys = 64;
 
-// Which tiles of 64 keys a workgroup has to look at: one byte each, bit 0: some row may see some key, bit 1: every key has the one
-// document of all rows (or is a prefix key, seen by all).
+// Which tiles of 64 keys a workgroup has to look at: one byte each, bit w: some row of wave w may see some key, bit 4 + w: every key has
+// the one document of all rows of wave w (or is a prefix key, seen by all).
 __device__ __forceinline__ int next_tile(const unsigned char* kinds, int t, int tiles, int lane) {   // wave-uniform
   for (; t < tiles; t += 64) {
-    const uint64_t some = __ballot(t + lane < tiles && (kinds[min(t + lane, tiles - 1)] & 1));
+    const uint64_t some = __ballot(t + lane < tiles && (kinds[min(t + lane, tiles - 1)] & 15));
     if (some) return t + __ffsll((unsigned long long)some) - 1;
   }
   return tiles;
+}
+
+// The smallest and the largest of every 16 lanes (rotations within them), in all of them.
+template <int ROTATION> __device__ __forceinline__ int rotated(int x) { return __builtin_amdgcn_update_dpp(0, x, 0x120 + ROTATION, 0xF, 0xF, false); }
+__device__ __forceinline__ int least16(int x) {
+  x = min(x, rotated<8>(x)); x = min(x, rotated<4>(x)); x = min(x, rotated<2>(x));
+  return min(x, rotated<1>(x));
+}
+__device__ __forceinline__ int most16(int x) {
+  x = max(x, rotated<8>(x)); x = max(x, rotated<4>(x)); x = max(x, rotated<2>(x));
+  return max(x, rotated<1>(x));
 }
 }  // namespace
 
@@ -75,32 +86,43 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
     for (int i = 0; i < kRows / 64; ++i) rows_doc[i] = docs[min(row0 + i * 64 + lane, n - 1)];
     ask(wave * 4);
     w.begin(first + (size_t)row * ld + (size_t)h * DH, fk, sc.scale < 0.f);
-    // the documents of the workgroup's rows: smallest and largest, padding aside
-    int lo = INT32_MAX, hi = -1;
-    bool padded = false;
+    // The documents of each wave's rows: smallest and largest, padding aside, and whether there is but the one.  Lane l has wave l & 3's.
+    int lo = 0, hi = 0;
+    bool one = false;
 #pragma unroll
     for (int i = 0; i < kRows / 64; ++i) {
-      padded |= rows_doc[i] < 0;
-      if (rows_doc[i] >= 0) { lo = min(lo, rows_doc[i]); hi = max(hi, rows_doc[i]); }
-    }
+      const int d = rows_doc[i];
+      int least = d < 0 ? INT32_MAX : d, most = max(d, -1);
 #pragma unroll
-    for (int x = 32; x; x >>= 1) { lo = min(lo, __shfl_xor(lo, x)); hi = max(hi, __shfl_xor(hi, x)); }
-    const bool one = lo == hi && !__any(padded);
+      for (int x = 16; x; x >>= 1) { least = min(least, __shfl_xor(least, x)); most = max(most, __shfl_xor(most, x)); }
+      const uint64_t padded = __ballot(d < 0);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int l = __builtin_amdgcn_readlane(least, 32 * half), m = __builtin_amdgcn_readlane(most, 32 * half);
+        if ((lane & 3) == 2 * i + half) { lo = l; hi = m; one = l == m && (uint32_t)(padded >> 32 * half) == 0; }
+      }
+    }
     for (int t0 = wave * 4; t0 < tiles; t0 += 64) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int t = t0 + 16 * u + (lane >> 4);
-        bool some = false, all = one;
+        int least = INT32_MAX, most = -1;
+        bool rest = false;   // padding, or past the end
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int j = t * kKeys + i * 16 + (lane & 15);
-          const bool in = (d[u][i] >= lo) & (d[u][i] <= hi), here = (j < n) & (d[u][i] >= 0);
-          some |= (hi >= 0) & here & (in | (j < prefix));
-          all &= here & ((d[u][i] == lo) | (j < prefix));
+          const bool here = (t * kKeys + i * 16 + (lane & 15) < n) & (d[u][i] >= 0);
+          least = here ? min(least, d[u][i]) : least;
+          most = here ? max(most, d[u][i]) : most;
+          rest |= !here;
         }
-        const uint64_t s = __ballot(some), a = __ballot(all);
+        least = least16(least);
+        most = most16(most);
         const int sh = lane & 48;
-        if ((lane & 15) == 0 && t < tiles) kinds[t] = (unsigned char)(((s >> sh & 0xFFFF) != 0 ? 1 : 0) | ((a >> sh & 0xFFFF) == 0xFFFF ? 2 : 0));
+        rest = (__ballot(rest) >> sh & 0xFFFF) != 0;
+        const bool some = (hi >= 0) & (most >= 0) & ((t * kKeys < prefix) | ((least <= hi) & (most >= lo)));
+        const bool all = one & !rest & (((t + 1) * kKeys <= prefix) | ((least == lo) & (most == lo)));
+        const uint64_t ss = __ballot(some) >> sh & 15, aa = __ballot(all) >> sh & 15;
+        if ((lane & 15) == 0 && t < tiles) kinds[t] = (unsigned char)(ss | (aa & ss) << 4);
       }
       if (t0 + 64 < tiles) ask(t0 + 64);
     }
@@ -132,10 +154,9 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
   // Of a tile that some row of the workgroup does not see all of, the values that are not finite are taken out and come back
   // at the end, to the rows that see them.
   const int wg_sure = mk.causal ? max(row0 + 1, prefix) : n;
-  auto one_document = [&](int t) { return !docs || (__builtin_amdgcn_readfirstlane(kinds[t]) & 2) != 0; };
-  auto partly = [&](int t, bool one) { return (t + 1) * kKeys > wg_sure || !one; };
-  int* not_finite = reinterpret_cast<int*>(lds + 2 * BUF);
-  if (tid == 0) *not_finite = 0;
+  auto kind_of = [&](int t) { return docs ? __builtin_amdgcn_readfirstlane((int)kinds[t]) : 0xFF; };
+  auto partly = [&](int t, int kind) { return (t + 1) * kKeys > wg_sure || (kind & ~(kind >> 4) & 15) != 0; };
+  bool met = false;   // whether this wave took out a value that some row sees
 
   int t = docs ? next_tile(kinds, 0, tiles, lane) : 0;
   if (t < tiles) fetch(t, lds);
@@ -143,18 +164,14 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
   int side = 0;
   while (t < tiles) {
     const int next = docs ? next_tile(kinds, t + 1, tiles, lane) : t + 1;
-    wait_all_barrier();   // tile t is there, and nobody reads the other buffer any more
+    wait_all();   // this wave's part of tile t is there
     char* buf = lds + (side ? BUF : 0);
+    const int kb = t * kKeys, kind = kind_of(t);
+    if (partly(t, kind)) met |= value_loader.make_finite(buf + KB, lane, [&](int r) { return kb + r < end && (!docs || docs[kb + r] >= 0); });
+    wait_lds_barrier();   // all of it, and nobody reads the other buffer any more
     if (next < tiles) fetch(next, lds + (side ? 0 : BUF));
-    const int kb = t * kKeys;
-    const bool one = one_document(t);
-    if (partly(t, one)) {
-      const int* kd = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>() + 256);
-      const bool met = tile_make_finite<DH, kKeys, 256>(buf + KB, tid, [&](int r) { return kb + r < end && (!docs || kd[r] >= 0); });
-      if (met) *not_finite = 1;
-      wait_lds_barrier();
-    }
-    if (active && kb < none) {   // wave-uniform
+    const bool one = (kind >> (4 + wave) & 1) != 0;
+    if (active && kb < none && (kind >> wave & 1)) {   // wave-uniform
       __builtin_amdgcn_s_setprio(0);
       floatx16 s[2];
       tile_products<DH, 2>(s, w, buf, 0, fr, fk);
@@ -220,10 +237,9 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
     t = next;
     side ^= 1;
   }
-  wait_lds_barrier();
-  if (*not_finite) {   // workgroup-uniform
+  if (any_wave(met, reinterpret_cast<int*>(lds + 2 * BUF), wave, lane)) {   // workgroup-uniform
     for (int j = 0; j < end; ++j) {
-      if (!partly(j / kKeys, one_document(j / kKeys))) continue;
+      if (!partly(j / kKeys, kind_of(j / kKeys))) continue;
       const int d = docs ? docs[j] : 0;
       const bool see = (j < limit) & (d >= 0) & ((j < own_prefix) | (d == my_doc));
       const bf16_t* v = reinterpret_cast<const bf16_t*>(vbase + (size_t)j * ldb);

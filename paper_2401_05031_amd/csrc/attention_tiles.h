@@ -26,13 +26,6 @@ __device__ __forceinline__ void wait_lds_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-// Loads and LDS, of every wave of the workgroup.
-__device__ __forceinline__ void wait_all_barrier() {
-  wait_all();
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // Where the 16-byte pieces of a tile's rows lie.  A load instruction fills 64 consecutive pieces of LDS, so that no padding comes
 // for free; in its place pieces change places within a row by a rule on the row.  Keys are read 16 bytes a lane from 16 rows at
 // a time, values 8 bytes a lane by the transposing read, 4 rows x 64 bytes per 32 lanes: the rules put either on all 64 banks
@@ -55,6 +48,22 @@ template <int DH> struct TileRows {
 // LDS is read and written through restricted pointers below: unless the compiler can tell that a read is not of a place that a load
 // straight into LDS is still on its way to, it waits for all such loads before the read, the next tile's among them.
 __device__ __forceinline__ int4 read_four(const int* __restrict__ p, int i) { return *reinterpret_cast<const int4*>(p + 4 * i); }
+
+// Values that are not finite, in a tile of which some row does not see some key: a weight of 0 would not keep them out of that
+// row.  They become 0 in LDS, and those that some row sees are added at the end (add_not_finite).  Here one 16-byte piece: whether
+// it had any.
+__device__ __forceinline__ bool piece_make_finite(char* __restrict__ at) {
+  uint4 u = *reinterpret_cast<const uint4*>(at);
+  uint32_t* x = &u.x;
+  uint32_t odd[4];   // ones over the elements whose exponent is all ones, two at a time
+#pragma unroll
+  for (int k = 0; k < 4; ++k) odd[k] = ((((x[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;
+  if (!(odd[0] | odd[1] | odd[2] | odd[3])) return false;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] &= ~odd[k];
+  *reinterpret_cast<uint4*>(at) = u;
+  return true;
+}
 
 // Loads of one wave's share (WAVES waves share the work) of ROWS rows of keys (VALUES: of values) into LDS.  The same lane loads
 // the same piece of every tile: its place within the row is formed once.
@@ -94,6 +103,27 @@ template <int DH, int ROWS, int WAVES, bool VALUES> struct TileLoader {
         if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL)
           one(from, __umul24((uint32_t)min(EVEN ? row[0] + i * STEP : row[EVEN ? 0 : i], last), ld) + col[EVEN ? 0 : i], lds + (wave + i * WAVES) * 1024);
     }
+  }
+  // Of the pieces that this lane loaded, once they are there (no other wave need have waited); whether harmful(row) of the tile
+  // holds for one that had values to be taken out.
+  template <class F> __device__ __forceinline__ bool make_finite(char* __restrict__ lds, int lane, F harmful) const {
+    bool met = false;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i)
+      if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {
+        const int c = (wave + i * WAVES) * 64 + lane;
+        if (piece_make_finite(lds + c * 16)) met |= harmful(c / R::STRIDE);
+      }
+    return met;
+  }
+  // 0 in the place of those from row `valid` of the tile on.
+  __device__ __forceinline__ void zero_rows(char* __restrict__ lds, int lane, int valid) const {
+#pragma unroll
+    for (int i = 0; i < OWN; ++i)
+      if (TOTAL % WAVES == 0 || wave + i * WAVES < TOTAL) {
+        const int c = (wave + i * WAVES) * 64 + lane;
+        if (c >= valid * R::STRIDE) *reinterpret_cast<uint4*>(lds + c * 16) = uint4{0, 0, 0, 0};
+      }
   }
   static __device__ __forceinline__ void one(const char* __restrict__ from, uint32_t at, char* __restrict__ lds) {
     __builtin_amdgcn_global_load_lds(OTAS_GLOBAL(from + at), OTAS_LDS(lds), 16, 0, 0);
@@ -194,37 +224,12 @@ __device__ __forceinline__ void tile_sums(WaveRows<DH>& w, const floatx16 (&s)[N
   }
 }
 
-// Values that are not finite, in a tile of which some row does not see some key: a weight of 0 would not keep them out of that
-// row.  All threads of the workgroup go over the tile's values and put 0 in their place; harmful(row) of the tile says whether some row sees
-// that key, and the answer whether any such was met: those are added at the end (add_not_finite).  Barriers before and after are the caller's.
-template <int DH, int ROWS, int THREADS, class F>
-__device__ __forceinline__ bool tile_make_finite(char* __restrict__ lds_v, int tid, F harmful) {
-  typedef TileRows<DH> R;
-  bool met = false;
-#pragma unroll
-  for (int i = 0; i < (ROWS * R::STRIDE + THREADS - 1) / THREADS; ++i) {
-    const int c = i * THREADS + tid;
-    if (ROWS * R::STRIDE % THREADS == 0 || c < ROWS * R::STRIDE) {
-      uint4 u = *reinterpret_cast<const uint4*>(lds_v + c * 16);
-      uint32_t* x = &u.x;
-      uint32_t odd[4];   // ones over the elements whose exponent is all ones, two at a time
-#pragma unroll
-      for (int k = 0; k < 4; ++k) odd[k] = ((((x[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;
-      if (odd[0] | odd[1] | odd[2] | odd[3]) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] &= ~odd[k];
-        *reinterpret_cast<uint4*>(lds_v + c * 16) = u;
-        met |= harmful(c / R::STRIDE);
-      }
-    }
-  }
-  return met;
-}
-
-// 0 in the place of the tile's values from row `valid` on.
-template <int DH, int ROWS, int THREADS>
-__device__ __forceinline__ void tile_zero_rows(char* __restrict__ lds_v, int tid, int valid) {
-  for (int c = valid * TileRows<DH>::STRIDE + tid; c < ROWS * TileRows<DH>::STRIDE; c += THREADS) *reinterpret_cast<uint4*>(lds_v + c * 16) = uint4{0, 0, 0, 0};
+// Whether any lane of the workgroup's four waves says so; flags: 16 bytes of LDS of its own.
+__device__ __forceinline__ bool any_wave(bool mine, int* flags, int wave, int lane) {
+  const bool any = __any(mine);
+  if (lane == 0) flags[wave] = any;
+  wait_lds_barrier();
+  return (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
 }
 
 // Four consecutive values v of a key that the lane's row sees: what of them is not finite, added to its sums.

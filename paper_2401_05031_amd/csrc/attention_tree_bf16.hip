@@ -77,25 +77,23 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
   const Score2 score = Score2::of(sc, BIAS ? sc.slopes[head] : 0.f, BIAS ? positions[base + node] : 0);
   uint64_t line = 0;
   if (part == 0) line = lane_value(tree_lines(plan, 3 * B + 1, base, n, has_parents, lane), node);
-  int* not_finite = reinterpret_cast<int*>(lds + S::LDS - 16);
-  if (tid == 0) *not_finite = 0;
+  bool met = false;   // whether this wave took out a sibling's value
 
   fetch(0, lds);
   WaveRows<DH> w;
   w.begin(first + (size_t)node * ld + (size_t)head * DH, fk, sc.scale < 0.f);
   for (int i = 0; i < steps; ++i) {
-    wait_all_barrier();   // tile i is there, and nobody reads the other buffer any more
+    wait_all();   // this wave's part of tile i is there
     char* buf = lds + (i & 1 ? S::BUF : 0);
-    if (i + 1 < steps) fetch(i + 1, lds + (i & 1 ? 0 : S::BUF));
     const bool cached = i < cached_tiles;
     const int valid = cached ? min(KEYS, end - begin - i * KEYS) : n;
     if (!cached) {   // of siblings, values that are not finite are taken out and come back at the end to the nodes that see them
-      if (tile_make_finite<DH, KEYS, 256>(buf + S::KB, tid, [&](int r) { return r < n; })) *not_finite = 1;
-      wait_lds_barrier();
+      met |= value_loader.make_finite(buf + S::KB, lane, [&](int r) { return r < n; });
     } else if (valid < KEYS) {   // rows past the end repeat the last one, which may be infinite
-      tile_zero_rows<DH, KEYS, 256>(buf + S::KB, tid, valid);
-      wait_lds_barrier();
+      value_loader.zero_rows(buf + S::KB, lane, valid);
     }
+    wait_lds_barrier();   // all of it, and nobody reads the other buffer any more
+    if (i + 1 < steps) fetch(i + 1, lds + (i & 1 ? 0 : S::BUF));
     const int k0 = kg * 32 * NB;
     if (active && k0 < valid) {   // wave-uniform
       floatx16 s[NB];
@@ -153,8 +151,8 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
       tile_sums<DH, NB>(w, s, v, buf + S::KB, 2 * kg * NB, lane);
     }
   }
-  wait_lds_barrier();
-  if (*not_finite && kg == 0) {   // one of the waves that share rows
+  const bool not_finite = part == 0 && any_wave(met, reinterpret_cast<int*>(lds + S::LDS - 16), wave, lane);   // the siblings' part
+  if (not_finite && kg == 0) {   // one of the waves that share rows
     for (int j = 0; j < n; ++j) {
       const bf16_t* v = reinterpret_cast<const bf16_t*>(draft_v) + (size_t)j * ld;
 #pragma unroll
