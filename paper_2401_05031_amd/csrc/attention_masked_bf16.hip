@@ -216,17 +216,26 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
       } else if (!whole) {
         const int* kd = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>() + 256);
         const int left = limit - kb - 4 * fk, early = own_prefix - kb - 4 * fk;
+        const bool beyond = kb >= prefix;   // past the prefix (wave-uniform) the row's document and its limit decide, which is 0 for padding
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int4 d = read_four(kd, b * 8 + 2 * g + fk);
             const int dd[4] = {d.x, d.y, d.z, d.w};
+            if (beyond) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int j = 32 * b + 8 * g + e;
-              const bool see = (j < left) & (dd[e] >= 0) & ((j < early) | (dd[e] == my_doc));
-              s[b][4 * g + e] = see ? s[b][4 * g + e] : -INFINITY;
+              for (int e = 0; e < 4; ++e) {
+                const bool see = (32 * b + 8 * g + e < left) & (dd[e] == my_doc);
+                s[b][4 * g + e] = see ? s[b][4 * g + e] : -INFINITY;
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int j = 32 * b + 8 * g + e;
+                const bool see = (j < left) & (dd[e] >= 0) & ((j < early) | (dd[e] == my_doc));
+                s[b][4 * g + e] = see ? s[b][4 * g + e] : -INFINITY;
+              }
             }
           }
       }
