@@ -14,6 +14,8 @@
  *     entry point says how many it has), else through the context's plan buffer.  Calls of the first kind may be captured into a
  *     HIP graph (their host numbers are part of it); of the second kind they are refused under capture (EUNSUPPORTED), and
  *     limited to 1048576 entries (ENOMEM).
+ *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, attention over very
+ *     many queries of which one is very long (all are given as many workgroups as the longest).
  *   - Results do not depend on the order in which the device happens to run anything.
  */
 #ifndef OTAS_DECODE_H_
@@ -58,7 +60,7 @@ otas_status otas_rotary(otas_ctx *ctx, const void *qkv, int64_t T, int32_t kv_he
  * slopes are given, s - slopes[h] |position_i - position_j|. */
 typedef struct {
   float scale;          /* finite; 0 = 1 / sqrt(d_h) */
-  float cap;            /* finite, >= 0; 0 = none */
+  float cap;            /* finite, >= 0; 0 = none.  bf16 logits are off by up to 1e-6 cap; scale / cap up to 1e38 (EINVAL) */
   const float *slopes;  /* dev [H] or NULL */
 } otas_score_desc;
 
@@ -69,7 +71,7 @@ typedef struct {
  *   documents dev int32 [T] or NULL (a query is one document); a negative number marks padding
  *   positions dev int32 [T] or NULL (i, j themselves): for the distance only; within +- 2^29
  *   score     NULL = all defaults
- *   o         dev [T, D], no overlap with qkv.  A row that sees nothing, or no key of weight, is zero.
+ *   o         dev [T, D], no overlap with any other array.  A row that sees nothing, or no key of weight, is zero.
  * Keys and values that a row does not see do not reach it, infinities and NaN included.
  * Lengths up to OTAS_MAX_LONG_SEQ (EUNSUPPORTED).  Host numbers: 2 B + 1. */
 otas_status otas_attention_masked(otas_ctx *ctx, const void *qkv, int32_t kv_heads, const int32_t *offsets, int32_t B,
@@ -79,7 +81,8 @@ otas_status otas_attention_masked(otas_ctx *ctx, const void *qkv, int32_t kv_hea
 /* A cache: `slots` places for one query each, of `capacity` entries.  An entry is a token's key and value heads, its position
  * and the attention weight that it has gathered.  The caller owns the memory and knows which query has which slot and how many
  * entries of it are filled (they are entries 0 .. length - 1; those behind are neither read nor written, except where a call
- * says so). */
+ * says so).  The four arrays overlap neither each other nor any other array of a call (EINVAL where k and v are one, or the call's
+ * qkv, o or workspace lies in them). */
 typedef struct {
   void *k, *v;         /* dev [slots, kv_heads, capacity, d_h], model dtype */
   int32_t *positions;  /* dev [slots, capacity] */
@@ -108,7 +111,7 @@ otas_status otas_cache_append(otas_ctx *ctx, const otas_kv_cache *cache, const v
  *   add_mass != 0: entry j's mass grows by the weights it got, summed over the query's nodes and all heads (cache->mass required)
  *   workspace dev >= otas_attention_tree_workspace_bytes for the same offsets, length and add_mass, 256-byte aligned.  The bytes
  *   grow with the lengths; with add_mass there may be 4 for every row, head and entry among them
- *   o dev [T, D], no overlap.  A node without a key of weight is zero.   Host numbers: 3 B + 1, with parents T / 4 more.
+ *   o dev [T, D]; o and the workspace overlap no other array.  A node without a key of weight is zero.   Host numbers: 3 B + 1, with parents T / 4 more.
  * The split of a long cache between workgroups, and with it the last bits of o, depends on the whole call's lengths. */
 size_t otas_attention_tree_workspace_bytes(const otas_ctx *ctx, int32_t kv_heads, const int32_t *offsets, const int32_t *length,
                                            int32_t B, int32_t add_mass);

@@ -280,7 +280,7 @@ static hipError_t attention_masked_f32(const void* qkv, const int32_t* plan, siz
                                        int H, int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s) {
   const int xblks = (max_n + 31) / 32;
   const int64_t wgs = (int64_t)xblks * H * B;
-  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  if (wgs > kMostGroups) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   return with_tiles(dh, [&](auto dt, auto whole) {
     constexpr int DT = decltype(dt)::value;
@@ -448,7 +448,7 @@ static hipError_t attention_tree_any(const CacheRef& c, const void* qkv, int H, 
                                      bool add_mass, const TreeShape& shape, float* workspace, void* o, hipStream_t s) {
   const int64_t TH = T_ * H, wgs = (int64_t)B * c.KV * shape.groups * shape.parts;
   const int xblks = (max_len + 31) / 32;
-  if (wgs > INT32_MAX || (TH + 3) / 4 > INT32_MAX || (int64_t)B * xblks > INT32_MAX) return hipErrorInvalidValue;
+  if (wgs > kMostGroups || (TH + 3) / 4 > kMostGroups || (int64_t)B * xblks > kMostGroups) return kTooManyGroups;
   float* ends = workspace;
   float* tops = workspace + 2 * TH;
   float* sums = tops + 2 * TH * shape.parts;

@@ -281,7 +281,7 @@ hipError_t launch_attention_masked_bf16(const void* qkv, const int32_t* plan, si
                                         int KV, int dh, const ScoreArgs& sc, const MaskArgs& mk, void* o, hipStream_t s) {
   const int xblks = (max_n + kRows - 1) / kRows;
   const int64_t wgs = (int64_t)xblks * H * B;
-  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  if (wgs > kMostGroups) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   const int by_xcd = (int64_t)B * H % 8 == 0;
   auto run = [&](auto width, auto cap, auto bias) {

@@ -293,7 +293,7 @@ hipError_t launch_attention_tree_bf16(const CacheRef& c, const void* qkv, int H,
   const int64_t join_wgs = shape.parts > 1 ? (TH + 3) / 4 : 0;
   const bool by_logits = add_mass && shape.rows == 32 && max_len > 0;
   const int xblks = (max_len + 255) / 256, kblks = (max_len + 31) / 32;
-  if (wgs > INT32_MAX || join_wgs + (int64_t)B * kblks > INT32_MAX) return hipErrorInvalidValue;
+  if (wgs > kMostGroups || join_wgs + (int64_t)B * kblks > kMostGroups) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   TreeBuffers buf;
   buf.TH = TH;

@@ -40,6 +40,18 @@ otas_status place_plan(otas_ctx* c, const std::vector<int32_t>& plan) {
   return upload_plan(c, plan);
 }
 
+// A launch of an operator; one of more workgroups than a launch may have is refused.
+#define OTAS_LAUNCH_FITTING(kind, expr)                      \
+  do {                                                       \
+    hipError_t _e;                                           \
+    {                                                        \
+      LaunchTimer _t(c, kind, c->stream);                    \
+      _e = (expr);                                           \
+    }                                                        \
+    if (_e == kTooManyGroups) return OTAS_EUNSUPPORTED;      \
+    OTAS_HIP(_e);                                            \
+  } while (0)
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
@@ -62,6 +74,7 @@ otas_status cache_ok(const otas_ctx* c, const otas_kv_cache* cache) {
   if (!cache || !cache->k || !cache->v || !cache->positions) return OTAS_EINVAL;
   if (cache->slots <= 0 || cache->capacity <= 0 || !kv_heads_ok(c, cache->kv_heads)) return OTAS_EINVAL;
   if (cache->capacity > OTAS_MAX_LONG_SEQ) return OTAS_EUNSUPPORTED;
+  if (cache->k == cache->v) return OTAS_EINVAL;
   if (!aligned16(cache->k) || !aligned16(cache->v) || !aligned4(cache->positions) || !aligned4(cache->mass)) return OTAS_EINVAL;
   return OTAS_OK;
 }
@@ -75,6 +88,12 @@ otas_status slots_ok(const otas_kv_cache* cache, const int32_t* slot, const int3
   }
   return OTAS_OK;
 }
+// Whether an array has a byte in common with the cache's keys or values.  (Sizes past 64 bits are everything.)
+bool in_cache(const otas_ctx* c, const otas_kv_cache* cache, const void* p, size_t bytes) {
+  const double d = (double)cache->slots * cache->kv_heads * cache->capacity * (c->desc.D / c->desc.H) * elem_size(c->desc.dtype);
+  const size_t limit = SIZE_MAX - std::max((uintptr_t)cache->k, (uintptr_t)cache->v), all = d < (double)limit ? (size_t)d : limit;
+  return overlap(p, bytes, cache->k, all) || overlap(p, bytes, cache->v, all);
+}
 CacheRef cache_ref(const otas_ctx* c, const otas_kv_cache* cache) {
   return CacheRef{cache->k, cache->v, cache->positions, cache->mass, cache->capacity, cache->kv_heads, c->desc.D / c->desc.H};
 }
@@ -85,6 +104,9 @@ otas_status score_ok(const otas_ctx* c, const otas_score_desc* score, ScoreArgs*
   if (!std::isfinite(score->scale) || !std::isfinite(score->cap) || score->cap < 0.f || !aligned4(score->slopes)) return OTAS_EINVAL;
   if (score->scale != 0.f) out->scale = score->scale;
   out->cap = score->cap;
+  // The kernels' factors, exp2 in place of exp and tanh by it, have to be finite too.
+  const double scale = std::fabs((double)out->scale), most = 3.4e38;
+  if (scale * 1.5 > most || (score->cap > 0.f && (score->cap * 1.5 > most || scale / score->cap * 3.0 > most))) return OTAS_EINVAL;
   out->slopes = score->slopes;
   return OTAS_OK;
 }
@@ -159,7 +181,7 @@ otas_status otas_rotary(otas_ctx* c, const void* qkv, int64_t T, int32_t kv_head
     if (T == 0 || (out == qkv && d.rot_dim == 0)) return OTAS_OK;
     OnDevice on(c);
     if (!on.ok) return OTAS_EDEVICE;
-    OTAS_LAUNCH(K_MISC, launch_rotary(c->desc.dtype, qkv, out, positions, T, c->desc.H, kv_heads, dh, r, c->stream));
+    OTAS_LAUNCH_FITTING(K_MISC, launch_rotary(c->desc.dtype, qkv, out, positions, T, c->desc.H, kv_heads, dh, r, c->stream));
     return OTAS_OK;
   });
 }
@@ -191,7 +213,7 @@ otas_status otas_attention_masked(otas_ctx* c, const void* qkv, int32_t kv_heads
     if (!on.ok) return OTAS_EDEVICE;
     const otas_status placed = place_plan(c, plan);
     if (placed != OTAS_OK) return placed;
-    OTAS_LAUNCH(K_ATTN, launch_attention_masked(c->desc.dtype, qkv, plan.data(), plan.size(), c->d_plan, B, max_n, c->desc.H, kv_heads,
+    OTAS_LAUNCH_FITTING(K_ATTN, launch_attention_masked(c->desc.dtype, qkv, plan.data(), plan.size(), c->d_plan, B, max_n, c->desc.H, kv_heads,
                                                 c->desc.D / c->desc.H, sc, MaskArgs{documents, positions, causal != 0}, o, c->stream));
     return OTAS_OK;
   });
@@ -205,7 +227,7 @@ otas_status otas_cache_append(otas_ctx* c, const otas_kv_cache* cache, const voi
     otas_status st = cache_ok(c, cache);
     if (st != OTAS_OK) return st;
     if (!aligned16(qkv) || !aligned4(positions) || !offsets_ok(row_offsets, B)) return OTAS_EINVAL;
-    if (row_offsets[B] > 0 && (!qkv || !positions)) return OTAS_EINVAL;
+    if (row_offsets[B] > 0 && (!qkv || !positions || in_cache(c, cache, qkv, qkv_bytes(c, T, cache->kv_heads)))) return OTAS_EINVAL;
     st = slots_ok(cache, slot, length, B, true);
     if (st != OTAS_OK) return st;
     const int64_t N = row_offsets[B];
@@ -288,7 +310,8 @@ otas_status otas_attention_tree(otas_ctx* c, const otas_kv_cache* cache, const v
     if (T > 0 && workspace_bytes < floats * sizeof(float)) return OTAS_ENOMEM;
     const size_t in_bytes = qkv_bytes(c, T, cache->kv_heads), out_bytes = rows_bytes(c, T);
     if (overlap(qkv, in_bytes, o, out_bytes) || overlap(workspace, floats * sizeof(float), o, out_bytes) ||
-        overlap(workspace, floats * sizeof(float), qkv, in_bytes))
+        overlap(workspace, floats * sizeof(float), qkv, in_bytes) || in_cache(c, cache, o, out_bytes) ||
+        in_cache(c, cache, workspace, floats * sizeof(float)))
       return OTAS_EINVAL;
     std::vector<int32_t> plan(3 * (size_t)B + 1 + (chains ? 0 : (size_t)(T + 3) / 4), 0);
     std::copy(offsets, offsets + B + 1, plan.begin());
@@ -302,7 +325,7 @@ otas_status otas_attention_tree(otas_ctx* c, const otas_kv_cache* cache, const v
     if (!on.ok) return OTAS_EDEVICE;
     st = place_plan(c, plan);
     if (st != OTAS_OK) return st;
-    OTAS_LAUNCH(K_ATTN, launch_attention_tree(c->desc.dtype, cache_ref(c, cache), qkv, c->desc.H, positions, plan.data(), plan.size(), c->d_plan,
+    OTAS_LAUNCH_FITTING(K_ATTN, launch_attention_tree(c->desc.dtype, cache_ref(c, cache), qkv, c->desc.H, positions, plan.data(), plan.size(), c->d_plan,
                                               B, T, max_len, !chains, sc, add_mass != 0, shape, (float*)workspace, o, c->stream));
     return OTAS_OK;
   });
@@ -346,6 +369,7 @@ otas_status otas_cache_evict(otas_ctx* c, const otas_kv_cache* cache, const int3
       max_moves = std::max(max_moves, moves);
     }
     if (workspace_bytes < ((size_t)B + at) * sizeof(int32_t)) return OTAS_ENOMEM;
+    if (in_cache(c, cache, workspace, ((size_t)B + at) * sizeof(int32_t))) return OTAS_EINVAL;
     if (max_moves > 0) {
       OnDevice on(c);
       if (!on.ok) return OTAS_EDEVICE;

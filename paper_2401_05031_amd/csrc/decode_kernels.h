@@ -9,6 +9,11 @@
 
 namespace otas {
 
+// Workgroups of 256 threads that one launch may have (its threads are counted in 32 bits), and what a launcher returns, with nothing
+// launched, for a call of more.
+constexpr int64_t kMostGroups = UINT32_MAX / 256;
+constexpr hipError_t kTooManyGroups = hipErrorInvalidConfiguration;
+
 struct RotaryArgs {
   double turns[64];   // full turns per position of every pair (negative: the inverse)
   float magnitude;

@@ -131,7 +131,7 @@ hipError_t launch_rotary(int dtype, const void* qkv, void* out, const int32_t* p
   // Rows per workgroup: angles of several rows keep all threads busy, but a small call wants its rows on many CUs.
   const int tokens = T >= 8192 ? 8 : T >= 2048 ? 4 : T >= 1024 ? 2 : 1;
   const int64_t wgs = (T + tokens - 1) / tokens;
-  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  if (wgs > kMostGroups) return kTooManyGroups;
   const int wide = dtype == 0 ? 4 : 8;
   const int v = dh % wide ? 4 : wide;   // dh % 4 == 0
 #define OTAS_ROTARY(T_, V_)                                                                                                     \

@@ -95,6 +95,11 @@ int main() {
     }
     otas_score_desc t = {NAN, 0.f, nullptr};
     IS(OTAS_EINVAL, otas_attention_masked(c, qkv, 2, off, 3, 1, nullptr, nullptr, nullptr, &t, o));
+    // factors that the kernels could not hold
+    const otas_score_desc extremes[] = {{3e38f, 0.f, nullptr}, {0.f, 3e38f, nullptr}, {1.f, 1e-40f, nullptr}, {-3e38f, 0.f, nullptr}, {1e30f, 1e-20f, nullptr}};
+    for (const otas_score_desc& x : extremes) IS(OTAS_EINVAL, otas_attention_masked(c, qkv, 2, off, 3, 1, nullptr, nullptr, nullptr, &x, o));
+    const otas_score_desc wide[] = {{-2e38f, 0.f, nullptr}, {1e-30f, 1e30f, nullptr}, {1.f, 1e-37f, nullptr}};
+    for (const otas_score_desc& x : wide) IS(OTAS_OK, otas_attention_masked(c, qkv, 2, off, 3, 1, nullptr, nullptr, nullptr, &x, o));
     const int32_t longer[] = {0, OTAS_MAX_LONG_SEQ + 1}, longest[] = {0, OTAS_MAX_LONG_SEQ};
     IS(OTAS_EUNSUPPORTED, otas_attention_masked(c, qkv, 2, longer, 1, 1, nullptr, nullptr, nullptr, nullptr, o));
     IS(OTAS_OK, otas_attention_masked(c, qkv, 2, longest, 1, 1, nullptr, nullptr, nullptr, nullptr, o));
@@ -124,6 +129,23 @@ int main() {
     IS(OTAS_EINVAL, otas_cache_append(c, &no_pos, qkv, 8, roff, rows, pos, slot, len, 3, out));
     IS(OTAS_EUNSUPPORTED, otas_cache_append(c, &huge, qkv, 8, roff, rows, pos, slot, len, 3, out));
     IS(OTAS_OK, otas_cache_append(c, &no_mass, qkv, 8, roff, rows, pos, slot, len, 3, out));
+
+    // arrays of a call within the cache; the cache's two arrays in one
+    const size_t held = (size_t)600 * 2 * 100 * 64 * (dtype == OTAS_F32 ? 4 : 2);
+    const otas_kv_cache one = cache_but([](auto& x) { x.v = x.k; });
+    IS(OTAS_EINVAL, otas_cache_append(c, &one, qkv, 8, roff, rows, pos, slot, len, 3, out));
+    for (char* in : {(char*)k.k, (char*)k.v}) {
+      IS(OTAS_EINVAL, otas_cache_append(c, &k, in, 8, roff, rows, pos, slot, len, 3, out));
+      IS(OTAS_EINVAL, otas_cache_append(c, &k, in + held - 256, 8, roff, rows, pos, slot, len, 3, out));
+      IS(OTAS_OK, otas_cache_append(c, &k, in + held, 8, roff, rows, pos, slot, len, 3, out));
+      IS(OTAS_EINVAL, otas_attention_tree(c, &k, qkv, off, nullptr, nullptr, slot, len, 3, nullptr, 0, in + 256, (size_t)1 << 30, o));
+      IS(OTAS_EINVAL, otas_attention_tree(c, &k, qkv, off, nullptr, nullptr, slot, len, 3, nullptr, 0, ws, (size_t)1 << 30, in - 256));
+      const int32_t half[] = {50, 0, 20};
+      IS(OTAS_EINVAL, otas_cache_evict(c, &k, slot, len, half, 3, 0, nullptr, in, (size_t)1 << 30, out));
+    }
+    const otas_kv_cache endless = cache_but([](auto& x) { x.slots = INT32_MAX; x.capacity = OTAS_MAX_LONG_SEQ; });
+    IS(OTAS_EINVAL, otas_cache_append(c, &endless, (char*)k.k + (1ull << 50), 8, roff, rows, pos, slot, len, 3, out));
+    IS(OTAS_OK, otas_cache_append(c, &endless, qkv, 8, roff, rows, pos, slot, len, 3, out));
 
     const int32_t parents[] = {-1, 0, 0, -1, 0, 1, 2, 3}, chain[] = {-1, 0, 1, -1, 0, 1, 2, 3};
     size_t need = otas_attention_tree_workspace_bytes(c, 2, off, len, 3, 1);

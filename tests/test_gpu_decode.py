@@ -594,3 +594,204 @@ def test_calls_that_the_binding_refuses(lib):
         with pytest.raises(lib.OtasError) as e:
             call()
         assert e.value.status == status, call
+
+
+# ------------------------------------------------------------------------------------- calls at the edges of the header
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype,H,KV,dh,T,rot", [("bf16", 4, 2, 128, 8203, 122), ("bf16", 3, 1, 64, 300, 58), ("bf16", 2, 2, 80, 1030, 2), ("bf16", 5, 5, 8, 70, 6),
+                                                 ("bf16", 2, 1, 100, 17, 98), ("bf16", 4, 4, 96, 2050, 72), ("f32", 4, 1, 128, 8200, 126), ("f32", 2, 2, 68, 9, 66),
+                                                 ("f32", 4, 2, 4, 1100, 2)])
+def test_rotary_halves_that_no_chunk_divides(lib, dtype, H, KV, dh, T, rot, in_place):
+    import torch
+    ctx, g = context(dtype, H, dh), gen(T + rot)
+    qkv = normal(g, (T, (H + 2 * KV) * dh), dtype)
+    pos = torch.randint(0, 2 ** 17, (T,), generator=g, device="cuda", dtype=torch.int32)
+    want, bound = plain.rotary(qkv, H, KV, pos, rot, False, plain.frequencies(rot))
+    src = qkv.clone()
+    out = src if in_place else torch.empty_like(qkv)
+    ctx.otas_rotary(src, KV, pos, lib.Rotary(rot), out)
+    within(out, want, bound + 1e-6 * (2.0 ** 17 * 2.0 ** -52 * 6.3), "rotary")
+    assert in_place or torch.equal(src, qkv)
+    kept = torch.ones((H + 2 * KV, dh), dtype=torch.bool, device="cuda")
+    kept[:H + KV, :rot] = False
+    assert torch.equal(out.view(T, -1, dh)[:, kept], qkv.view(T, -1, dh)[:, kept])
+
+
+@pytest.mark.parametrize("scale", [-0.25, 0.03125, 1.5])
+@pytest.mark.parametrize("dtype,H,KV,dh,cap,slopes", [("f32", 2, 1, 64, 0.0, True), ("f32", 2, 1, 36, 3.0, False), ("bf16", 2, 1, 64, 0.0, False), ("bf16", 2, 2, 80, 0.0, True),
+                                                      ("bf16", 4, 1, 128, 20.0, False), ("bf16", 2, 1, 96, 5.0, True)])
+def test_scales_of_either_sign(lib, dtype, H, KV, dh, cap, slopes, scale):
+    import torch
+    ctx, g, off = context(dtype, H, dh), gen(int(scale * 64) + dh), [0, 150, 331]
+    qkv = normal(g, (331, (H + 2 * KV) * dh), dtype)
+    sl = slopes_of(H) if slopes else None
+    score = lib.Score(scale=scale, cap=cap, slopes=sl)
+    o = torch.empty((331, H * dh), dtype=qkv.dtype, device="cuda")
+    ctx.otas_attention_masked(qkv, KV, off, o, prefix=[3, 100], score=score)
+    within(o, *plain.masked(qkv, H, KV, off, True, [3, 100], None, None, scale, cap, sl), "masked")
+    cache = new_cache(lib, g, dtype, 2, KV, 420, dh)
+    before = clone_cache(lib, cache)
+    for nodes in (1, 20):                               # a few rows of a key head, and many
+        rows, doff, cached = qkv[:2 * nodes].contiguous(), [0, nodes, 2 * nodes], [400, 129]
+        pos = torch.arange(850, 850 + 2 * nodes, device="cuda", dtype=torch.int32)
+        ws = torch.empty(ctx.otas_attention_tree_workspace_bytes(KV, doff, cached, add_mass=True), dtype=torch.uint8, device="cuda")
+        o = torch.empty((2 * nodes, H * dh), dtype=qkv.dtype, device="cuda")
+        cache.mass.copy_(before.mass)
+        ctx.otas_attention_tree(cache, rows, doff, None, pos, [1, 0], cached, ws, o, score=score, add_mass=True)
+        w, b, grown, gb = plain.tree(rows, H, cache.k, cache.v, cache.positions, before.mass, doff, None, pos, [1, 0], cached, scale, cap, sl)
+        within(o, w, b, "tree")
+        for q, s in enumerate((1, 0)):
+            within(cache.mass[s, :cached[q]], grown[s, :cached[q]], gb[s, :cached[q]] + 1e-30, "mass")
+
+
+@pytest.mark.parametrize("dtype,H,KV,dh", [("f32", 2, 1, 64), ("bf16", 8, 2, 64), ("bf16", 3, 3, 80)])
+def test_more_queries_than_the_arguments_hold(lib, dtype, H, KV, dh):
+    """Their numbers go through the plan buffer: lengths of zero to a few, in one call of each operator."""
+    import torch
+    ctx, g, rng = context(dtype, H, dh), gen(31), np.random.default_rng(31)
+    B, capacity = 1001, 90
+    lens = [int(x) for x in rng.integers(0, 6, B)]
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    T = int(off[-1])
+    qkv = normal(g, (T, (H + 2 * KV) * dh), dtype)
+    prefix = [int(rng.integers(0, n + 1)) for n in lens]
+    o = torch.empty((T, H * dh), dtype=qkv.dtype, device="cuda")
+    ctx.otas_attention_masked(qkv, KV, off, o, prefix=prefix)
+    within(o, *plain.masked(qkv, H, KV, off, True, prefix), "masked")
+    cache = new_cache(lib, g, dtype, B, KV, capacity, dh)
+    slots, cached = [int(s) for s in rng.permutation(B)], [int(x) for x in rng.integers(0, capacity - 6, B)]
+    parents = sum([tree_of(rng, n, "roots") for n in lens], [])
+    before = clone_cache(lib, cache)
+    ws = torch.empty(ctx.otas_attention_tree_workspace_bytes(KV, off, cached, add_mass=True), dtype=torch.uint8, device="cuda")
+    ctx.otas_attention_tree(cache, qkv, off, parents, None, slots, cached, ws, o, add_mass=True)
+    w, b, grown, gb = plain.tree(qkv, H, before.k, before.v, before.positions, before.mass, off, parents, None, slots, cached)
+    within(o, w, b, "tree")
+    filled = torch.zeros((B, capacity), dtype=torch.bool, device="cuda")
+    for q in range(B):
+        filled[slots[q], :cached[q]] = True
+    within(cache.mass[filled], grown[filled], gb[filled] + 1e-30, "mass")
+    assert torch.equal(cache.mass[~filled], before.mass[~filled])
+    pos = torch.arange(T, device="cuda", dtype=torch.int32)
+    now = ctx.otas_cache_append(cache, qkv, off, None, pos, slots, cached).tolist()
+    q = int(np.argmax(lens))
+    assert torch.equal(cache.v[slots[q], KV - 1, cached[q]:now[q]], qkv.view(T, H + 2 * KV, dh)[off[q]:off[q + 1], H + 2 * KV - 1])
+    keep = [n // 2 for n in now]
+    want = clone_cache(lib, cache)
+    for q, (to, src) in enumerate(plain.evict(cache.mass, cache.positions, slots, now, keep, 1, None)):
+        s = slots[q]
+        want.k[s][:, to], want.v[s][:, to] = want.k[s][:, src], want.v[s][:, src]
+        want.positions[s][to], want.mass[s][to] = want.positions[s][src], want.mass[s][src]
+    ws = torch.empty(ctx.otas_cache_evict_workspace_bytes(now, keep), dtype=torch.uint8, device="cuda")
+    assert ctx.otas_cache_evict(cache, slots, now, keep, ws, lead=1).tolist() == keep and same_cache(cache, want)
+
+
+@pytest.mark.parametrize("dtype,dh,slopes,cap,n", [("bf16", 64, True, 0.0, 4500), ("bf16", 80, False, 20.0, 4200), ("f32", 64, False, 0.0, 1900)])
+def test_long_rows_of_documents(lib, dtype, dh, slopes, cap, n):
+    """More tiles than a wave looks at at once; documents that come back, that end inside a wave's rows and that no row of a wave
+    has; a prefix that ends inside a tile; padding in the middle and behind the last."""
+    import torch
+    ctx, g = context(dtype, 2, dh), gen(n)
+    d = torch.cat([torch.full((k,), i, dtype=torch.int32) for k, i in ((700, 5), (301, 2), (17, -1), (500, 5), (n - 1518 - 133, 9), (133, -7))]).cuda()
+    off, prefix = [0, n, n + 70], [77, 0]
+    d = torch.cat([d, torch.zeros(70, dtype=torch.int32, device="cuda")])
+    qkv = normal(g, (n + 70, 4 * dh), dtype)
+    sl = slopes_of(2) if slopes else None
+    for causal in (True, False):
+        o = torch.empty((n + 70, 2 * dh), dtype=qkv.dtype, device="cuda")
+        ctx.otas_attention_masked(qkv, 1, off, o, causal=causal, prefix=prefix, documents=d, score=lib.Score(cap=cap, slopes=sl))
+        want, bound = plain.masked(qkv, 2, 1, off, causal, prefix, d, None, None, cap, sl)
+        within(o, want, bound, "documents")
+        assert bool((o[d < 0] == 0).all())
+
+
+def test_offsets_beyond_32_bits(lib):
+    """Slots and rows more than 2^31 elements into their arrays: what the same numbers give at the front."""
+    import torch
+    H, KV, dh, capacity, slots = 4, 2, 128, 1 << 20, 9
+    ctx, g = context("bf16", H, dh), gen(3)
+    assert (slots - 1) * KV * capacity * dh >= 2 ** 31
+    far = lib.KVCache(*(torch.empty((slots, KV, capacity, dh), dtype=torch.bfloat16, device="cuda") for _ in range(2)),
+                      torch.empty((slots, capacity), dtype=torch.int32, device="cuda"), torch.zeros((slots, capacity), device="cuda"))
+    n, W = 3000, (H + 2 * KV) * dh
+    T = 2 ** 31 // W + 40
+    qkv = torch.empty((T, W), dtype=torch.bfloat16, device="cuda")
+    rows = normal(g, (40, W), "bf16")
+    qkv[-40:] = rows
+    pos = torch.arange(T, device="cuda", dtype=torch.int32)
+    out = torch.empty_like(rows)
+    ctx.otas_rotary(rows, KV, pos[-40:].contiguous(), lib.Rotary(122), out)
+    ctx.otas_rotary(qkv, KV, pos, lib.Rotary(122), qkv)
+    assert torch.equal(qkv[-40:], out)
+    near = lib.KVCache(normal(g, (1, KV, n + 40, dh), "bf16"), normal(g, (1, KV, n + 40, dh), "bf16"), pos[:n + 40].view(1, -1).clone(),
+                       torch.rand((1, n + 40), generator=g, device="cuda"))
+    base = capacity - n - 40                            # entries up to the last one that a slot holds
+    for a, b in ((far.k, near.k), (far.v, near.v)):
+        a[8, :, :n + 40] = b[0]
+    far.positions[8, :n + 40], far.mass[8, :n + 40] = near.positions[0], near.mass[0]
+    r = list(range(T - 40, T))
+    assert ctx.otas_cache_append(far, qkv, [0, 40], r, pos, [8], [n]).tolist() == [n + 40]
+    ctx.otas_cache_append(near, out, [0, 40], None, pos[-40:].contiguous(), [0], [n])
+    assert torch.equal(far.k[8, :, :n + 40], near.k[0]) and torch.equal(far.positions[8, :n + 40], near.positions[0])
+    ctx.otas_cache_append(far, qkv, [0, 40], r, pos, [8], [base + n])
+    assert torch.equal(far.v[8, :, -40:], near.v[0, :, n:])
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    o = [torch.empty((12, H * dh), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for i, (c, s) in enumerate(((far, 8), (near, 0))):
+        ctx.otas_attention_tree(c, out[:12].contiguous(), [0, 12], None, None, [s], [n + 40], ws, o[i], add_mass=True)
+        assert ctx.otas_cache_evict(c, [s], [n + 40], [n - 500], ws, lead=4).tolist() == [n - 500]
+    assert torch.equal(o[0], o[1]) and torch.equal(far.mass[8, :n - 500], near.mass[0, :n - 500])
+    assert torch.equal(far.k[8, :, :n - 500], near.k[0, :, :n - 500]) and torch.equal(far.v[8, :, :n - 500], near.v[0, :, :n - 500])
+
+
+def test_graphs_that_share_a_workspace(lib):
+    """Two captured trees of different shapes with one workspace, replayed in turn with an eager call between them."""
+    import torch
+    import paper_2401_05031_amd as otas
+    H, KV, dh = 4, 2, 64
+    stream = torch.cuda.Stream()
+    cfg = synth.Config("graphs", L=1, D=H * dh, H=H, F=64, dtype="bf16", B=1, n0=4, strategies=[(0, 0)], seed=5)
+    ctx = otas.Context.from_host_weights(1, H * dh, H, 64, otas.OTAS_BF16, 1e-6, 1, synth.all_weights(cfg), stream=stream.cuda_stream)
+    g = gen(21)
+    cache = new_cache(lib, g, "bf16", 3, KV, 2000, dh)
+    mass = cache.mass.clone()
+    calls = []
+    for off, slots, cached in (([0, 1, 2], [0, 2], [2000, 900]), ([0, 33, 40], [1, 0], [700, 1999]), ([0, 4], [2], [0])):
+        qkv = normal(g, (off[-1], (H + 2 * KV) * dh), "bf16")
+        calls.append((off, slots, cached, qkv, torch.empty((off[-1], H * dh), dtype=qkv.dtype, device="cuda")))
+    ws = torch.empty(max(ctx.otas_attention_tree_workspace_bytes(KV, c[0], c[2], add_mass=True) for c in calls), dtype=torch.uint8, device="cuda")
+
+    def run(c):
+        ctx.otas_attention_tree(cache, c[3], c[0], None, None, c[1], c[2], ws, c[4], add_mass=True)
+    want = []
+    for c in calls:
+        cache.mass.copy_(mass)
+        torch.cuda.synchronize()
+        run(c)
+        torch.cuda.synchronize()
+        want.append((c[4].clone(), cache.mass.clone()))
+    graphs = []
+    for c in calls[:2]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            run(c)
+    for turn in range(3):
+        for i, go in ((0, graphs[0].replay), (1, graphs[1].replay), (2, lambda: run(calls[2])), (1, graphs[1].replay)):
+            cache.mass.copy_(mass)
+            calls[i][4].fill_(9.0)
+            ws.fill_(255)
+            torch.cuda.synchronize()
+            go()
+            torch.cuda.synchronize()
+            assert torch.equal(calls[i][4], want[i][0]) and torch.equal(cache.mass, want[i][1]), (turn, i)
+    ctx.close()
+
+
+def test_refusals_of_very_wide_calls(lib):
+    import torch
+    ctx = context("bf16", 16, 64)
+    n = 300000
+    qkv, o = torch.empty((n, 18 * 64), dtype=torch.bfloat16, device="cuda"), torch.empty((n, 1024), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(lib.OtasError) as e:             # 900 x 16 x 2344 row blocks of 128, nearly all of them empty
+        ctx.otas_attention_masked(qkv, 1, [0] + [n] * 900, o)
+    assert e.value.status == 5
+    ctx.otas_attention_masked(qkv[:5].contiguous(), 1, [0] + [5] * 900, o[:5].contiguous())
