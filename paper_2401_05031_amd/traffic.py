@@ -25,7 +25,7 @@ FAMILIES = {
 # decoder's kernels around its cache (its attention counts as attention).
 REST = ("prepend_kernel", "deep_prompt_kernel", "patchify_kernel", "embed_finish_kernel", "task_head_kernel",
         "fill_i32_kernel", "copy_i32_kernel", "spin_kernel", "clock_probe_kernel",
-        "rotary_kernel", "cache_append_kernel", "cache_evict_select_kernel", "cache_evict_move_kernel")
+        "rotary_kernel", "rotary_odd_halves_kernel", "cache_append_kernel", "cache_evict_select_kernel", "cache_evict_move_kernel")
 DEFAULT_OUT = os.path.join(os.path.dirname(os.path.abspath(__file__)), "hbm_traffic.json")
 
 
