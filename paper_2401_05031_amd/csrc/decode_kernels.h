@@ -52,25 +52,50 @@ hipError_t launch_attention_masked_bf16(const void* qkv, const int32_t* plan, si
 
 // How a call of the tree attention is cut up (pure host).  A workgroup has up to `rows` of the nodes x (H / KV) rows of a key
 // head, and `chunk` of the cache's entries; `parts` = most chunks of a query.
+//   A chunk costs its workgroup some 6 us before the first product and a share of the join afterwards, and too few leave CUs without
+// work.  Rows of 64 and 128 and fp32: as many parts as bring the call to 512 and 1024 workgroups (8 x 48 nodes over 4000: 42 us, 54 with
+// 1024).  bf16 and 32 rows or fewer: one part up to 384 entries (no join: 24 queries over 300 17.7 -> 14.2 us); blocks of 128
+// entries while that makes no more workgroups than CUs; a workgroup per CU where
+// that leaves 512 entries or fewer to each (8 queries over 6000, 2 key heads: 19 us; 27 with blocks of 128); else 384 entries or more and up to
+// 768 workgroups, which are counted from every query's own length: the longest query's many parts leave nothing to do for those of
+// shorter queries (24 queries of 400 .. 8000: 105 -> 96 us; with weights added up 125 -> 115).
 struct TreeShape {
   int rows, groups, chunk, parts, room;   // room: what the workspace has place for; >= parts, and grows with the lengths
 };
 inline TreeShape tree_shape(int dtype, int dh, int H, int KV, const int32_t* off, const int32_t* length, int B) {
   TreeShape t{32, 1, 0, 1, 1};
-  int most = 0, longest = 0;
+  int64_t most = 0, longest = 0;
   for (int q = 0; q < B; ++q) {
-    most = std::max(most, off[q + 1] - off[q]);
-    longest = std::max(longest, (int)length[q]);
+    most = std::max<int64_t>(most, off[q + 1] - off[q]);
+    longest = std::max<int64_t>(longest, length[q]);
   }
-  const int rows = most * (H / KV);
-  if (dtype != 0 && bf16_width(dh)) t.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-  t.groups = std::max(1, (rows + t.rows - 1) / t.rows);
-  const int64_t wgs = (int64_t)B * KV * t.groups;
-  const int target = t.rows > 32 ? 512 : 1024;
-  const int wanted = (int)std::max<int64_t>(1, std::min<int64_t>(target / wgs, (longest + 127) / 128));
-  t.chunk = std::max(128, ((longest + wanted - 1) / wanted + 127) & ~127);
-  t.parts = std::max(1, (longest + t.chunk - 1) / t.chunk);
-  t.room = wanted;
+  const bool bf16 = dtype != 0 && bf16_width(dh);
+  const int64_t rows = most * (H / KV);
+  if (bf16) t.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  t.groups = (int)std::max<int64_t>(1, (rows + t.rows - 1) / t.rows);
+  const bool few = bf16 && t.rows == 32;
+  const int64_t wgs = (int64_t)B * KV * t.groups, target = few ? 768 : t.rows > 32 ? 512 : 1024;
+  auto pieces = [](int64_t n, int64_t of) { return std::max<int64_t>(1, (n + of - 1) / of); };
+  auto whole = [](int64_t n) { return std::max<int64_t>(128, (n + 127) & ~127); };
+  int64_t least = 128;
+  if (few && longest <= 384) {
+    least = 384;
+  } else if (few && wgs * pieces(longest, 128) > 256) {
+    const int64_t each = pieces(longest, std::max<int64_t>(1, 256 / wgs));
+    least = wgs <= 256 && each <= 512 ? whole(each) : 384;
+  }
+  const int64_t wanted = std::max<int64_t>(1, std::min(target / wgs, pieces(longest, least)));
+  int64_t chunk = whole(pieces(longest, wanted));
+  if (few && wanted > 1) {   // the smallest chunk, down to half of that, that keeps to the target
+    for (int64_t c = std::max(least, whole(pieces(longest, 2 * wanted))); c < chunk; c += std::max<int64_t>(128, c / 8 & ~127)) {
+      int64_t used = 0;
+      for (int q = 0; q < B; ++q) used += pieces(length[q], c);
+      if (used * KV <= target) chunk = c;   // ends the loop
+    }
+  }
+  t.chunk = (int)chunk;
+  t.parts = (int)pieces(longest, chunk);
+  t.room = (int)std::max<int64_t>(1, std::min((few ? 2 : 1) * (target / wgs), pieces(longest, 128)));
   return t;
 }
 // Floats of workspace: ends [T H][2]; where there is room for more than one part, for each largest logits and weight sums [T H][2]
