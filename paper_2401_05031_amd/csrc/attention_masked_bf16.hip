@@ -216,7 +216,9 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
       } else if (!whole) {
         const int* kd = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>() + 256);
         const int left = limit - kb - 4 * fk, early = own_prefix - kb - 4 * fk;
-        const bool beyond = kb >= prefix;   // past the prefix (wave-uniform) the row's document and its limit decide, which is 0 for padding
+        // Past the prefix (wave-uniform) the row's document and its limit decide, which is 0 for padding (2 x 4000 with five documents, width 64:
+        // 57 -> 54 us).  At 128 the second form's registers do not fit, and it gave nothing there.
+        const bool beyond = DH < 128 && kb >= prefix;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
