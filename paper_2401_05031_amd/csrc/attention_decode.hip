@@ -1,5 +1,5 @@
 // Attention of the decoder's operators with fp32 products (f32 models, and bf16 ones of head widths that the kernels of
-// attention_decode_bf16.hip are not built for):
+// attention_masked_bf16.hip and attention_tree_bf16.hip are not built for):
 //   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = exp(s_ij - max_j s_ij) over the keys j that row i sees,
 // in one pass over the keys with the running maximum and sum of the softmax.  All arithmetic is fp32, on
 // v_mfma_f32_32x32x2_f32 for both products; bf16 operands are widened.
@@ -236,7 +236,9 @@ template <typename T> struct PackedKeys {
   __device__ bool partial(int kb) const { return documents || kb + 32 > full; }
 };
 
-// Four waves have 32 rows of a head between them and take the key blocks in turn.
+// Four waves have 32 rows of a head between them and take the key blocks in turn: a short query of few heads then still has a
+// wave for every SIMD.  8 queries of 209 .. 261 rows behind a prefix of 197, 12 heads of 64: 29 us, where the products alone would
+// take 8 (756 workgroups of two or three blocks of keys a wave, 3 us before the first; 16 of them find no room in the first round).
 template <typename T, int DT, bool WHOLE>
 __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_masked_f32_kernel(const T* __restrict__ qkv, PlanAny plan, int B, int H, int KV, int width, int xblks,
                                                                    ScoreArgs sc, MaskArgs mk, T* __restrict__ o) {

@@ -1,5 +1,11 @@
 // otas_attention_masked in bf16: four waves have 128 rows of a head and walk the keys that any of them sees in tiles of 64, which
 // travel from global memory into the one LDS buffer while the other is worked on; one barrier a tile.
+//   Two workgroups, eight waves, fill a CU's registers (2 a SIMD; 3 would spill from width 80 on and gave nothing at 64).  128 rows read
+// a tile once for four waves; with 64 keys a tile is as large as two buffers and two workgroups leave room for.  Bound by the vector
+// ALU, 10 instructions a logit beside 1 / 8 of a matrix instruction, at a clock of 1.9 - 2.0 GHz: 8192 capped causal rows of 16 heads of
+// 128 in 330 us, 0.83 PFLOP/s where a large matrix product reaches 1.27; 5000 rows of 16 heads of 80 without a cap 114 us (0.56).
+// 3 x 4000 rows of seven documents with slopes take 95 us: a workgroup has 7 tiles of 2.3 us each (3.5 where keys are masked) after
+// 5 us for its plan, the kinds of tiles and the first tile.
 #include "attention_tiles.h"
 
 namespace otas {
