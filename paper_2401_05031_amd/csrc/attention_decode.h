@@ -80,6 +80,9 @@ inline hipError_t with_tiles(int dh, F f) {
   return hipErrorInvalidValue;
 }
 
+// What sums relative to m count relative to top >= m.  Nothing of weight so far (m = -inf): they are 0, or NaN where a logit was, and stay.
+__device__ __forceinline__ float to_top(float m, float top) { return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top); }
+
 // A 64-bit value of lane `from`.
 __device__ inline uint64_t lane_value(uint64_t v, int from) {
   const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, from), hi = (uint32_t)__shfl((int)(uint32_t)(v >> 32), from);

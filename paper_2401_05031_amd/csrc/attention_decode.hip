@@ -165,7 +165,7 @@ __device__ __forceinline__ void rows_join(const FloatRows<T, DT>& r, int dh, flo
   float m_all = -INFINITY;
 #pragma unroll
   for (int w = 0; w < 4; ++w) m_all = fmaxf(m_all, ml[w * 64 + fr]);
-  const float k = r.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r.m - m_all);
+  const float k = to_top(r.m, m_all);
   float* mine = osh + (wave * 32 + fr) * LDO;
 #pragma unroll
   for (int t = 0; t < DT; ++t)
@@ -179,8 +179,7 @@ __device__ __forceinline__ void rows_join(const FloatRows<T, DT>& r, int dh, flo
 #pragma unroll
   for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 64 + row]);
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
-    if (ml[w * 64 + row] != -INFINITY) l += ml[w * 64 + 32 + row] * __builtin_amdgcn_exp2f(ml[w * 64 + row] - m);
+  for (int w = 0; w < 4; ++w) l += ml[w * 64 + 32 + row] * to_top(ml[w * 64 + row], m);
   for (int d = (tid & 7) * 4; d < dh; d += 32) {
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

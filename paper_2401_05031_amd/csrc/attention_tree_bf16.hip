@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
     float top = -INFINITY;
 #pragma unroll
     for (int k = 0; k < KG; ++k) top = fmaxf(top, ml[(k * RW + rw) * 64 + fr]);
-    const float f = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - top);
+    const float f = to_top(w.m, top);
     float* mine = osh + (wave * 32 + fr) * S::LDO;
 #pragma unroll
     for (int t = 0; t < WaveRows<DH>::DT; ++t)
@@ -222,10 +222,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
 #pragma unroll
     for (int k = 0; k < KG; ++k) m = fmaxf(m, ml[(k * RW + rb) * 64 + ri]);
 #pragma unroll
-    for (int k = 0; k < KG; ++k) {
-      const float mk = ml[(k * RW + rb) * 64 + ri];
-      if (mk != -INFINITY) l += ml[(k * RW + rb) * 64 + 32 + ri] * __builtin_amdgcn_exp2f(mk - m);
-    }
+    for (int k = 0; k < KG; ++k) l += ml[(k * RW + rb) * 64 + 32 + ri] * to_top(ml[(k * RW + rb) * 64 + ri], m);
     for (int d = (tid % TPR) * 4; d < DH; d += 4 * TPR) {
       floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

@@ -16,10 +16,9 @@ __device__ __forceinline__ float2 join_ends(const float* tops, int64_t TH, int64
     float top = m;
 #pragma unroll
     for (int i = 0; i < 4; ++i) top = fmaxf(top, e[i].x);
-    const float ref = top == -INFINITY ? 0.f : top;
-    l *= __builtin_amdgcn_exp2f(m - ref);
+    l *= to_top(m, top);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) l += p0 + i < parts ? e[i].y * __builtin_amdgcn_exp2f(e[i].x - ref) : 0.f;
+    for (int i = 0; i < 4; ++i) l += p0 + i < parts ? e[i].y * to_top(e[i].x, top) : 0.f;
     m = top;
   }
   return make_float2(m, l);
@@ -58,11 +57,11 @@ __global__ __launch_bounds__(256) void attention_tree_join_kernel(CacheRef c, Pl
       float top = e.x;
 #pragma unroll
       for (int i = 0; i < 8; ++i) top = fmaxf(top, t[i].x);
-      const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(e.x - ref);
+      const float f = to_top(e.x, top);
       acc.x *= f; acc.y *= f; e.y *= f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float k = p0 + i < parts ? __builtin_amdgcn_exp2f(t[i].x - ref) : 0.f;
+        const float k = p0 + i < parts ? to_top(t[i].x, top) : 0.f;
         if (k != 0.f) {   // wave-uniform
           e.y += k * t[i].y;
           acc.x += k * v[i].x;

@@ -795,3 +795,29 @@ def test_refusals_of_very_wide_calls(lib):
         ctx.otas_attention_masked(qkv, 1, [0] + [n] * 900, o)
     assert e.value.status == 5
     ctx.otas_attention_masked(qkv[:5].contiguous(), 1, [0] + [5] * 900, o[:5].contiguous())
+
+
+@pytest.mark.parametrize("dtype,H,KV,dh", [("f32", 2, 1, 64), ("f32", 2, 2, 20), ("bf16", 4, 2, 64), ("bf16", 2, 1, 80), ("bf16", 2, 1, 128), ("bf16", 2, 1, 40)])
+def test_a_query_that_is_not_a_number(lib, dtype, H, KV, dh):
+    """Its row is NaN, as the formula says, however the keys are split; no other row changes."""
+    import torch
+    ctx, g = context(dtype, H, dh), gen(8)
+    qkv = normal(g, (200, (H + 2 * KV) * dh), dtype)
+    bad = qkv.clone()
+    bad[[3, 150], :H * dh] = float("nan")
+    ok = torch.ones(200, dtype=torch.bool, device="cuda")
+    ok[[3, 150]] = False
+    for cap in (0.0, 20.0):
+        a, b = (torch.empty((200, H * dh), dtype=qkv.dtype, device="cuda") for _ in range(2))
+        ctx.otas_attention_masked(qkv, KV, [0, 200], a, score=lib.Score(cap=cap))
+        ctx.otas_attention_masked(bad, KV, [0, 200], b, score=lib.Score(cap=cap))
+        assert torch.equal(a[ok], b[ok]) and bool(b[~ok].isnan().all())
+        cache = new_cache(lib, g, dtype, 1, KV, 3000, dh)
+        for nodes in (5, 20, 40):
+            for cached in (0, 100, 3000):
+                ws = torch.empty(ctx.otas_attention_tree_workspace_bytes(KV, [0, nodes], [cached]), dtype=torch.uint8, device="cuda")
+                x, o = qkv[:nodes].contiguous(), [torch.empty((nodes, H * dh), dtype=qkv.dtype, device="cuda") for _ in range(2)]
+                for out in o:
+                    ctx.otas_attention_tree(cache, x, [0, nodes], None, None, [0], [cached], ws, out, score=lib.Score(cap=cap))
+                    x = bad[:nodes].contiguous()
+                assert torch.equal(o[0][ok[:nodes]], o[1][ok[:nodes]]) and bool(o[1][3].isnan().all()), (nodes, cached)
