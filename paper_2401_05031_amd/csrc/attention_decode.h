@@ -51,10 +51,6 @@ struct RowScore {
   }
   __device__ float scaled(float s) const { return cap > 0.f ? cap2 * tanhf(s * scale) : s * scale; }
   __device__ float with_distance(float s, int key_position) const { return s - slope2 * fabsf((float)(position - key_position)); }
-  __device__ float logit(float s, int key_position) const {
-    s = scaled(s);
-    return sloped ? with_distance(s, key_position) : s;
-  }
   __device__ void capped(floatx16& s) const {
     if (cap > 0.f) {
 #pragma unroll

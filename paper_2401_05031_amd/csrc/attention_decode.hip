@@ -414,6 +414,11 @@ __global__ __launch_bounds__(256) void attention_tree_mass_kernel(CacheRef c, co
       const int mine = min(row0 + fr, n * G - 1);
       floatx4 qf[4 * DT];
       load_heads<T, DT>(qf, qkv + (size_t)(base + mine / G) * ld + (size_t)(kh * G + mine % G) * dh, dh, fk);
+      // what the rows' logits are formed with and relative to: lane fr of either half has row row0 + fr
+      const int64_t my_at = (int64_t)(base + mine / G) * H + kh * G + mine % G;
+      const float my_m = ends[2 * my_at], my_l = ends[2 * my_at + 1];
+      const float my_inv = my_l == 0.f || row0 + fr >= n * G ? 0.f : 1.f / my_l;
+      const RowScore my = RowScore::of(sc, kh * G + mine % G, sc.slopes ? positions[base + mine / G] : 0);
       floatx16 s;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -425,14 +430,12 @@ __global__ __launch_bounds__(256) void attention_tree_mass_kernel(CacheRef c, co
         }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int r = row0 + 8 * (e >> 2) + 4 * fk + (e & 3);
-        if (r < n * G) {
-          const int node = r / G, head = kh * G + r % G;
-          const int64_t at = (int64_t)(base + node) * H + head;
-          const RowScore score = RowScore::of(sc, head, sc.slopes ? positions[base + node] : 0);
-          const float m = ends[2 * at], l = ends[2 * at + 1];
-          if (l != 0.f) got += __builtin_amdgcn_exp2f(score.logit(s[e], kpos) - m) / l;
-        }
+        if (row0 + 8 * (e >> 2) + (e & 3) >= n * G) continue;   // of either half
+        const int r = 8 * (e >> 2) + 4 * fk + (e & 3);
+        const float m = __shfl(my_m, r), inv = __shfl(my_inv, r);
+        float v = my.scaled(s[e]);
+        if (my.sloped) v -= __shfl(my.slope2, r) * fabsf((float)(__shfl(my.position, r) - kpos));
+        got += inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(v - m) * inv;
       }
     }
   }
