@@ -187,12 +187,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
       const bool whole = kb + kKeys <= sure && one;
       bool done = false;
       if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);
-      if (CAP && !done) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[b][e] = score.capped(s[b][e]);
-      }
+      if (CAP && !done) tile_capped<2>(s, score, cap);
       if (BIAS) {
         const int* kp = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>());
         const float near = (float)(score.position - kb - 4 * fk);

@@ -282,6 +282,27 @@ struct CapArgs {
   }
 };
 
+// Products into capped logits, in units of ln 2, where slopes or masks come between them and the weights: by the polynomial if all
+// of the wave's are small enough, keys that no row sees among them.
+template <int NB> __device__ __forceinline__ void tile_capped(floatx16 (&s)[NB], const Score2& score, const CapArgs& cap) {
+  float most = 0.f;   // NaN is passed over here and stays one in either form
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) most = fmaxf(fmaxf(most, fabsf(s[b][e])), fabsf(s[b][e + 1]));
+  if (__all(most <= cap.limit)) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[b][e] *= cap.slope(s[b][e]);
+  } else {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[b][e] = score.capped(s[b][e]);
+  }
+}
+
 // The sums are rescaled only when a maximum has grown by more than 8 (a weight may be up to 2^8 then: no accuracy is lost in a
 // floating format).
 template <int DH>

@@ -106,12 +106,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
       const bool whole = cached && k0 + 32 * NB <= valid;
       bool done = false;
       if (CAP && !BIAS && whole && !(RW == 1 && out.logits)) done = tile_weights_capped<DH, NB>(w, s, cap);
-      if (CAP && !done) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[b][e] = score.capped(s[b][e]);
-      }
+      if (CAP && !done) tile_capped<NB>(s, score, cap);
       if (BIAS) {
         const int* kp = reinterpret_cast<const int*>(buf + 2 * S::KB + value_slack<DH>()) + k0;
 #pragma unroll
