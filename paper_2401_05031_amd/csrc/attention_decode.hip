@@ -340,8 +340,8 @@ template <typename T> struct DraftKeys {
   __device__ bool partial(int) const { return true; }
 };
 
-// A workgroup has 32 rows (nodes x heads that share a key head) and one chunk of the cache; the first chunk's also the nodes
-// themselves.  With one chunk the rows are done, else the sums go to the workspace for the join.
+// A workgroup has 32 rows (nodes x heads that share a key head) and one chunk of the cache, or the nodes themselves; with one chunk
+// both, and the rows are done, else the sums go to the workspace for the join.
 template <typename T, int DT, bool WHOLE>
 __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_tree_f32_kernel(CacheRef c, const T* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
                                                                  PlanAny plan, int B, bool has_parents, TreeShape shape, ScoreArgs sc,
@@ -356,7 +356,10 @@ __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_tree_f32_kerne
   const int kh = id % c.KV, q = id / c.KV, dh = WHOLE ? 32 * DT : c.dh, G = H / c.KV;
   const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), row0 = group * 32;
   const int64_t slot = plan.at(B + 1 + q);
-  if (row0 >= n * G || (part > 0 && part * shape.chunk >= len)) return;
+  // The last part may be the nodes' of queries of several chunks.
+  const int chunks = shape.chunks(len);
+  const bool apart = shape.apart && shape.parts > 1 && part == shape.parts - 1, nodes = apart || (part == 0 && (chunks <= 1 || !shape.apart));
+  if (row0 >= n * G || (apart ? chunks <= 1 : part > 0 && part >= chunks)) return;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), fr = lane & 31, fk = lane >> 5;
   const int row = min(row0 + fr, n * G - 1), node = row / G, head = kh * G + row % G;
   const size_t ld = (size_t)(H + 2 * c.KV) * dh;
@@ -364,19 +367,20 @@ __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_tree_f32_kerne
   const RowScore score = RowScore::of(sc, head, sc.slopes ? positions[base + node] : 0);
   FloatRows<T, DT> r;
   rows_begin<T, DT>(r, first + (size_t)node * ld + (size_t)head * dh, dh, fk);
-  const int begin = part * shape.chunk, end = min(len, begin + shape.chunk);   // chunks are whole blocks
+  const int begin = apart ? 0 : part * shape.chunk, end = apart ? 0 : min(len, begin + shape.chunk);   // chunks are whole blocks
   if (begin < end) {
     const T* heads_k = (const T*)c.k + (slot * c.KV + kh) * c.capacity * dh;
     const T* heads_v = (const T*)c.v + (slot * c.KV + kh) * c.capacity * dh;
     const CachedKeys<T> keys{heads_k, heads_v, dh, end, fk, score, c.positions + slot * c.capacity};
     rows_stream<T, DT>(r, keys, dh, (begin >> 5) + wave, (end + 31) >> 5, 4, fr, fk);
   }
-  if (part == 0) {
+  if (nodes) {
     const uint64_t line = tree_lines(plan, 3 * B + 1, base, n, has_parents, lane);
     const DraftKeys<T> keys{first + (size_t)(H + kh) * dh, first + (size_t)(H + c.KV + kh) * dh, (int)ld, n, fk, lane_value(line, node), score, positions + base};
     rows_stream<T, DT>(r, keys, dh, wave, (n + 31) >> 5, 4, fr, fk);
   }
-  const bool only = len <= shape.chunk;   // the rows' one chunk
+  const bool only = chunks <= 1;   // the rows' one chunk
+  const int64_t place = apart ? chunks : part;
   rows_join<T, DT>(r, dh, f32_lds, [&](int i, int d, floatx4 v, float m, float l) {
     if (row0 + i >= n * G) return;
     const int64_t at = (int64_t)(base + (row0 + i) / G) * H + kh * G + (row0 + i) % G;
@@ -384,8 +388,8 @@ __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_tree_f32_kerne
       store_row4<T>(o + at * dh + d, v, l);
       if (ends && d == 0) { ends[2 * at] = m; ends[2 * at + 1] = l; }
     } else {
-      *reinterpret_cast<floatx4*>(sums + ((int64_t)part * TH + at) * dh + d) = v;
-      if (d == 0) { tops[2 * (part * TH + at)] = m; tops[2 * (part * TH + at) + 1] = l; }
+      *reinterpret_cast<floatx4*>(sums + (place * TH + at) * dh + d) = v;
+      if (d == 0) { tops[2 * (place * TH + at)] = m; tops[2 * (place * TH + at) + 1] = l; }
     }
   });
 }

@@ -3,9 +3,9 @@
 // waves have 32 rows each, and 4 / RW share those rows, every one with its own keys of a tile, to be joined at the end: the usual
 // single token has few rows, and then all four waves work on keys.  What bounds few rows is the cache's own bytes; what bounds
 // many is the matrix cores and the exponentials, as in otas_attention_masked.
-//   32 queries of one token over 5700 .. 8192 entries (8 key heads of 128, with weights added up): 198 us and 13 for the join, 919 MB at
-// 4.4 TB/s.  8 x 48 nodes over 2000 .. 4000: 34 and 6.5 us (512 workgroups of 8 tiles, the first 6 us after the launch).  One token over
-// 1537 entries: 10.9 and 4.0 us, a chain of launch, plan, queries, one tile, the waves' join.
+//   32 queries of one token over 5700 .. 8192 entries (8 key heads of 128, with weights added up): 198 us and 8 for the join, 919 MB at
+// 4.5 TB/s.  8 x 48 nodes over 2000 .. 4000: 31 and 7.5 us (576 workgroups of up to 8 tiles, the first 6 us after the launch).  One token over
+// 1537 entries: 8.8 and 3.8 us, a chain of launch, plan, queries, one tile, the waves' join.
 #include "attention_tiles.h"
 #include "attention_tree_join.h"
 
@@ -46,20 +46,23 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
   const int part = unit % shape.parts, kh = unit / shape.parts % c.KV, q = unit / shape.parts / c.KV, G = H / c.KV;
   const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G, group0 = group * 32 * RW;
   const int64_t slot = plan.at(B + 1 + q);
-  if (group0 >= rows || (part > 0 && part * shape.chunk >= len)) return;
+  // The last part may be the nodes' of queries of several chunks.
+  const int chunks = shape.chunks(len);
+  const bool apart = shape.apart && shape.parts > 1 && part == shape.parts - 1, nodes = apart || (part == 0 && (chunks <= 1 || !shape.apart));
+  if (group0 >= rows || (apart ? chunks <= 1 : part > 0 && part >= chunks)) return;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fk = lane >> 5;
   const int rw = wave % RW, kg = wave / RW, row0 = group0 + rw * 32;
   const bool active = row0 < rows;
   const int row = min(row0 + fr, rows - 1), node = row / G, head = kh * G + row % G;
   const size_t ld = (size_t)(H + 2 * c.KV) * DH;
   const bf16_t* first = qkv + (size_t)base * ld;
-  const int begin = part * shape.chunk, end = min(len, begin + shape.chunk);
+  const int begin = apart ? 0 : part * shape.chunk, end = apart ? 0 : min(len, begin + shape.chunk);
   const char* cached_k = reinterpret_cast<const char*>((const bf16_t*)c.k + ((slot * c.KV + kh) * c.capacity + begin) * DH);
   const char* cached_v = reinterpret_cast<const char*>((const bf16_t*)c.v + ((slot * c.KV + kh) * c.capacity + begin) * DH);
   const char* draft_k = reinterpret_cast<const char*>(first + (size_t)(H + kh) * DH);
   const char* draft_v = reinterpret_cast<const char*>(first + (size_t)(H + c.KV + kh) * DH);
   const int32_t* cached_pos = c.positions + slot * c.capacity + begin;
-  const int cached_tiles = (max(0, end - begin) + KEYS - 1) / KEYS, steps = cached_tiles + (part == 0 ? 1 : 0);   // the nodes themselves last
+  const int cached_tiles = (max(0, end - begin) + KEYS - 1) / KEYS, steps = cached_tiles + (nodes ? 1 : 0);   // the nodes themselves last
 
   TileLoader<DH, KEYS, 4, false> key_loader;
   TileLoader<DH, KEYS, 4, true> value_loader;
@@ -79,7 +82,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
   };
   const Score2 score = Score2::of(sc, BIAS ? sc.slopes[head] : 0.f, BIAS ? positions[base + node] : 0);
   uint64_t line = 0;
-  if (part == 0) line = lane_value(tree_lines(plan, 3 * B + 1, base, n, has_parents, lane), node);
+  if (nodes) line = lane_value(tree_lines(plan, 3 * B + 1, base, n, has_parents, lane), node);
   bool met = false;   // whether this wave took out a sibling's value
 
   fetch(0, lds);
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
       tile_sums<DH, NB>(w, s, v, buf + S::KB, 2 * kg * NB, lane);
     }
   }
-  const bool not_finite = part == 0 && any_wave(met, reinterpret_cast<int*>(lds + S::LDS - 16), wave, lane);   // the siblings' part
+  const bool not_finite = nodes && any_wave(met, reinterpret_cast<int*>(lds + S::LDS - 16), wave, lane);
   if (not_finite && kg == 0) {   // one of the waves that share rows
     for (int j = 0; j < n; ++j) {
       const bf16_t* v = reinterpret_cast<const bf16_t*>(draft_v) + (size_t)j * ld;
@@ -161,7 +164,8 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
     }
   }
 
-  const bool only = len <= shape.chunk;   // the rows' one chunk: done
+  const bool only = chunks <= 1;   // the rows' one chunk: done
+  const int64_t place = apart ? chunks : part;
   auto finish = [&](int r, int d, floatx4 v, float m, float l) {   // columns d .. d + 3 of row r of the query's
     const int64_t at = (int64_t)(base + r / G) * H + kh * G + r % G;
     if (only) {
@@ -171,10 +175,10 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
       for (int e = 0; e < 4; ++e) x[e] = (bf16_t)(l == 0.f ? 0.f : v[e] * inv);
       *reinterpret_cast<bf16x4*>(o + at * DH + d) = x;
     } else {
-      *reinterpret_cast<floatx4*>(out.sums + ((int64_t)part * out.TH + at) * DH + d) = v;
+      *reinterpret_cast<floatx4*>(out.sums + (place * out.TH + at) * DH + d) = v;
     }
     if (d == 0) {
-      if (!only) { out.tops[2 * (part * out.TH + at)] = m; out.tops[2 * (part * out.TH + at) + 1] = l; }
+      if (!only) { out.tops[2 * (place * out.TH + at)] = m; out.tops[2 * (place * out.TH + at) + 1] = l; }
       else if (out.ends) { out.ends[2 * at] = m; out.ends[2 * at + 1] = l; }
     }
   };

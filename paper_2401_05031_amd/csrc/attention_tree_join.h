@@ -1,6 +1,6 @@
 // The parts of a tree's rows joined, for both types of attention_decode.hip and attention_tree_bf16.hip: maxima in units of ln 2.
-// Bound by latency (4 us for one token of 13 parts: the launch and two round trips to L2) or, with weights added up from the logits, by
-// their bytes (32 x 16 rows over 8192 entries: 13 us for 50 MB, most of it from L2).
+// Bound by latency (3.8 us for one token of 14 parts: the launch and two round trips to L2) or, with weights added up from the logits, by
+// their bytes (32 x 16 rows over 8192 entries: 8 us for 15 MB of logits, from L2).
 #pragma once
 #include "attention_decode.h"
 
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void attention_tree_join_kernel(CacheRef c, Pl
       const int mid = (lo + hi) >> 1;
       if (plan.at(mid) <= row) lo = mid; else hi = mid;
     }
-    const int len = plan.at(2 * B + 1 + lo), parts = (len + shape.chunk - 1) / shape.chunk;
+    const int parts = shape.parts_of(plan.at(2 * B + 1 + lo));
     if (parts <= 1) return;   // written already
     // lane d has columns 2 d and 2 d + 1; eight parts at a time, so that their loads overlap
     const bool mine = 2 * lane < dh;
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) void attention_tree_join_kernel(CacheRef c, Pl
     return;
   }
   const int id = (int)blockIdx.x - join_wgs, q = id / xblks, e0 = (id % xblks) * 256;
-  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), parts = (len + shape.chunk - 1) / shape.chunk;
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), parts = shape.parts_of(len);
   const int64_t slot = plan.at(B + 1 + q);
   if (e0 >= len || n == 0) return;   // workgroup-uniform
   for (int r = tid; r < n * H; r += 256) {

@@ -59,11 +59,19 @@ hipError_t launch_attention_masked_bf16(const void* qkv, const int32_t* plan, si
 // that leaves 512 entries or fewer to each (8 queries over 6000, 2 key heads: 19 us; 27 with blocks of 128); else 384 entries or more and up to
 // 768 workgroups, which are counted from every query's own length: the longest query's many parts leave nothing to do for those of
 // shorter queries (24 queries of 400 .. 8000: 105 -> 96 us; with weights added up 125 -> 115).
+//   The nodes themselves follow a query's first chunk, which makes its workgroup the last by 3 us; or they are a part of their own
+// (`apart`), behind the chunks, where there are several: one token over 1537 entries 14.6 -> 12.6 us, 8 x 48 nodes over 4000 42 -> 39, fp32 6 x 40 over
+// 5000 105 -> 85.  bf16 rows of 32 have them apart while all workgroups find a CU: one fits a CU there at width 128, and
+// more of them cost a full chip more than they save (32 tokens over 8192 205 -> 238 us).
 struct TreeShape {
-  int rows, groups, chunk, parts, room;   // room: what the workspace has place for; >= parts, and grows with the lengths
+  int rows, groups, chunk, parts;   // parts: of the longest query, the nodes' among them
+  int apart;                        // 1: the nodes have a part of their own
+  int room;                         // parts that the workspace has place for; >= parts, and grows with the lengths
+  __host__ __device__ int chunks(int length) const { return (length + chunk - 1) / chunk; }
+  __host__ __device__ int parts_of(int length) const { return chunks(length) > 1 ? chunks(length) + apart : 1; }
 };
 inline TreeShape tree_shape(int dtype, int dh, int H, int KV, const int32_t* off, const int32_t* length, int B) {
-  TreeShape t{32, 1, 0, 1, 1};
+  TreeShape t{32, 1, 128, 1, 0, 1};
   int64_t most = 0, longest = 0;
   for (int q = 0; q < B; ++q) {
     most = std::max<int64_t>(most, off[q + 1] - off[q]);
@@ -94,8 +102,10 @@ inline TreeShape tree_shape(int dtype, int dh, int H, int KV, const int32_t* off
     }
   }
   t.chunk = (int)chunk;
-  t.parts = (int)pieces(longest, chunk);
-  t.room = (int)std::max<int64_t>(1, std::min((few ? 2 : 1) * (target / wgs), pieces(longest, 128)));
+  t.apart = !few || wgs * (t.chunks((int)longest) + 1) <= 256;
+  t.parts = t.parts_of((int)longest);
+  const int64_t most_chunks = std::min((few ? 2 : 1) * (target / wgs), pieces(longest, 128));
+  t.room = most_chunks > 1 ? (int)most_chunks + 1 : 1;
   return t;
 }
 // Floats of workspace: ends [T H][2]; where there is room for more than one part, for each largest logits and weight sums [T H][2]
