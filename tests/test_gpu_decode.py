@@ -821,3 +821,28 @@ def test_a_query_that_is_not_a_number(lib, dtype, H, KV, dh):
                     ctx.otas_attention_tree(cache, x, [0, nodes], None, None, [0], [cached], ws, out, score=lib.Score(cap=cap))
                     x = bad[:nodes].contiguous()
                 assert torch.equal(o[0][ok[:nodes]], o[1][ok[:nodes]]) and bool(o[1][3].isnan().all()), (nodes, cached)
+
+
+@pytest.mark.parametrize("dtype,H,KV,dh,B,nodes,longest", [("bf16", 16, 16, 128, 20, 1, 2600), ("bf16", 16, 8, 64, 24, 3, 1900), ("bf16", 8, 8, 96, 40, 2, 900),
+                                                           ("f32", 8, 4, 64, 24, 2, 700)])
+def test_many_queries_over_long_caches_of_all_lengths(lib, dtype, H, KV, dh, B, nodes, longest):
+    """A full chip: lengths from none to the longest, cut by every query's own length, the nodes behind the first chunk or apart."""
+    import torch
+    ctx, g, rng = context(dtype, H, dh), gen(B + longest), np.random.default_rng(B)
+    cache = new_cache(lib, g, dtype, B, KV, longest, dh)
+    cached = [int(x) for x in rng.integers(0, longest, B)]
+    cached[:4] = [longest, 0, 384, 385]
+    slots = [int(s) for s in rng.permutation(B)]
+    off = [nodes * q for q in range(B + 1)]
+    qkv = normal(g, (nodes * B, (H + 2 * KV) * dh), dtype, 1.5)
+    before = clone_cache(lib, cache)
+    ws = torch.full((ctx.otas_attention_tree_workspace_bytes(KV, off, cached),), 255, dtype=torch.uint8, device="cuda")
+    for mass in (True, False):
+        o = torch.empty((nodes * B, H * dh), dtype=qkv.dtype, device="cuda")
+        cache.mass.copy_(before.mass)
+        ctx.otas_attention_tree(cache, qkv, off, [-1, 0, 0][:nodes] * B, None, slots, cached, ws, o, add_mass=mass)
+        w, b, grown, gb = plain.tree(qkv, H, before.k, before.v, before.positions, before.mass, off, [-1, 0, 0][:nodes] * B, None, slots, cached)
+        within(o, w, b, "tree")
+        for q in range(B if mass else 0):
+            within(cache.mass[slots[q], :cached[q]], grown[slots[q], :cached[q]], gb[slots[q], :cached[q]] + 1e-30, "mass")
+    assert same_cache(cache, before)
