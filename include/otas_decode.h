@@ -121,7 +121,8 @@ otas_status otas_attention_tree(otas_ctx *ctx, const otas_kv_cache *cache, const
                                 size_t workspace_bytes, void *o);
 
 /* Cuts caches down to keep[q] entries.  Entries are ranked: first those that are protected (entry < lead, or position >=
- * recent_from[q]), then by mass, largest first (NaN counts as least), ties to the lower entry.  The first keep[q] stay: an entry
+ * recent_from[q]), which are alike whatever their mass, then the others by mass, largest first (NaN counts as least); ties go to the
+ * lower entry.  (So where more are protected than keep[q], the lowest of them stay.)  The first keep[q] stay: an entry
  * below keep[q] that stays does not move, and the j-th that stays from above takes, with position and mass, the place of
  * the j-th below that goes (so no more is moved than has to be, and entries are in no order afterwards).  Entries from keep[q]
  * on are left as they were.

@@ -534,7 +534,8 @@ class Context:
         return int(self._lib.otas_cache_evict_workspace_bytes(self._h, length.address, kept.address, length.n))
 
     def otas_cache_evict(self, cache, slots, lengths, keep, workspace, lead=0, recent_from=None) -> np.ndarray:
-        """Cuts every query's slot down to its keep entries of most mass; returns the new lengths."""
+        """Cuts every query's slot down to keep entries: the protected ones, the lowest first, then those of most mass; returns the
+        new lengths."""
         c = self._need_cache(cache)
         slot = _Ints(slots, "slots")
         B = slot.n

@@ -6,7 +6,7 @@
 namespace otas {
 
 // ------------------------------------------------------------------------------------------------- which entries stay
-// Scores become unsigned numbers in the same order (NaN lowest, protected entries highest), which stay in LDS up to 32768 entries
+// Scores become unsigned numbers in the same order (NaN lowest, protected entries highest and alike), which stay in LDS up to 32768 entries
 // (beyond that they are formed again in every pass).  The keep-th largest of them is found by 11, 11 and 10 bits, highest first: a
 // histogram of the bits over the entries that agree with those found so far (integer counts: any order gives the same), and a
 // scan from its top.  Bytes would take a fourth pass, and the highest of them is little but the exponent: weights of one
