@@ -64,8 +64,8 @@ __global__ __launch_bounds__(256) void attention_tree_join_kernel(CacheRef c, Pl
       acc.x *= f; acc.y *= f; e.y *= f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float k = p0 + i < parts ? to_top(t[i].x, top) : 0.f;
-        if (k != 0.f) {   // wave-uniform
+        if (p0 + i < parts) {   // wave-uniform; also where the factor is 0: NaN stays
+          const float k = to_top(t[i].x, top);
           e.y += k * t[i].y;
           acc.x += k * v[i].x;
           acc.y += k * v[i].y;
