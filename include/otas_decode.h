@@ -60,7 +60,8 @@ otas_status otas_rotary(otas_ctx *ctx, const void *qkv, int64_t T, int32_t kv_he
  * slopes are given, s - slopes[h] |position_i - position_j|. */
 typedef struct {
   float scale;          /* finite; 0 = 1 / sqrt(d_h) */
-  float cap;            /* finite, >= 0; 0 = none.  bf16 logits are off by up to 1e-6 cap; scale / cap up to 1e38 (EINVAL) */
+  float cap;            /* finite, >= 0; 0 = none.  For the cap a bf16 logit is off by up to 1e-6 cap, or 4e-6 of itself where cap > 256.
+                         * scale / cap up to 1e38 (EINVAL) */
   const float *slopes;  /* dev [H] or NULL */
 } otas_score_desc;
 

@@ -40,7 +40,7 @@ template <int DH> constexpr size_t masked_lds(int max_n, bool documents) {
   return 2 * masked_buffer<DH>() + 16 + (documents ? (size_t)(max_n + kKeys - 1) / kKeys + 64 : 0);
 }
 
-template <int DH, bool CAP, bool BIAS>
+template <int DH, int CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf16_t* __restrict__ qkv, PlanAny plan, int B, int H, int KV, int xblks,
                                                                        int by_xcd, ScoreArgs sc, CapArgs cap, MaskArgs mk, bf16_t* __restrict__ o) {
   typedef TileRows<DH> R;
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
       const bool whole = kb + kKeys <= sure && one;
       bool done = false;
       if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);
-      if (CAP && !done) tile_capped<2>(s, score, cap);
+      if (CAP && !done) tile_capped<CAP, 2>(s, score, cap);
       if (BIAS) {
         const int* kp = reinterpret_cast<const int*>(buf + 2 * KB + value_slack<DH>());
         const float near = (float)(score.position - kb - 4 * fk);
@@ -297,9 +297,12 @@ hipError_t launch_attention_masked_bf16(const void* qkv, const int32_t* plan, si
     return hipGetLastError();
   };
   auto pick = [&](auto width) {
-    const bool cap = sc.cap > 0.f, bias = sc.slopes != nullptr;
-    if (cap) return bias ? run(width, std::true_type{}, std::true_type{}) : run(width, std::true_type{}, std::false_type{});
-    return bias ? run(width, std::false_type{}, std::true_type{}) : run(width, std::false_type{}, std::false_type{});
+    auto with_bias = [&](auto cap) { return sc.slopes ? run(width, cap, std::true_type{}) : run(width, cap, std::false_type{}); };
+    switch (Score2::cap_form(sc.cap)) {
+      case 0: return with_bias(std::integral_constant<int, 0>{});
+      case 1: return with_bias(std::integral_constant<int, 1>{});
+    }
+    return with_bias(std::integral_constant<int, 2>{});
   };
   switch (dh) {
     case 64: return pick(std::integral_constant<int, 64>{});

@@ -253,27 +253,38 @@ struct Score2 {
     const float scale = fabsf(sc.scale);   // the sign is in the rows
     return Score2{sc.cap > 0.f ? 2.f * log2e * (scale / sc.cap) : scale * log2e, sc.cap * log2e, slope * log2e, position};
   }
-  // cap tanh(s scale / cap) = cap - 2 cap / (1 + exp(2 s scale / cap)): off by 2^-23 cap at most near zero, where the two cancel.
-  __device__ __forceinline__ float capped(float s) const {
-    return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * scale2)), cap2);
+  // cap tanh(x), x = s scale / cap, as cap - 2 cap / (1 + exp(2 x)): off by 3e-7 cap at most, near zero, where the two cancel.  CAP 2 (caps past
+  // kFarCap, where that would be more than 8e-5 of a logit, however small the logit): x - x^3 / 3 + 2 x^5 / 15 up to 3 / 32 (4e-8 of it
+  // off) and 1 - 2 / (1 + exp(2 x)) beyond (4e-6 of it off).
+  template <int CAP> __device__ __forceinline__ float capped(float s) const {
+    const float t = s * scale2, r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t));
+    if (CAP == 1) return fmaf(-2.f * cap2, r, cap2);
+    constexpr float h = 0.34657359028f;   // ln 2 / 2: x = h t
+    const float y = t * t, near = h * t * fmaf(fmaf(2.f / 15 * h * h * h * h, y, -h * h / 3), y, 1.f);
+    return cap2 * (fabsf(t) <= kSeries / h ? near : fmaf(-2.f, r, 1.f));
   }
+  static constexpr float kFarCap = 256.f, kSeries = 3.f / 32;
+  static int cap_form(float cap) { return cap > kFarCap ? 2 : cap > 0.f ? 1 : 0; }   // the kernels' CAP
 };
 
 // cap tanh(s scale / cap) for products that stay below three eighths of the cap, as they mostly do: an odd polynomial of degree 5
 // (least squares on a fine grid, re-weighted until the error is flat: 8e-7 of the cap) takes three full-rate instructions and no
 // more for the exponent, where exponential and reciprocal are two at quarter rate and four more; these kernels are bound by
-// the vector ALU there.  limit < 0: scale / cap is too far from 1 for its powers.
+// the vector ALU there.  Past kFarCap the series, whose error goes with the logit, up to 3 / 32 of the cap: logits of 24 and more.
+// limit < 0: scale / cap is too large for its powers; 2^24 at most, where none of them is too small.
 struct CapArgs {
   float a0, a1, a2, limit;   // logits in units of ln 2 = s (a0 + a1 s^2 + a2 s^4) while |s| <= limit
   static CapArgs of(const ScoreArgs& sc) {
     CapArgs r = {0.f, 0.f, 0.f, -1.f};
     if (!(sc.cap > 0.f)) return r;
     const double x = fabs((double)sc.scale) / sc.cap, k = sc.cap * 1.4426950408889634 * x;
-    if (x < 1.0 / 65536 || x > 65536.0 || sc.cap > 1e6f) return r;
-    r.a0 = (float)(0.9999854 * k);
-    r.a1 = (float)(-0.33248851 * k * x * x);
-    r.a2 = (float)(0.120988494 * k * x * x * x * x);
-    r.limit = (float)(0.375 / x);
+    const bool far = Score2::cap_form(sc.cap) == 2;
+    const double c0 = far ? 1.0 : 0.9999854, c1 = far ? -1.0 / 3 : -0.33248851, c2 = far ? 2.0 / 15 : 0.120988494;
+    if (x > 65536.0 || c2 * k * x * x * x * x > 1e38) return r;
+    r.a0 = (float)(c0 * k);
+    r.a1 = (float)(c1 * k * x * x);
+    r.a2 = (float)(c2 * k * x * x * x * x);
+    r.limit = (float)std::min((far ? (double)Score2::kSeries : 0.375) / x, 16777216.0);
     return r;
   }
   __device__ __forceinline__ float slope(float s) const {   // logit / s
@@ -284,7 +295,7 @@ struct CapArgs {
 
 // Products into capped logits, in units of ln 2, where slopes or masks come between them and the weights: by the polynomial if all
 // of the wave's are small enough, keys that no row sees among them.
-template <int NB> __device__ __forceinline__ void tile_capped(floatx16 (&s)[NB], const Score2& score, const CapArgs& cap) {
+template <int CAP, int NB> __device__ __forceinline__ void tile_capped(floatx16 (&s)[NB], const Score2& score, const CapArgs& cap) {
   float most = 0.f;   // NaN is passed over here and stays one in either form
 #pragma unroll
   for (int b = 0; b < NB; ++b)
@@ -299,7 +310,7 @@ template <int NB> __device__ __forceinline__ void tile_capped(floatx16 (&s)[NB],
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[b][e] = score.capped(s[b][e]);
+      for (int e = 0; e < 16; ++e) s[b][e] = score.capped<CAP>(s[b][e]);
   }
 }
 

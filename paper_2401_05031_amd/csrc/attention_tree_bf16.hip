@@ -21,7 +21,7 @@ template <int DH, int RW> struct TreeTile {
 
 // logits (of the cached entries, where their weights are to be added up and rows are few): [T H][stride], 4 bytes a row and
 // key written and read once, where forming them again would read the key's 2 d_h bytes once more.
-template <int DH, int RW, bool CAP, bool BIAS>
+template <int DH, int RW, int CAP, bool BIAS>
 __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tree_bf16_kernel(CacheRef c, const bf16_t* __restrict__ qkv, int H,
                                                                                               const int32_t* __restrict__ positions, PlanAny plan, int B,
                                                                                               bool has_parents, TreeShape shape, ScoreArgs sc, CapArgs cap,
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
       const bool whole = cached && k0 + 32 * NB <= valid;
       bool done = false;
       if (CAP && !BIAS && whole && !(RW == 1 && out.logits)) done = tile_weights_capped<DH, NB>(w, s, cap);
-      if (CAP && !done) tile_capped<NB>(s, score, cap);
+      if (CAP && !done) tile_capped<CAP, NB>(s, score, cap);
       if (BIAS) {
         const int* kp = reinterpret_cast<const int*>(buf + 2 * S::KB + value_slack<DH>()) + k0;
 #pragma unroll
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
             for (int e = 0; e < 4; ++e) s[b][4 * g + e] = fmaf(-score.slope2, fabsf(d[e]), CAP ? s[b][4 * g + e] : s[b][4 * g + e] * score.scale2);
           }
       }
-      constexpr bool SCALED = CAP || BIAS;
+      constexpr bool SCALED = CAP != 0 || BIAS;
       if (!whole) {
         // of this half's keys, from the wave's first on: how many are left, and which of the nodes the row sees
         const int left = valid - k0 - 4 * fk;
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
 // mass_j += sum_i exp(s_ij - m_i) / l_i with the logits formed again, for many rows.  A workgroup has 32 entries; its waves share out the key heads,
 // whose keys a lane holds while it goes through the rows 32 at a time: here a lane owns a key, so that the sum over rows is one
 // over its own registers.  Waves are added in order.
-template <int DH, bool CAP, bool BIAS>
+template <int DH, int CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attention_tree_mass_bf16_kernel(CacheRef c, const bf16_t* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
                                                                           PlanAny plan, int B, int xblks, ScoreArgs sc, const float* __restrict__ ends) {
   __shared__ float part[4][32];
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void attention_tree_mass_bf16_kernel(CacheR
       for (int e = 0; e < 16; ++e) {
         const int r = 8 * (e >> 2) + 4 * fk + (e & 3);
         const float m = __shfl(my_m, r), inv = __shfl(my_inv, r);
-        float v = CAP ? score.capped(s[e] * sign) : s[e] * sign * score.scale2;
+        float v = CAP ? score.capped<CAP>(s[e] * sign) : s[e] * sign * score.scale2;
         if (BIAS) v -= __shfl(my_slope, r) * fabsf((float)(__shfl(my_pos, r) - kpos));
         got += inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(v - m) * inv;
       }
@@ -331,9 +331,12 @@ hipError_t launch_attention_tree_bf16(const CacheRef& c, const void* qkv, int H,
     return hipErrorInvalidValue;
   };
   auto pick = [&](auto width) {
-    const bool cap = sc.cap > 0.f, bias = sc.slopes != nullptr;
-    if (cap) return bias ? by_rows(width, std::true_type{}, std::true_type{}) : by_rows(width, std::true_type{}, std::false_type{});
-    return bias ? by_rows(width, std::false_type{}, std::true_type{}) : by_rows(width, std::false_type{}, std::false_type{});
+    auto with_bias = [&](auto cap) { return sc.slopes ? by_rows(width, cap, std::true_type{}) : by_rows(width, cap, std::false_type{}); };
+    switch (Score2::cap_form(sc.cap)) {
+      case 0: return with_bias(std::integral_constant<int, 0>{});
+      case 1: return with_bias(std::integral_constant<int, 1>{});
+    }
+    return with_bias(std::integral_constant<int, 2>{});
   };
   switch (c.dh) {
     case 64: return pick(std::integral_constant<int, 64>{});

@@ -107,6 +107,8 @@ otas_status score_ok(const otas_ctx* c, const otas_score_desc* score, ScoreArgs*
   // The kernels' factors, exp2 in place of exp and tanh by it, have to be finite too.
   const double scale = std::fabs((double)out->scale), most = 3.4e38;
   if (scale * 1.5 > most || (score->cap > 0.f && (score->cap * 1.5 > most || scale / score->cap * 3.0 > most))) return OTAS_EINVAL;
+  // A cap that the scale is no float's part of: products of up to 2^115 are off by 2^-23 of themselves without it.
+  if (score->cap > 0.f && scale / score->cap < 1.17549435e-38) out->cap = 0.f;
   out->slopes = score->slopes;
   return OTAS_OK;
 }

@@ -2,7 +2,8 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_decode import _close, clone_cache, context, gen, new_cache, normal  # noqa: F401
+from tests import decode_plain as plain
+from tests.test_gpu_decode import _close, clone_cache, context, gen, new_cache, normal, slopes_of, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +63,46 @@ def test_a_key_that_is_not_a_number_behind_small_weights(lib, dtype, H, KV, dh, 
     of_head = out[1][nodes:].view(nodes, H, dh)[:, :H // KV]
     assert bool(of_head.isnan().all()) and bool(mass[1][1].isnan().all())
     assert torch.equal(out[0][:nodes], out[1][:nodes]) and torch.equal(mass[0][0], mass[1][0]) and bool(out[0].isfinite().all())
+
+
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("cap", [300.0, 1e4, 1e6, 1e9, 1e25, 2e38])
+@pytest.mark.parametrize("dtype,H,KV,dh", [("f32", 2, 1, 64), ("bf16", 2, 1, 64), ("bf16", 2, 1, 80), ("bf16", 2, 2, 96), ("bf16", 4, 1, 128), ("bf16", 2, 1, 40)])
+def test_caps_far_above_the_logits(lib, dtype, H, KV, dh, cap, slopes):
+    """A cap that no logit comes near costs a logit 2^-18 of itself at most, however large the cap is: outputs are off by what they
+    are without a cap, and by a mean of |v| times twice the largest change of a logit.
+    At 300 logits past 3 / 32 of the cap stand beside small ones."""
+    import torch
+    ctx, g, off, std = context(dtype, H, dh), gen(int(np.log2(cap)) + dh), [0, 150, 331], 2.0
+    qkv = normal(g, (331, (H + 2 * KV) * dh), dtype, std)
+    qkv[[20, 200], :H * dh] *= 8                          # logits of a hundred among others
+    sl = slopes_of(H) if slopes else None
+
+    def more(q, k, v):   # twice what a logit may be off by for the cap (tanhf in float32: 8 half steps), times the largest value
+        top = float((q.double() @ k.double().T.contiguous()).abs().max()) * dh ** -0.5
+        return 2 * (2.0 ** -18 if dtype == "bf16" else 8 * plain.F32) * top * float(v.double().abs().max())
+    score = lib.Score(cap=cap, slopes=sl)
+    o = torch.empty((331, H * dh), dtype=qkv.dtype, device="cuda")
+    ctx.otas_attention_masked(qkv, KV, off, o, prefix=[3, 100], score=score)
+    want = plain.masked(qkv, H, KV, off, True, [3, 100], None, None, None, cap, sl)[0]
+    bound = plain.masked(qkv, H, KV, off, True, [3, 100], None, None, None, 0.0, sl)[1]
+    x = qkv.view(331, H + 2 * KV, dh)
+    q, k, v = x[:, :H].reshape(-1, dh), x[:, H:H + KV].reshape(-1, dh), x[:, H + KV:]
+    within(o, want, bound + more(q, k, v), "masked")
+    cache = new_cache(lib, g, dtype, 2, KV, 420, dh)
+    before = clone_cache(lib, cache)
+    for nodes in (1, 20, 40):                             # a few rows of a key head, and many
+        rows, doff, cached = qkv[:2 * nodes].contiguous(), [0, nodes, 2 * nodes], [400, 129]
+        pos = torch.arange(850, 850 + 2 * nodes, device="cuda", dtype=torch.int32)
+        ws = torch.empty(ctx.otas_attention_tree_workspace_bytes(KV, doff, cached, add_mass=True), dtype=torch.uint8, device="cuda")
+        o = torch.empty((2 * nodes, H * dh), dtype=qkv.dtype, device="cuda")
+        cache.mass.copy_(before.mass)
+        ctx.otas_attention_tree(cache, rows, doff, None, pos, [1, 0], cached, ws, o, score=score, add_mass=True)
+        args = rows, H, cache.k, cache.v, cache.positions, before.mass, doff, None, pos, [1, 0], cached, None
+        w, _, grown, _ = plain.tree(*args, cap, sl)
+        _, b, _, gb = plain.tree(*args, 0.0, sl)
+        extra = more(q, torch.cat([k, cache.k.reshape(-1, dh)]), torch.cat([v.reshape(-1, dh), cache.v.reshape(-1, dh)]))
+        within(o, w, b + extra, "tree")
+        for i, s in enumerate((1, 0)):                    # a weight is off by twice the change of itself
+            grow = extra / float(torch.cat([v.reshape(-1, dh), cache.v.reshape(-1, dh)]).double().abs().max()) * (grown[s] - before.mass[s].double()).abs()
+            within(cache.mass[s, :cached[i]], grown[s, :cached[i]], (gb[s] + grow)[:cached[i]] + 1e-30, "mass")
