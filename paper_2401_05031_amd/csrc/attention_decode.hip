@@ -459,7 +459,7 @@ static hipError_t attention_tree_any(const CacheRef& c, const void* qkv, int H, 
   if (wgs > kMostGroups || (TH + 3) / 4 > kMostGroups || (int64_t)B * xblks > kMostGroups) return kTooManyGroups;
   float* ends = workspace;
   float* tops = workspace + 2 * TH;
-  float* sums = tops + 2 * TH * shape.parts;
+  float* sums = workspace + tree_sums_at(shape, T_, H);
   const PlanAny p = plan_any(plan, count, d_plan);
   return with_tiles(c.dh, [&](auto dt, auto whole) {
     constexpr int DT = decltype(dt)::value;

@@ -299,7 +299,7 @@ hipError_t launch_attention_tree_bf16(const CacheRef& c, const void* qkv, int H,
   buf.stride = tree_logit_stride(max_len);
   buf.ends = workspace;
   buf.tops = workspace + 2 * TH;
-  buf.sums = buf.tops + 2 * TH * shape.parts;
+  buf.sums = workspace + tree_sums_at(shape, T, H);
   buf.logits = by_logits ? workspace + tree_logits_at(shape, T, H, c.dh) : nullptr;
   if (!add_mass) buf.ends = nullptr;
   auto run = [&](auto width, auto rw, auto cap, auto bias) {

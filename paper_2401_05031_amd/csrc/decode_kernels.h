@@ -109,8 +109,10 @@ inline TreeShape tree_shape(int dtype, int dh, int H, int KV, const int32_t* off
   return t;
 }
 // Floats of workspace: ends [T H][2]; where there is room for more than one part, for each largest logits and weight sums [T H][2]
-// and sums [T H][dh]; where weights are added up over few rows (bf16), logits [T H][stride].
+// and sums [T H][dh]; where weights are added up over few rows (bf16), logits [T H][stride].  Sums and logits are accessed four at a
+// time and begin at multiples of four (dh is one, so that the sums end before the logits whatever the parts).
 inline int64_t tree_logit_stride(int max_len) { return (max_len + 3) / 4 * 4; }
+inline size_t tree_sums_at(const TreeShape& t, int64_t T, int H) { return ((size_t)T * H * 2 * (1 + (size_t)t.parts) + 3) / 4 * 4; }
 inline size_t tree_logits_at(const TreeShape& t, int64_t T, int H, int dh) {
   return ((size_t)T * H * ((t.room > 1 ? (size_t)t.room * (dh + 2) : 0) + 2) + 3) / 4 * 4;
 }

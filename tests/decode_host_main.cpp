@@ -1,0 +1,60 @@
+// Host arithmetic of the decoder's operators (include/otas_decode.h) that no GPU is needed for: where the parts of a workspace lie, limits
+// of launches, factors of a rotation.  Built as decode_api_main.cpp is, see test_decode_host.py.
+#define __HIP_PLATFORM_AMD__ 1
+#include <hip/hip_runtime.h>
+#ifndef __align__
+#define __align__(n) __attribute__((aligned(n)))
+#endif
+#ifndef HIP_SYMBOL
+#define HIP_SYMBOL(x) (&x)
+#endif
+#include "../paper_2401_05031_amd/csrc/api.hip"
+#include "../paper_2401_05031_amd/csrc/decode_api.hip"
+
+extern "C" hipError_t hipMalloc(void** p, size_t n) { *p = std::calloc(1, n); return hipSuccess; }
+extern "C" hipError_t hipHostMalloc(void** p, size_t n, unsigned) { *p = std::calloc(1, n); return hipSuccess; }
+extern "C" hipError_t hipFree(void* p) { std::free(p); return hipSuccess; }
+extern "C" hipError_t hipHostFree(void* p) { std::free(p); return hipSuccess; }
+extern "C" hipError_t hipGetSymbolAddress(void** p, const void*) { static int32_t cell[64]; *p = cell; return hipSuccess; }
+
+#define CHECK(e) do { if (!(e)) { std::fprintf(stderr, "line %d: %s\n", __LINE__, #e); return 1; } } while (0)
+#define IS(want, call) do { const otas_status got_ = (call); if (got_ != (want)) { std::fprintf(stderr, "line %d: %s -> %d\n", __LINE__, #call, (int)got_); return 1; } } while (0)
+
+// Sums and logits of a tree begin at multiples of four floats, one behind the other and within what the caller is asked for.
+static int workspace_places() {
+  int uneven = 0;
+  for (int dtype : {0, 1})
+    for (int dh : {4, 20, 64, 80, 128})
+      for (int H : {1, 3, 6, 7})
+        for (int KV : {1, 3})
+          for (int B : {1, 3, 40})
+            for (int n : {1, 2, 9, 64})
+              for (int l : {0, 1, 130, 300, 600, 1100, 5000, 70000}) {
+                if (H % KV) continue;
+                std::vector<int32_t> off(B + 1), len(B);
+                for (int q = 0; q <= B; ++q) off[q] = n * q;
+                for (int q = 0; q < B; ++q) len[q] = l * (q + 1) / B;
+                const int64_t T = off[B], TH = T * H;
+                const TreeShape t = tree_shape(dtype, dh, H, KV, off.data(), len.data(), B);
+                CHECK(t.parts >= 1 && t.room >= t.parts);
+                if (t.parts > 1) {
+                  const size_t sums = tree_sums_at(t, T, H);
+                  uneven += 2 * TH * (1 + t.parts) % 4 != 0;
+                  CHECK(sums % 4 == 0 && sums >= (size_t)(2 * TH * (1 + t.parts)));
+                  CHECK(sums + (size_t)TH * t.parts * dh <= tree_logits_at(t, T, H, dh));
+                }
+                CHECK(tree_logits_at(t, T, H, dh) % 4 == 0);
+                for (bool mass : {false, true}) {
+                  const bool logits = mass && dtype != 0 && bf16_width(dh) && t.rows == 32;
+                  CHECK(tree_workspace_floats(t, dtype, T, H, dh, l, mass) >= tree_logits_at(t, T, H, dh) + (logits ? (size_t)TH * l : 0));
+                }
+              }
+  CHECK(uneven > 100);   // the case was met
+  return 0;
+}
+
+int main() {
+  if (workspace_places()) return 1;
+  std::puts("decode host ok");
+  return 0;
+}

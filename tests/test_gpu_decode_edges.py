@@ -106,3 +106,25 @@ def test_caps_far_above_the_logits(lib, dtype, H, KV, dh, cap, slopes):
         for i, s in enumerate((1, 0)):                    # a weight is off by twice the change of itself
             grow = extra / float(torch.cat([v.reshape(-1, dh), cache.v.reshape(-1, dh)]).double().abs().max()) * (grown[s] - before.mass[s].double()).abs()
             within(cache.mass[s, :cached[i]], grown[s, :cached[i]], (gb[s] + grow)[:cached[i]] + 1e-30, "mass")
+
+
+@pytest.mark.parametrize("dtype,H,KV,dh,nodes,cached", [("f32", 3, 3, 64, [1], [300]), ("f32", 3, 1, 8, [1, 0, 2], [900, 5, 300]), ("bf16", 3, 3, 64, [1], [600]),
+                                                        ("bf16", 3, 1, 128, [1, 2], [0, 640]), ("bf16", 3, 1, 64, [15], [700]), ("bf16", 3, 1, 80, [41], [2000])])
+def test_trees_of_an_odd_number_of_rows(lib, dtype, H, KV, dh, nodes, cached):
+    """Rows times heads odd and several parts: the sums' place in the workspace is none that follows from the rows alone."""
+    import torch
+    ctx, g, B = context(dtype, H, dh), gen(dh + len(nodes)), len(nodes)
+    cache = new_cache(lib, g, dtype, B, KV, max(cached), dh)
+    before = clone_cache(lib, cache)
+    off = [0, *np.cumsum(nodes).tolist()]
+    qkv = normal(g, (off[-1], (H + 2 * KV) * dh), dtype)
+    n = ctx.otas_attention_tree_workspace_bytes(KV, off, cached)
+    ws = torch.full((n + 256,), 255, dtype=torch.uint8, device="cuda")
+    o = torch.empty((off[-1], H * dh), dtype=qkv.dtype, device="cuda")
+    assert off[-1] * H % 2 == 1
+    ctx.otas_attention_tree(cache, qkv, off, None, None, list(range(B)), cached, ws[:n], o, add_mass=True)
+    w, b, grown, gb = plain.tree(qkv, H, before.k, before.v, before.positions, before.mass, off, None, None, list(range(B)), cached)
+    within(o, w, b, "tree")
+    for q in range(B):
+        within(cache.mass[q, :cached[q]], grown[q, :cached[q]], gb[q, :cached[q]] + 1e-30, "mass")
+    assert bool((ws[n:] == 255).all())
