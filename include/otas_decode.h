@@ -14,8 +14,9 @@
  *     entry point says how many it has), else through the context's plan buffer.  Calls of the first kind may be captured into a
  *     HIP graph (their host numbers are part of it); of the second kind they are refused under capture (EUNSUPPORTED), and
  *     limited to 1048576 entries (ENOMEM).
- *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, attention over very
- *     many queries of which one is very long (all are given as many workgroups as the longest).
+ *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, 2^24 of
+ *     otas_cache_append, attention over very many queries of which one is very long (all are given as many workgroups as the longest).
+ *     otas_cache_evict has a limit of its own.
  *   - Results do not depend on the order in which the device happens to run anything.
  */
 #ifndef OTAS_DECODE_H_
@@ -130,7 +131,8 @@ otas_status otas_attention_tree(otas_ctx *ctx, const otas_kv_cache *cache, const
  *   slot, length, keep host [B], slots differ from each other, keep >= 0 (keep >= length: nothing happens)
  *   recent_from host [B] or NULL (none protected by position);  lead >= 0
  *   workspace dev >= otas_cache_evict_workspace_bytes for the same numbers, 256-byte aligned; cache->mass required
- *   length_out host [B] = min(length, keep), filled on return.   Host numbers: 5 B. */
+ *   length_out host [B] = min(length, keep), filled on return.   Host numbers: 5 B.
+ *   Up to 65535 queries, whose min(keep, length - keep) add up to less than 2^30 - B / 2 (EUNSUPPORTED). */
 size_t otas_cache_evict_workspace_bytes(const otas_ctx *ctx, const int32_t *length, const int32_t *keep, int32_t B);
 otas_status otas_cache_evict(otas_ctx *ctx, const otas_kv_cache *cache, const int32_t *slot, const int32_t *length,
                              const int32_t *keep, int32_t B, int32_t lead, const int32_t *recent_from, void *workspace,

@@ -241,6 +241,7 @@ otas_status otas_cache_append(otas_ctx* c, const otas_kv_cache* cache, const voi
     } else if (N > T) {
       return OTAS_EINVAL;
     }
+    if (N > kMostGroups) return OTAS_EUNSUPPORTED;   // a workgroup a row
     const size_t count = 3 * (size_t)B + 1 + (rows ? (size_t)N : 0);
     if (count > kPlanInts) return OTAS_ENOMEM;
     std::vector<int32_t> plan(count);   // row offsets [B+1] | slot [B] | length [B] | rows [N]

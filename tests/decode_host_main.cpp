@@ -53,8 +53,40 @@ static int workspace_places() {
   return 0;
 }
 
+// As many workgroups as a launch may have, and one more.
+static int most_workgroups() {
+  char* const base = (char*)(uintptr_t)(1ull << 40);
+  void *qkv = base, *ws = base + (1ull << 44);
+  for (int dtype : {(int)OTAS_F32, (int)OTAS_BF16}) {
+    const otas_model_desc d = {1, 64, 1, 64, dtype, 1e-6f, 1};
+    otas_layer_weights w;
+    std::fill((const void**)&w, (const void**)(&w + 1), qkv);
+    otas_ctx* c = nullptr;
+    CHECK(otas_create(&c, &d, &w, nullptr) == OTAS_OK);
+    const otas_kv_cache k = {base + (1ull << 45), base + (1ull << 46), (int32_t*)qkv, (float*)qkv, 70000, 1, OTAS_MAX_LONG_SEQ};
+    std::vector<int32_t> off(17), slot(16), len(16, 0), out(16);
+    for (int q = 0; q < 16; ++q) { slot[q] = 15 - q; off[q + 1] = (q + 1) << 20; }
+    IS(OTAS_EUNSUPPORTED, otas_cache_append(c, &k, qkv, 1 << 24, off.data(), nullptr, (int32_t*)qkv, slot.data(), len.data(), 16, out.data()));
+    off[16] -= 1;
+    IS(OTAS_OK, otas_cache_append(c, &k, qkv, 1 << 24, off.data(), nullptr, (int32_t*)qkv, slot.data(), len.data(), 16, out.data()));
+    CHECK(out[0] == 1 << 20 && out[15] == (1 << 20) - 1);
+    // an eviction's queries, and its lists of places and sources: 2 x 524288 entries a query here
+    const int B = 65536;
+    std::vector<int32_t> all(B), n(B, 10), five(B, 5), rest(B);
+    for (int q = 0; q < B; ++q) all[q] = q;
+    IS(OTAS_EUNSUPPORTED, otas_cache_evict(c, &k, all.data(), n.data(), five.data(), B, 0, nullptr, ws, (size_t)1 << 40, rest.data()));
+    IS(OTAS_OK, otas_cache_evict(c, &k, all.data(), n.data(), five.data(), B - 1, 0, nullptr, ws, (size_t)1 << 40, rest.data()));
+    std::fill(n.begin(), n.end(), OTAS_MAX_LONG_SEQ);
+    std::fill(five.begin(), five.end(), OTAS_MAX_LONG_SEQ / 2);
+    IS(OTAS_EUNSUPPORTED, otas_cache_evict(c, &k, all.data(), n.data(), five.data(), 2048, 0, nullptr, ws, (size_t)1 << 40, rest.data()));
+    IS(OTAS_OK, otas_cache_evict(c, &k, all.data(), n.data(), five.data(), 2047, 0, nullptr, ws, (size_t)1 << 40, rest.data()));
+    CHECK(otas_destroy(c) == OTAS_OK);
+  }
+  return 0;
+}
+
 int main() {
-  if (workspace_places()) return 1;
+  if (workspace_places() || most_workgroups()) return 1;
   std::puts("decode host ok");
   return 0;
 }
