@@ -41,7 +41,8 @@ extern "C" {
  *   OTAS_ROTARY_BY_PARTS  w f_i + (1 - w) f_i / factor,  w = (original_length f_i / (2 pi) - slow_turns) / (fast_turns - slow_turns)
  *                         held to [0, 1]: pairs that turn often within the original length keep their pace
  *   layout  OTAS_ROTARY_HALF pair i = elements (i, i + rot_dim / 2), OTAS_ROTARY_INTERLEAVED (2 i, 2 i + 1)
- * Angles are formed in 64 bits and reduced there, so that far positions lose nothing.
+ * Angles are formed in 64 bits and reduced there, so that far positions lose nothing.  A description whose base or angles do not fit
+ * 64 bits is refused (EINVAL).
  *   positions dev int32 [T], any value;  out dev [T, (H + 2 kv_heads) d_h], may be qkv (then only what turns is written), else no
  *   overlap.  rot_dim even, 0 .. d_h (0: a copy).  No host numbers. */
 enum { OTAS_ROTARY_HALF = 0, OTAS_ROTARY_INTERLEAVED = 1 };

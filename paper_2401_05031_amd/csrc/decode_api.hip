@@ -136,6 +136,7 @@ bool rotary_args(const otas_rotary_desc& d, RotaryArgs* r) {
   const int pairs = d.rot_dim / 2;
   double base = d.base;
   if (d.scaling == OTAS_ROTARY_BASE) base *= std::pow(d.factor, (double)d.rot_dim / (d.rot_dim - 2));
+  if (!std::isfinite(base) || base <= 0.0) return false;
   for (int i = 0; i < pairs; ++i) {
     double turns = std::pow(base, -2.0 * i / d.rot_dim) / (2.0 * 3.14159265358979323846);
     if (d.scaling == OTAS_ROTARY_LINEAR) turns /= d.factor;
@@ -143,7 +144,7 @@ bool rotary_args(const otas_rotary_desc& d, RotaryArgs* r) {
       const double w = std::min(1.0, std::max(0.0, (d.original_length * turns - d.slow_turns) / (d.fast_turns - d.slow_turns)));
       turns = w * turns + (1.0 - w) * turns / d.factor;
     }
-    if (!std::isfinite(turns)) return false;
+    if (!std::isfinite(turns * 2147483648.0)) return false;   // the farthest position's
     r->turns[i] = d.inverse ? -turns : turns;
   }
   for (int i = pairs; i < 64; ++i) r->turns[i] = 0.0;

@@ -85,8 +85,31 @@ static int most_workgroups() {
   return 0;
 }
 
+// Rotations whose base or whose farthest angle is no number in 64 bits, and their like that are.
+static int rotations() {
+  char* const base = (char*)(uintptr_t)(1ull << 40);
+  const otas_model_desc d = {1, 128, 1, 64, OTAS_F32, 1e-6f, 1};
+  otas_layer_weights w;
+  std::fill((const void**)&w, (const void**)(&w + 1), base);
+  otas_ctx* c = nullptr;
+  CHECK(otas_create(&c, &d, &w, nullptr) == OTAS_OK);
+  auto turn = [&](int rot, int scaling, double b, double factor) {
+    const otas_rotary_desc r = {rot, OTAS_ROTARY_HALF, scaling, 0, b, factor, 4096.0, 32.0, 1.0, 1.0};
+    return otas_rotary(c, base, 5, 1, (int32_t*)base, &r, base);
+  };
+  IS(OTAS_EINVAL, turn(4, OTAS_ROTARY_BASE, 10000.0, 1e160));     // base 1e324: all but the first pair would stand still
+  IS(OTAS_OK, turn(4, OTAS_ROTARY_BASE, 10000.0, 1e150));
+  IS(OTAS_EINVAL, turn(128, OTAS_ROTARY_BASE, 1e300, 1e10));
+  IS(OTAS_EINVAL, turn(4, OTAS_ROTARY_BASE, 1.0, 1e-170));        // base 0
+  IS(OTAS_EINVAL, turn(4, OTAS_ROTARY_LINEAR, 1e-300, 1e-154));   // 1e304 at position 1, infinity from 1e4 on
+  IS(OTAS_OK, turn(4, OTAS_ROTARY_LINEAR, 1e-300, 1.0));
+  IS(OTAS_OK, turn(4, OTAS_ROTARY_PLAIN, 1e300, 0.0));
+  CHECK(otas_destroy(c) == OTAS_OK);
+  return 0;
+}
+
 int main() {
-  if (workspace_places() || most_workgroups()) return 1;
+  if (workspace_places() || most_workgroups() || rotations()) return 1;
   std::puts("decode host ok");
   return 0;
 }
