@@ -128,3 +128,25 @@ def test_trees_of_an_odd_number_of_rows(lib, dtype, H, KV, dh, nodes, cached):
     for q in range(B):
         within(cache.mass[q, :cached[q]], grown[q, :cached[q]], gb[q, :cached[q]] + 1e-30, "mass")
     assert bool((ws[n:] == 255).all())
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype,H,KV,dh,T,rot,interleaved", [("f32", 2, 1, 64, 1, 64, False), ("f32", 4, 2, 20, 37, 10, True), ("f32", 4, 1, 128, 1101, 126, False),
+                                                             ("bf16", 2, 1, 128, 8203, 128, False), ("bf16", 4, 2, 128, 8203, 122, False), ("bf16", 5, 5, 8, 70, 6, False),
+                                                             ("bf16", 2, 1, 12, 65, 8, True), ("bf16", 4, 4, 80, 2051, 80, True), ("bf16", 2, 1, 100, 17, 98, False)])
+def test_rotary_writes_its_rows_alone(lib, dtype, H, KV, dh, T, rot, interleaved, in_place):
+    """Three rows on either side of the output keep their bits, in the kernels of whole and of odd halves."""
+    import torch
+    ctx, g, W = context(dtype, H, dh), gen(T + rot), (H + 2 * KV) * dh
+    qkv = normal(g, (T, W), dtype)
+    pos = torch.randint(0, 2 ** 17, (T,), generator=g, device="cuda", dtype=torch.int32)
+    lead = 2 if W * qkv.element_size() % 16 else 3        # the output begins at a multiple of 16 bytes
+    assert lead * W * qkv.element_size() % 16 == 0
+    whole = torch.full((T + lead + 3, W), 7.0, dtype=qkv.dtype, device="cuda")
+    out = whole[lead:lead + T]
+    if in_place:
+        out.copy_(qkv)
+    ctx.otas_rotary(out if in_place else qkv, KV, pos, lib.Rotary(rot, layout=lib.OTAS_ROTARY_INTERLEAVED if interleaved else lib.OTAS_ROTARY_HALF), out)
+    want, bound = plain.rotary(qkv, H, KV, pos, rot, interleaved, plain.frequencies(rot))
+    within(out, want, bound + 1e-6 * (2.0 ** 17 * 2.0 ** -52 * 6.3), "rotary")
+    assert bool((whole[:lead] == 7.0).all()) and bool((whole[lead + T:] == 7.0).all())
