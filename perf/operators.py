@@ -375,10 +375,12 @@ _CONTEXTS = {}
 
 
 def _context(st):
-    """The program's context for this model shape: one for all its calls."""
+    """The program's context for this model shape on the current device and stream, to which a context is bound."""
     import paper_2401_05031_amd as otas
     H, KV, dh = st["heads"]
-    key = (H, dh, st["dt"])
+    device = torch.cuda.current_device()
+    # torch.cuda.current_stream() makes an object, 2.7 us; its number alone takes 0.1
+    key = (H, dh, st["dt"], device, torch._C._cuda_getCurrentRawStream(device))
     if key not in _CONTEXTS:
         D = H * dh
         sizes = {"ln1_g": (D,), "ln1_b": (D,), "w_qkv": (3 * D, D), "b_qkv": (3 * D,), "w_proj": (D, D), "b_proj": (D,), "ln2_g": (D,), "ln2_b": (D,),
