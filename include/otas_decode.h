@@ -75,6 +75,8 @@ typedef struct {
  *   positions dev int32 [T] or NULL (i, j themselves): for the distance only; within +- 2^29
  *   score     NULL = all defaults
  *   o         dev [T, D], no overlap with any other array.  A row that sees nothing, or no key of weight, is zero.
+ *   Logits, weights and sums are float.  bf16 models with d_h of 64, 80, 96 or 128 round each weight to bf16 (by 2^-8 of itself at most)
+ *   before it meets its value; the weights' sum takes them unrounded.  The same goes for otas_attention_tree.
  * Keys and values that a row does not see do not reach it, infinities and NaN included.
  * Lengths up to OTAS_MAX_LONG_SEQ (EUNSUPPORTED).  Host numbers: 2 B + 1. */
 otas_status otas_attention_masked(otas_ctx *ctx, const void *qkv, int32_t kv_heads, const int32_t *offsets, int32_t B,
@@ -85,7 +87,7 @@ otas_status otas_attention_masked(otas_ctx *ctx, const void *qkv, int32_t kv_hea
  * and the attention weight that it has gathered.  The caller owns the memory and knows which query has which slot and how many
  * entries of it are filled (they are entries 0 .. length - 1; those behind are neither read nor written, except where a call
  * says so).  The four arrays overlap neither each other nor any other array of a call (EINVAL where k and v are one, or the call's
- * qkv, o or workspace lies in them). */
+ * qkv, o or workspace has a byte in common with k or v; the others are not looked at). */
 typedef struct {
   void *k, *v;         /* dev [slots, kv_heads, capacity, d_h], model dtype */
   int32_t *positions;  /* dev [slots, capacity] */

@@ -2,7 +2,9 @@
 // attention_masked_bf16.hip and attention_tree_bf16.hip are not built for):
 //   o_i = sum_j w_ij v_j / sum_j w_ij,  w_ij = exp(s_ij - max_j s_ij) over the keys j that row i sees,
 // in one pass over the keys with the running maximum and sum of the softmax.  All arithmetic is fp32, on
-// v_mfma_f32_32x32x2_f32 for both products; bf16 operands are widened.
+// v_mfma_f32_32x32x2_f32 for both products; bf16 operands are widened, at the fp32 rate: 2 x 2000 causal bf16 rows of 16 heads of 48, 72
+// and 112 take 171, 258 and 400 us (72 TFLOP/s) where 64, 80 and 128 take 45, 50 and 61; a token of 24 queries over 4000 entries of 4 key
+// heads of 72 takes 78 us, of 80 38.
 #include "attention_decode.h"
 #include "attention_tree_join.h"
 

@@ -1,9 +1,11 @@
 // otas_attention_masked in bf16: four waves have 128 rows of a head and walk the keys that any of them sees in tiles of 64, which
 // travel from global memory into the one LDS buffer while the other is worked on; one barrier a tile.
 //   Two workgroups, eight waves, fill a CU's registers (2 a SIMD; 3 would spill from width 80 on and gave nothing at 64).  128 rows read
-// a tile once for four waves; with 64 keys a tile is as large as two buffers and two workgroups leave room for.  Bound by the vector
-// ALU, 10 instructions a logit beside 1 / 8 of a matrix instruction, at a clock of 1.9 - 2.0 GHz: 8192 capped causal rows of 16 heads of
-// 128 in 330 us, 0.83 PFLOP/s where a large matrix product reaches 1.27; 5000 rows of 16 heads of 80 without a cap 114 us (0.56).
+// a tile once for four waves; with 64 keys a tile is as large as two buffers and two workgroups leave room for.  Bound by the matrix
+// cores and the vector ALU in turn, which hardly overlap: 64 logits of a wave at width 128 take one matrix instruction (32 clocks) and 10
+// vector ones (4 each, most at full rate), and of 8192 capped causal rows' 7.0e8 SIMD clocks the matrix cores are busy in 2.7e8 and the
+// vector ALU in 4.0e8.  At a clock of 1.9 - 2.0 GHz those rows take 330 us with 16 heads of 128, 0.84 PFLOP/s where a large matrix product
+// reaches 1.27; without a cap 290 us (0.95), 16 heads of 80 229 us (0.75), 64 199 us (0.69).
 // 3 x 4000 rows of seven documents with slopes take 95 us: a workgroup has 7 tiles of 2.3 us each (3.5 where keys are masked) after
 // 5 us for its plan, the kinds of tiles and the first tile.
 #include "attention_tiles.h"
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(256, 2) void attention_masked_bf16_kernel(const bf1
       tile_products<DH, 2>(s, w, buf, 0, fr, fk);
       short8_t v[WaveRows<DH>::DT];
       first_values<DH>(v, buf + KB, 0, lane);
-      __builtin_amdgcn_s_setprio(1);   // the vector ALU is the bound: a wave that needs it goes before one at its products (358 -> 335 us, 8192 capped rows)
+      __builtin_amdgcn_s_setprio(1);   // a wave that needs the vector ALU, the busier of the two, goes before one at its products (358 -> 340 us, 8192 capped rows)
       const bool whole = kb + kKeys <= sure && one;
       bool done = false;
       if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);

@@ -269,8 +269,8 @@ struct Score2 {
 
 // cap tanh(s scale / cap) for products that stay below three eighths of the cap, as they mostly do: an odd polynomial of degree 5
 // (least squares on a fine grid, re-weighted until the error is flat: 8e-7 of the cap) takes three full-rate instructions and no
-// more for the exponent, where exponential and reciprocal are two at quarter rate and four more; these kernels are bound by
-// the vector ALU there.  Past kFarCap the series, whose error goes with the logit, up to 3 / 32 of the cap: logits of 24 and more.
+// more for the exponent, where exponential and reciprocal are two at quarter rate and four more; the vector ALU is what these
+// kernels keep busiest.  Past kFarCap the series, whose error goes with the logit, up to 3 / 32 of the cap: logits of 24 and more.
 // limit < 0: scale / cap is too large for its powers; 2^24 at most, where none of them is too small.
 struct CapArgs {
   float a0, a1, a2, limit;   // logits in units of ln 2 = s (a0 + a1 s^2 + a2 s^4) while |s| <= limit

@@ -11,7 +11,7 @@ namespace otas {
 // turns), then sincospif, shared by all heads of the row.  Then they walk the rows in chunks of V elements (16 bytes where
 // heads and pairs allow it).  A chunk of the first half of the pairs is turned together with its partner by one thread,
 // so that a call in place has no other thread read what it writes.  Memory-bound: a row's bytes in and out once (16384 bf16 rows of
-// 16 + 2 x 8 heads of 128, 268 MB: 50 us, 5.3 TB/s; 37 rows 3.9 us, a launch's latency).
+// 16 + 2 x 8 heads of 128, 268 MB: 50 us, 5.3 TB/s; as many float rows of 12 + 2 x 12 heads of 64, 302 MB: 51 us; 37 rows 3.9 us, a launch's latency).
 template <typename T, int V> struct alignas(V * sizeof(T)) Chunk { T x[V]; };
 
 // The cosines and sines of the pairs of nt rows from t0 on, those of a row 64 apart.  All threads of the workgroup.
