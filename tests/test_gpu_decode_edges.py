@@ -150,3 +150,54 @@ def test_rotary_writes_its_rows_alone(lib, dtype, H, KV, dh, T, rot, interleaved
     want, bound = plain.rotary(qkv, H, KV, pos, rot, interleaved, plain.frequencies(rot))
     within(out, want, bound + 1e-6 * (2.0 ** 17 * 2.0 ** -52 * 6.3), "rotary")
     assert bool((whole[:lead] == 7.0).all()) and bool((whole[lead + T:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,H,KV,dh", [("f32", 4, 2, 64), ("bf16", 8, 2, 64), ("bf16", 12, 4, 80)])
+def test_a_layer_of_the_librarys_operators(lib, dtype, H, KV, dh):
+    """LayerNorm, a projection to grouped heads, rotation, masked attention, the cache, the next token over it, the projection back onto
+    the float residual: every step against the 64-bit form on what the step before it gave."""
+    import torch
+    ctx, g, D = context(dtype, H, dh), gen(H * dh), H * dh
+    off, T, W = [0, 130, 131, 200], 200, (H + 2 * KV) * dh
+    half = plain.half_step(torch.float32 if dtype == "f32" else torch.bfloat16)
+    x = normal(g, (T, D), dtype)
+    gain, shift = normal(g, (D,), dtype, 0.1) + 1, normal(g, (D,), dtype, 0.1)
+    w_in, b_in, w_out, b_out = normal(g, (W, D), dtype, D ** -0.5), normal(g, (W,), dtype), normal(g, (D, D), dtype, D ** -0.5), normal(g, (D,), dtype)
+
+    def product(a, w, b):   # (result, what sums in float32 may be off by)
+        p = a.double() @ w.double().T.contiguous() + b.double()
+        return p, plain.F32 * (w.shape[1] + 2) * (a.double().abs() @ w.double().abs().T.contiguous() + b.double().abs())
+    h = torch.empty_like(x)
+    ctx.otas_layer_norm(x, gain, shift, T, h)
+    z = x.double()
+    s = (z - z.mean(1, keepdim=True)) / (z.var(1, unbiased=False, keepdim=True) + 1e-6).sqrt()
+    want = s * gain.double() + shift.double()
+    # the library's LayerNorm has tests of its own: mean and variance to within the sums' D half steps here
+    within(h, want, half * want.abs() + plain.F32 * (D + 16) * (gain.double() * (1 + s.abs()) + want.abs()), "norm")
+    qkv = torch.empty((T, W), dtype=x.dtype, device="cuda")
+    ctx.otas_linear(h, w_in, b_in, None, T, W, D, 0, qkv)
+    p, b = product(h, w_in, b_in)
+    within(qkv, p, b + half * p.abs() * (1 + 2 ** -6), "projection")
+    pos = torch.cat([torch.arange(z - a, device="cuda", dtype=torch.int32) for a, z in zip(off, off[1:])])
+    rope = lib.Rotary(dh)
+    p, b = plain.rotary(qkv, H, KV, pos, dh, False, plain.frequencies(dh))
+    ctx.otas_rotary(qkv, KV, pos, rope, qkv)
+    within(qkv, p, b, "rotary")
+    o = torch.empty((T, D), dtype=x.dtype, device="cuda")
+    ctx.otas_attention_masked(qkv, KV, off, o)
+    within(o, *plain.masked(qkv, H, KV, off, True), "attention")
+    cache = new_cache(lib, g, dtype, 3, KV, 160, dh)
+    rows = [i for a, z in zip(off, off[1:]) for i in range(a, z - 1)]   # all but every query's last row
+    roff, slots = [0, 129, 129, 197], [2, 0, 1]
+    filled = ctx.otas_cache_append(cache, qkv, roff, rows, pos, slots, [0, 0, 0]).tolist()
+    last = qkv[[129, 130, 199]].contiguous()
+    ws = torch.empty(ctx.otas_attention_tree_workspace_bytes(KV, [0, 1, 2, 3], filled), dtype=torch.uint8, device="cuda")
+    o1 = torch.empty((3, D), dtype=x.dtype, device="cuda")
+    ctx.otas_attention_tree(cache, last, [0, 1, 2, 3], None, None, slots, filled, ws, o1)
+    p, b = plain.masked(qkv, H, KV, off, True)
+    within(o1, p[[129, 130, 199]], b[[129, 130, 199]], "next token")
+    res = x.float()
+    p, b = product(o, w_out, b_out)
+    want = p + res.double()
+    ctx.otas_linear(o, w_out, b_out, res, T, D, D, 2, res)
+    within(res, want, b + plain.F32 * (p.abs() + want.abs()) * 2, "residual")
