@@ -234,7 +234,8 @@ __global__ __launch_bounds__(256, RW == 1 && DH > 64 ? 1 : 2) void attention_tre
 // mass_j += sum_i exp(s_ij - m_i) / l_i with the logits formed again, for many rows.  A workgroup has 32 entries; its waves share out the key heads,
 // whose keys a lane holds while it goes through the rows 32 at a time: here a lane owns a key, so that the sum over rows is one
 // over its own registers.  Waves are added in order.  A block of 32 x 32 takes 32 cross-lane reads of the rows' maxima and
-// sums, 64 with slopes, beside 4 to 8 matrix instructions, and the cache's keys are read a second time: 8 x 48 nodes over 2000 .. 4000 entries of 8 key heads of 128 take 36 us without and 67 with weights.
+// sums, 64 with slopes, beside 4 to 8 matrix instructions, and the cache's keys are read a second time: 8 x 48 nodes over
+// 2000 .. 4000 entries of 8 key heads of 128 take 36 us without and 67 with weights.
 template <int DH, int CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attention_tree_mass_bf16_kernel(CacheRef c, const bf16_t* __restrict__ qkv, int H, const int32_t* __restrict__ positions,
                                                                           PlanAny plan, int B, int xblks, ScoreArgs sc, const float* __restrict__ ends) {

@@ -15,8 +15,8 @@ namespace otas {
 // that move there, in rising order.
 //   One workgroup's LDS reads, barriers and ballots: 7.2 us for 1000 entries, 21.8 for 16 queries of 16000 (2 of them the loads, 7 the
 // three passes, 8 the two walks at the end).  Sums over the waves in one step in place of a loop, one walk of counting in place of
-// two and the waves' numbers in scalars took 1.1 and 2.4 us off.  Past 32768 entries the one workgroup reads them five times: a cache of 500000 entries
-// cut by a fiftieth takes 670 us, 33000 51 us, 32000 40.
+// two and the waves' numbers in scalars took 1.1 and 2.4 us off.  Past 32768 entries the one workgroup
+// reads them five times: a cache of 500000 entries cut by a fiftieth takes 670 us, 33000 51 us, 32000 40.
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64, kEvictBins = 2048, kEvictInLds = 32768;
 
 struct EvictQuery {
