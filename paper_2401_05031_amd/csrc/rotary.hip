@@ -2,6 +2,7 @@
 #include "common.h"
 #include "decode_kernels.h"
 #include "plan_args.h"
+#include "rotary_angles.h"
 
 namespace otas {
 
@@ -12,21 +13,6 @@ namespace otas {
 // heads and pairs allow it).  A chunk of the first half of the pairs is turned together with its partner by one thread,
 // so that a call in place has no other thread read what it writes.  Memory-bound: a row's bytes in and out once (16384 bf16 rows of
 // 16 + 2 x 8 heads of 128, 268 MB: 50 us, 5.3 TB/s; as many float rows of 12 + 2 x 12 heads of 64, 302 MB: 51 us; 37 rows 3.9 us, a launch's latency).
-template <typename T, int V> struct alignas(V * sizeof(T)) Chunk { T x[V]; };
-
-// The cosines and sines of the pairs of nt rows from t0 on, those of a row 64 apart.  All threads of the workgroup.
-__device__ __forceinline__ void rotary_angles(float2* cs, const int32_t* __restrict__ positions, int64_t t0, int nt, const RotaryArgs& r) {
-  const int pairs = r.rot >> 1;
-  for (int i = (int)threadIdx.x; i < nt * pairs; i += 256) {
-    const int t = i / pairs, p = i - t * pairs;
-    const double turn = (double)positions[t0 + t] * r.turns[p];
-    float sn, c;
-    sincospif((float)(2.0 * (turn - rint(turn))), &sn, &c);
-    cs[t * 64 + p] = make_float2(c * r.magnitude, sn * r.magnitude);
-  }
-  __syncthreads();
-}
-
 template <typename T, int V>
 __global__ __launch_bounds__(256) void rotary_kernel(const T* qkv, T* out, const int32_t* __restrict__ positions, int64_t rows, int heads,
                                                      int W, int dh, int tokens, RotaryArgs r) {
