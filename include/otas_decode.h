@@ -1,7 +1,8 @@
 /*
  * otas_decode.h -- C ABI of the operators with which a decoder reads the encoder's output on AMD MI355X (gfx950):
- * rotary positions, masked attention over packed rows, a key/value cache of fixed capacity, attention of drafted
- * tokens over it, and eviction from it by accumulated attention weight.
+ * rotary positions, also with norms of the heads, masked and windowed attention over packed rows, a key/value cache of fixed
+ * capacity, attention of drafted tokens over it, eviction from it by accumulated attention weight, attention of its last tokens
+ * through a window, and all of the latter with the cache held in 4 bits.
  *
  * The conventions are those of otas.h: contexts, streams, errors, host and dev pointers.  In addition:
  *   - H, d_h = D / H and the element type are the context's; its layers' weights are not read.  d_h is any multiple of 4 up
@@ -140,6 +141,86 @@ size_t otas_cache_evict_workspace_bytes(const otas_ctx *ctx, const int32_t *leng
 otas_status otas_cache_evict(otas_ctx *ctx, const otas_kv_cache *cache, const int32_t *slot, const int32_t *length,
                              const int32_t *keep, int32_t B, int32_t lead, const int32_t *recent_from, void *workspace,
                              size_t workspace_bytes, int32_t *length_out);
+
+/* Norms of query and key heads with rotary positions in the same pass: every query head x of d_h elements becomes
+ *   y = (x - c) r gain,   r = 1 / sqrt(mean((x - c)^2) + eps),   c = mean(x) where center != 0, else 0,
+ * every key head the same with its own gain, and y is turned as otas_rotary turns it (rot_dim 0: not at all).  Values stay as they are.
+ *   q_gain, k_gain dev, model dtype, [d_h], with per_head != 0 [H, d_h] and [kv_heads, d_h], or NULL (ones)
+ *   eps finite, > 0 (EINVAL).  Means, norms and rotation are float, rounded once; heads of elements beyond 1e18, whose squares' sum
+ *   is no float, are not for this entry point.
+ *   positions may be NULL where rot_dim is 0.  out may be qkv (then only query and key heads are written), else no overlap; the gains overlap
+ *   no part of out (EINVAL).  No host numbers.  Up to 2^27 rows, as otas_rotary. */
+typedef struct {
+  const void *q_gain, *k_gain;
+  float eps;
+  int32_t center, per_head;
+} otas_head_norm_desc;
+otas_status otas_norm_rotary(otas_ctx *ctx, const void *qkv, int64_t T, int32_t kv_heads, const otas_head_norm_desc *norm,
+                             const int32_t *positions, const otas_rotary_desc *rope, void *out);
+
+/* Attention over packed rows through a sliding window, with first tokens that stay visible: row i of a query sees row j of it where
+ *   j <= i  and  (i - j < window or j < sinks)                                         (i, j counted within the query),
+ * so at least itself.  window >= 1 (EINVAL), INT32_MAX or anything past the longest query: all rows before it;  sinks >= 0.
+ * score, o, what infinities and NaN in rows that are not seen do (nothing), lengths as in otas_attention_masked; the distance for slopes is
+ * i - j.  Keys outside window and sinks are not read.  Host numbers: B + 1. */
+otas_status otas_attention_window(otas_ctx *ctx, const void *qkv, int32_t kv_heads, const int32_t *offsets, int32_t B,
+                                  int32_t window, int32_t sinks, const otas_score_desc *score, void *o);
+
+/* The same for the last tokens of a cache whose entries lie in the order of their tokens (as otas_cache_append leaves them; not after
+ * otas_cache_evict): a query's n rows are its last n entries, which are in the cache already, and row i is entry
+ * t = length[q] - n + i, which sees the entries j of its slot with j <= t and (t - j < window or j < sinks).
+ *   qkv dev [T, (H + 2 kv_heads) d_h], kv_heads the cache's: only the query heads are read.  One row is a token that was just appended, many
+ *   are a run of drafts or a prompt taken in pieces.
+ *   offsets, slot, length host: 0 <= rows of a query <= length[q] (EINVAL); slots may repeat
+ *   score NULL = all defaults; the distance for slopes is t - j.  Neither the cache's positions nor its mass are touched.
+ *   workspace dev >= otas_attention_recent_workspace_bytes for the same kv_heads, offsets, length, window and sinks, 256-byte aligned
+ *   o dev [T, D]; o and the workspace overlap no other array.   Host numbers: 3 B + 1.
+ * d_h a multiple of 8 up to 128 (EUNSUPPORTED).  Keys and values that a row does not see do not reach it.  A row that sees a key or value
+ * that is not finite is not finite where it counts, or all NaN.  f32 models form products from operands cut into three
+ * bf16 pieces each, without loss but for the product of the two last (2^-30 of the product): sums are float.  bf16 models round
+ * weights as otas_attention_masked does.  The split of a long window between workgroups, and with it the last bits of o, depends on the whole
+ * call's lengths. */
+size_t otas_attention_recent_workspace_bytes(const otas_ctx *ctx, int32_t kv_heads, const int32_t *offsets, const int32_t *length,
+                                             int32_t B, int32_t window, int32_t sinks);
+otas_status otas_attention_recent(otas_ctx *ctx, const otas_kv_cache *cache, const void *qkv, const int32_t *offsets,
+                                  const int32_t *slot, const int32_t *length, int32_t B, int32_t window, int32_t sinks,
+                                  const otas_score_desc *score, void *workspace, size_t workspace_bytes, void *o);
+
+/* A cache in 4 bits an element (the E2M1 elements and E8M0 scales of the OCP Microscaling formats, blocks of 32).  The elements of a head
+ * of an entry form groups of OTAS_CACHE4_GROUP, the last one of the rest.  A group has one scale 2^e: e is the smallest
+ * exponent with max |x| <= 7 2^e, held to [-125, 125], so that no element is off by more than half a step of its place in
+ *   0, 1/2, 1, 3/2, 2, 3, 4, 6   (times 2^e)
+ * (but beyond 7 2^125, which becomes 6 2^125).  An element is held as the nearest of these, of two as near the one whose code (its
+ * place in the list) is even, with the sign in bit 3; an element at an even place lies in the low half of its byte.  The scale is held as
+ * e + 127.  A group with an element that is not finite is held as scale 255, codes 0: all of it reads as NaN.
+ *   k, v              dev [slots, kv_heads, capacity, d_h / 2] bytes, aligned to 16
+ *   k_scales, v_scales dev [slots, kv_heads, ceil(d_h / 32), capacity] bytes, aligned to 16
+ * capacity a multiple of 32 (EINVAL);  d_h a multiple of 8 (EUNSUPPORTED from every call).  The four arrays overlap neither each
+ * other nor any other array of a call (EINVAL where they do).  Entries are tokens in order: there is no position and no mass.
+ * What lies behind a slot's entries is not used, whatever it holds, and not written. */
+#define OTAS_CACHE4_GROUP 32
+typedef struct {
+  void *k, *v;
+  void *k_scales, *v_scales;
+  int32_t slots, kv_heads, capacity;
+} otas_kv_cache4;
+
+/* otas_cache_append for it: rows[i] (NULL: row i), i = row_offsets[q] .. row_offsets[q+1] - 1, become entries length[q],
+ * length[q] + 1, .. of slot[q].  Arguments and limits as there.   Host numbers: 3 B + 1, and with rows row_offsets[B] more. */
+otas_status otas_cache4_append(otas_ctx *ctx, const otas_kv_cache4 *cache, const void *qkv, int64_t T, const int32_t *row_offsets,
+                               const int32_t *rows, const int32_t *slot, const int32_t *length, int32_t B, int32_t *length_out);
+
+/* Entries first[q] .. first[q] + (row_offsets[q+1] - row_offsets[q]) - 1 of slot[q] as rows row_offsets[q] .. of kv, in the model's dtype
+ * (which holds them exactly): the key heads, then the value heads.   kv dev [row_offsets[B], 2 kv_heads d_h]; slots may repeat;
+ * what is asked for lies within the capacity (EINVAL).   Host numbers: 3 B + 1. */
+otas_status otas_cache4_read(otas_ctx *ctx, const otas_kv_cache4 *cache, const int32_t *slot, const int32_t *first,
+                             const int32_t *row_offsets, int32_t B, void *kv);
+
+/* otas_attention_recent over it, with the same arguments and workspace.  Products are of the held values, exactly; nothing
+ * is rounded to fewer bits than there. */
+otas_status otas_attention_cache4(otas_ctx *ctx, const otas_kv_cache4 *cache, const void *qkv, const int32_t *offsets,
+                                  const int32_t *slot, const int32_t *length, int32_t B, int32_t window, int32_t sinks,
+                                  const otas_score_desc *score, void *workspace, size_t workspace_bytes, void *o);
 
 #ifdef __cplusplus
 }

@@ -22,6 +22,7 @@ OTAS_CLOCK_PROBE_MAX_SAMPLES = 65536
 OTAS_ROTARY_HALF, OTAS_ROTARY_INTERLEAVED = 0, 1
 OTAS_ROTARY_PLAIN, OTAS_ROTARY_LINEAR, OTAS_ROTARY_BASE, OTAS_ROTARY_BY_PARTS = 0, 1, 2, 3
 OTAS_DECODE_ARGUMENTS, OTAS_MAX_LONG_SEQ, OTAS_MAX_TREE_NODES = 960, 1048576, 64
+OTAS_CACHE4_GROUP = 32
 _WEIGHT_FIELDS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_proj", "b_proj",
                   "ln2_g", "ln2_b", "w_fc1", "b_fc1", "w_fc2", "b_fc2")
 
@@ -62,6 +63,15 @@ class _ScoreDesc(C.Structure):
 
 class _KVCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("positions", C.c_void_p), ("mass", C.c_void_p),
+                ("slots", C.c_int32), ("kv_heads", C.c_int32), ("capacity", C.c_int32)]
+
+
+class _HeadNormDesc(C.Structure):
+    _fields_ = [("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("eps", C.c_float), ("center", C.c_int32), ("per_head", C.c_int32)]
+
+
+class _KVCache4(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
                 ("slots", C.c_int32), ("kv_heads", C.c_int32), ("capacity", C.c_int32)]
 
 
@@ -131,6 +141,13 @@ def load_library():
         "otas_attention_tree": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, sz, vp]),
         "otas_cache_evict_workspace_bytes": (sz, [vp, vp, vp, i32]),
         "otas_cache_evict": (i32, [vp, vp, vp, vp, vp, i32, i32, vp, vp, sz, vp]),
+        "otas_norm_rotary": (i32, [vp, vp, i64, i32, vp, vp, vp, vp]),
+        "otas_attention_window": (i32, [vp, vp, i32, vp, i32, i32, i32, vp, vp]),
+        "otas_attention_recent_workspace_bytes": (sz, [vp, i32, vp, vp, i32, i32, i32]),
+        "otas_attention_recent": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]),
+        "otas_cache4_append": (i32, [vp, vp, vp, i64, vp, vp, vp, vp, i32, vp]),
+        "otas_cache4_read": (i32, [vp, vp, vp, vp, vp, i32, vp]),
+        "otas_attention_cache4": (i32, [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, sz, vp]),
         "otas_sched_create": (i32, [C.POINTER(_SchedParams), i32, _I32P, i32, _F64P, _F64P, i32, _F64P, _I32P,
                                     C.POINTER(vp)]),
         "otas_sched_destroy": (None, [vp]),
@@ -158,6 +175,8 @@ EXPORTED = ("otas_create", "otas_destroy", "otas_schedule", "otas_workspace_byte
             "otas_clock_probe_start", "otas_clock_probe_read",
             "otas_rotary", "otas_attention_masked", "otas_cache_append", "otas_attention_tree_workspace_bytes",
             "otas_attention_tree", "otas_cache_evict_workspace_bytes", "otas_cache_evict",
+            "otas_norm_rotary", "otas_attention_window", "otas_attention_recent_workspace_bytes", "otas_attention_recent",
+            "otas_cache4_append", "otas_cache4_read", "otas_attention_cache4",
             "otas_sched_create", "otas_sched_destroy", "otas_sched_rate_table", "otas_sched_add_query", "otas_sched_allocate",
             "otas_sched_num_batches", "otas_sched_batch_info", "otas_sched_batch_queries", "otas_sched_estimate",
             "otas_sched_remove")
@@ -249,6 +268,45 @@ class KVCache:
         self.desc = _KVCache(k.data_ptr(), v.data_ptr(), positions.data_ptr(), None if mass is None else mass.data_ptr(),
                              self.slots, self.kv_heads, self.capacity)
         self.address = C.addressof(self.desc)
+
+
+class HeadNorm:
+    """otas_head_norm_desc: q_gain, k_gain of the model's dtype on the GPU ([d_h], per_head: [heads, d_h]) or None (ones)."""
+
+    def __init__(self, q_gain=None, k_gain=None, eps: float = 1e-6, center: bool = False, per_head: bool = False):
+        self.q_gain, self.k_gain, self.per_head = q_gain, k_gain, per_head
+        self.desc = _HeadNormDesc(_ptr(q_gain), _ptr(k_gain), eps, 1 if center else 0, 1 if per_head else 0)
+        self.address = C.addressof(self.desc)
+
+
+class KVCache4:
+    """otas_kv_cache4 on tensors: k, v uint8 [slots, kv_heads, capacity, head width / 2], k_scales, v_scales uint8 [slots, kv_heads,
+    groups of 32 elements, capacity]; contiguous, on one GPU."""
+
+    def __init__(self, k, v, k_scales, v_scales):
+        import torch
+        if k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("k and v must be [slots, kv_heads, capacity, head width / 2]")
+        self.slots, self.kv_heads, self.capacity, half = k.shape
+        self.head_width = 2 * half
+        small = (self.slots, self.kv_heads, -(-self.head_width // OTAS_CACHE4_GROUP), self.capacity)
+        if k_scales.shape != small or v_scales.shape != small:
+            raise ValueError(f"k_scales and v_scales must be {small}")
+        self.device_index = k.get_device()
+        for t in (k, v, k_scales, v_scales):
+            if t.dtype != torch.uint8 or t.get_device() != self.device_index or self.device_index < 0 or not t.is_contiguous():
+                raise ValueError("k, v, k_scales and v_scales must be contiguous uint8 tensors on one GPU")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.desc = _KVCache4(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), self.slots, self.kv_heads, self.capacity)
+        self.address = C.addressof(self.desc)
+
+    @classmethod
+    def empty(cls, slots: int, kv_heads: int, capacity: int, head_width: int, device="cuda") -> "KVCache4":
+        """A cache on new memory, whose content is undefined until it is appended to; capacity a multiple of 32."""
+        import torch
+        groups = -(-head_width // OTAS_CACHE4_GROUP)
+        shapes = 2 * [(slots, kv_heads, capacity, head_width // 2)] + 2 * [(slots, kv_heads, groups, capacity)]
+        return cls(*[torch.empty(s, dtype=torch.uint8, device=device) for s in shapes])
 
 
 def otas_schedule(n0: int, P: int, r: int, n_lead: int, L: int) -> List[int]:
@@ -545,6 +603,79 @@ class Context:
         _check(self._lib.otas_cache_evict(self._h, c, slot.address, length.address, kept.address, B, lead, recent.address, ws, room,
                                           out.ctypes.data), "otas_cache_evict")
         return out
+
+    def otas_norm_rotary(self, qkv, kv_heads, norm, positions, rope, out) -> None:
+        """Norms (norm: HeadNorm) and rotary positions (rope: Rotary) on the query and key heads of packed rows; out may be qkv."""
+        import torch
+        T, W, at = self._need_rows(qkv, kv_heads)
+        to = at if out is qkv else self._need("out", out, (T, W), self.torch_dtype)
+        dh = self.D // self.H
+        for name, gain, heads in (("norm.q_gain", norm.q_gain, self.H), ("norm.k_gain", norm.k_gain, kv_heads)):
+            if gain is not None:
+                self._need(name, gain, (heads, dh) if norm.per_head else (dh,), self.torch_dtype)
+        _check(self._lib.otas_norm_rotary(self._h, at, T, kv_heads, norm.address,
+                                          None if positions is None else self._need("positions", positions, (T,), torch.int32), rope.address, to),
+               "otas_norm_rotary")
+
+    def otas_attention_window(self, qkv, kv_heads, offsets, o, window, sinks=0, score=None) -> None:
+        """Attention over packed rows: every row sees the last `window` rows up to itself and the query's first `sinks`."""
+        T, _, at = self._need_rows(qkv, kv_heads)
+        off = _Ints(offsets, "offsets")
+        if off.last != T:
+            raise ValueError(f"offsets end at {off.last}, qkv has {T} rows")
+        _check(self._lib.otas_attention_window(self._h, at, kv_heads, off.address, off.n - 1, window, sinks, self._need_score(score),
+                                               self._need("o", o, (T, self.D), self.torch_dtype)), "otas_attention_window")
+
+    def otas_attention_recent_workspace_bytes(self, kv_heads, offsets, lengths, window, sinks=0) -> int:
+        off = _Ints(offsets, "offsets")
+        length = _Ints(lengths, "lengths", off.n - 1)
+        return int(self._lib.otas_attention_recent_workspace_bytes(self._h, kv_heads, off.address, length.address, off.n - 1, window, sinks))
+
+    def _attention_last(self, name, c, cache, qkv, offsets, slots, lengths, workspace, o, window, sinks, score) -> None:
+        T, _, at = self._need_rows(qkv, cache.kv_heads)
+        off = _Ints(offsets, "offsets")
+        B = off.n - 1
+        slot, length = _Ints(slots, "slots", B), _Ints(lengths, "lengths", B)
+        if off.last != T:
+            raise ValueError(f"offsets end at {off.last}, qkv has {T} rows")
+        ws, room = self._need_workspace(workspace)
+        _check(getattr(self._lib, name)(self._h, c, at, off.address, slot.address, length.address, B, window, sinks, self._need_score(score), ws, room,
+                                        self._need("o", o, (T, self.D), self.torch_dtype)), name)
+
+    def otas_attention_recent(self, cache, qkv, offsets, slots, lengths, workspace, o, window, sinks=0, score=None) -> None:
+        """Attention of the last tokens of each slot (lengths: entries, theirs among them) over the last `window` and first `sinks` entries."""
+        self._attention_last("otas_attention_recent", self._need_cache(cache), cache, qkv, offsets, slots, lengths, workspace, o, window, sinks, score)
+
+    def otas_attention_cache4(self, cache, qkv, offsets, slots, lengths, workspace, o, window, sinks=0, score=None) -> None:
+        """otas_attention_recent over a cache in 4 bits (KVCache4)."""
+        self._attention_last("otas_attention_cache4", self._need_cache4(cache), cache, qkv, offsets, slots, lengths, workspace, o, window, sinks, score)
+
+    def _need_cache4(self, cache) -> int:
+        if cache.head_width != self.D // self.H or cache.device_index != self.device_index:
+            raise ValueError(f"cache: want head width {self.D // self.H} on GPU {self.device_index}, got {cache.head_width} on GPU {cache.device_index}")
+        return cache.address
+
+    def otas_cache4_append(self, cache, qkv, row_offsets, rows, slots, lengths) -> np.ndarray:
+        """Puts rows (None: all, in order) behind the entries of their queries' slots, in 4 bits; returns the new lengths."""
+        c = self._need_cache4(cache)
+        T, _, at = self._need_rows(qkv, cache.kv_heads)
+        off = _Ints(row_offsets, "row_offsets")
+        B = off.n - 1
+        row, slot, length = _Ints(rows, "rows", off.last), _Ints(slots, "slots", B), _Ints(lengths, "lengths", B)
+        out = np.empty(max(B, 0), dtype=np.int32)
+        _check(self._lib.otas_cache4_append(self._h, c, at, T, off.address, row.address, slot.address, length.address, B, out.ctypes.data),
+               "otas_cache4_append")
+        return out
+
+    def otas_cache4_read(self, cache, slots, first, row_offsets, kv) -> None:
+        """Entries first[q] .. of every query's slot as rows [row_offsets[-1], 2 kv_heads d_h] of the model's dtype."""
+        c = self._need_cache4(cache)
+        off = _Ints(row_offsets, "row_offsets")
+        B = off.n - 1
+        slot, begin = _Ints(slots, "slots", B), _Ints(first, "first", B)
+        shape = (max(off.last or 0, 0), 2 * cache.kv_heads * (self.D // self.H))
+        _check(self._lib.otas_cache4_read(self._h, c, slot.address, begin.address, off.address, B, self._need("kv", kv, shape, self.torch_dtype)),
+               "otas_cache4_read")
 
     def otas_timing_enable(self, on: bool) -> None:
         _check(self._lib.otas_timing_enable(self._h, 1 if on else 0), "otas_timing_enable")

@@ -1,0 +1,641 @@
+// Attention of a query's last tokens over its cache, through a window: otas_attention_recent (a cache of the model's dtype) and
+// otas_attention_cache4 (one of 4 bits an element).
+//   A workgroup has 16 R rows (tokens x heads that share a key head) and a share of the tiles of 32 entries that they see.  Its four
+// waves have the same rows and take tiles in turn, each on its own: no barrier and no LDS before the end, where the four are joined.
+//   Both products are formed transposed on v_mfma_f32_16x16x32_bf16,
+//     S^T[key, row] = K Q^T,   O^T[d, row] += V^T P^T,
+// lane (i = lane & 15, b = lane >> 4) supplying row i and k-slots 8 b .. 8 b + 7 of either operand.  Sums over k do not care which k
+// lies in which slot, nor the rows of a tile which d they are, so that operands are taken from memory as they lie:
+//   K: of a key's head lane b has the b-th run of STEPS words of eight elements (16 bytes at 4 bits and width 128); queries likewise.
+//   V: of the tile's 32 keys lane b has those of 4 j + b, and lane i the head's i-th eight elements of each: V^T's row i of product t is
+//      element 8 i + t.  A pair of keys' elements change places between two registers (v_perm_b32), nothing leaves the lane.
+//   S: rows 4 b + e of the first and second product are keys 4 e + b and 16 + 4 e + b: what lane b needs of P for those keys is what it has.
+// bf16 models: queries, keys and values as they are, weights rounded to bf16 (by 2^-8 of themselves at most, as much as the output's own
+// rounding), their sum unrounded.  f32 models: every float operand x is cut into three bf16 pieces whose sum is x (8 bits each, by
+// truncation, so that none overflows), and the products of all pieces but the last two's are added up.  What is held in 4 bits is one
+// piece.
+#include "attention_tiles.h"
+#include "cache4.h"
+
+namespace otas {
+
+namespace {
+
+struct RecentBuffers {
+  float *sums, *tops;
+  int64_t TH;
+};
+
+__device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
+// The upper halves, or the lower ones, of two words as a pair, the first's in the lower half.
+__device__ __forceinline__ uint32_t uppers(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ uint32_t lowers(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+
+// Pieces of two floats, as pairs.
+__device__ __forceinline__ void cut(float x, float y, uint32_t (&piece)[3]) {
+  constexpr uint32_t upper = 0xFFFF0000u;
+  piece[0] = uppers(bits(x), bits(y));
+  x -= __uint_as_float(bits(x) & upper);
+  y -= __uint_as_float(bits(y) & upper);
+  piece[1] = uppers(bits(x), bits(y));
+  x -= __uint_as_float(bits(x) & upper);
+  y -= __uint_as_float(bits(y) & upper);
+  piece[2] = uppers(bits(x), bits(y));
+}
+
+struct Words { uint32_t x[4]; };   // eight bf16
+__device__ __forceinline__ bf16x8 operand(const Words& w) {
+  bf16x8 f;
+  __builtin_memcpy(&f, &w, 16);
+  return f;
+}
+__device__ __forceinline__ floatx4 product(const Words& a, const Words& b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(a), operand(b), c, 0, 0, 0);
+}
+
+// Eight elements of the model's dtype as pieces.
+template <typename T> constexpr int pieces_of() { return sizeof(T) == 4 ? 3 : 1; }
+template <typename T> struct Eight;
+template <> struct Eight<bf16_t> {
+  uint4 u;
+  __device__ __forceinline__ void load(const char* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void clear() { u = uint4{0, 0, 0, 0}; }
+  template <int I> __device__ __forceinline__ void pair(uint32_t (&piece)[1]) const { piece[0] = I == 0 ? u.x : I == 1 ? u.y : I == 2 ? u.z : u.w; }
+  // Elements that are not finite become 0; whether there were any.
+  __device__ __forceinline__ bool make_finite() {
+    uint32_t* x = &u.x;
+    uint32_t any = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t odd = ((((x[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;   // ones over elements whose exponent is all ones
+      any |= odd;
+      x[k] &= ~odd;
+    }
+    return any != 0;
+  }
+  __device__ __forceinline__ float element(int j) const { const uint32_t w = (&u.x)[j >> 1]; return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16); }
+};
+template <> struct Eight<float> {
+  floatx4 a, b;
+  __device__ __forceinline__ void load(const char* p) { a = *reinterpret_cast<const floatx4*>(p); b = *reinterpret_cast<const floatx4*>(p + 16); }
+  __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
+  template <int I> __device__ __forceinline__ void pair(uint32_t (&piece)[3]) const {
+    if (I < 2) cut(a[2 * I & 3], a[(2 * I & 3) + 1], piece); else cut(b[2 * I & 3], b[(2 * I & 3) + 1], piece);
+  }
+  __device__ __forceinline__ bool make_finite() {
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (!__builtin_isfinite(a[k])) { a[k] = 0.f; any = true; }
+      if (!__builtin_isfinite(b[k])) { b[k] = 0.f; any = true; }
+    }
+    return any;
+  }
+  __device__ __forceinline__ float element(int j) const { return j < 4 ? a[j & 3] : b[j & 3]; }
+};
+
+// What a lane has loaded of a tile, and the operands it makes of that.  KeyPieces: pieces of a key's and a value's elements.
+template <typename T, bool FOUR, int STEPS, bool EXACT> struct Tile;
+
+// Where the heads of a slot lie, and which parts of a tile are a lane's.
+struct Source {
+  const char *k, *v, *ks, *vs;   // the slot's key head; ks, vs: its scales
+  int64_t capacity;
+  int words, key, i, b;          // runs of eight elements a head; the lane's key of the first 16; its places
+};
+
+template <int STEPS, bool EXACT> struct Codes {
+  static constexpr int PIECES = 1, SCALES = STEPS == 3 ? 3 : 1;
+  uint32_t k[2][STEPS], ks[2][SCALES], v[8];
+  uint4 vs[2];
+  __device__ __forceinline__ void load(const Source& s, int tile) {
+    const int64_t row = s.words * 4;
+    const char* k0 = s.k + (int64_t)tile * kRecentTile * row;
+    const char* v0 = s.v + (int64_t)tile * kRecentTile * row;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char* p = k0 + (s.key + 16 * h) * (int)row + s.b * STEPS * 4;
+      if (EXACT) {
+        __builtin_memcpy(k[h], p, STEPS * 4);
+      } else {
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+          const bool there = s.b * STEPS + st < s.words;
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(p + (there ? 4 * st : -s.b * STEPS * 4));
+          k[h][st] = there ? w : 0;
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < SCALES; ++g) {
+        const int group = min(s.b * STEPS + g, s.words - 1) >> 2;
+        ks[h][g] = (uint8_t)s.ks[group * s.capacity + tile * kRecentTile + s.key + 16 * h];
+      }
+    }
+    const int word = min(s.i, s.words - 1);
+    const char* p = v0 + s.b * (int)row + word * 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const uint32_t*>(p + 4 * j * (int)row);
+    const char* q = s.vs + (word >> 2) * s.capacity + tile * kRecentTile;
+    vs[0] = *reinterpret_cast<const uint4*>(q);
+    vs[1] = *reinterpret_cast<const uint4*>(q + 16);
+  }
+  // The lane's key of the first (H = 0) or second 16: its words ST as operands.
+  template <int H, int ST> __device__ __forceinline__ void key(Words (&w)[1]) const {
+    const uint32_t byte = ks[H][SCALES == 1 ? 0 : ST];
+    const float f = scale4(byte);
+    w[0].x[0] = pair4_bf16<0>(k[H][ST], f);
+    w[0].x[1] = pair4_bf16<1>(k[H][ST], f);
+    w[0].x[2] = pair4_bf16<2>(k[H][ST], f);
+    w[0].x[3] = pair4_bf16<3>(k[H][ST], f);
+    if (byte == kNoNumber) w[0].x[0] = 0x7FC07FC0u;   // a product with it is NaN, whatever the others are
+  }
+  __device__ __forceinline__ uint32_t value_byte(int j, int b) const {
+    const uint32_t w = j == 0 ? vs[0].x : j == 1 ? vs[0].y : j == 2 ? vs[0].z : j == 3 ? vs[0].w : j == 4 ? vs[1].x : j == 5 ? vs[1].y : j == 6 ? vs[1].z : vs[1].w;
+    return w >> (8 * b) & 255;
+  }
+  uint32_t vb[8];   // scales of the lane's keys
+  // Values ready for use: keys from `end` on of the tile (their scales may be anything) and groups that are no numbers become 0.
+  // Whether there were any of the latter among the former keys.
+  __device__ __forceinline__ bool prepare(int b, int end, bool) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      vb[j] = value_byte(j, b);
+      if (end < kRecentTile) vb[j] = 4 * j + b < end ? vb[j] : 0;
+      most = max(most, vb[j]);
+    }
+    if (!__any(most == kNoNumber)) return false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (vb[j] == kNoNumber) { vb[j] = 0; v[j] = 0; }
+    return true;
+  }
+  template <int I> __device__ __forceinline__ void value_pair(int j, uint32_t (&piece)[1]) const { piece[0] = pair4_bf16<I>(v[j], scale4(vb[j])); }
+};
+
+template <typename T, int STEPS, bool EXACT> struct Plain {
+  static constexpr int PIECES = pieces_of<T>();
+  Eight<T> k[2][STEPS], v[8];
+  __device__ __forceinline__ void load(const Source& s, int tile) {
+    const int row = s.words * 8 * (int)sizeof(T);
+    const char* k0 = s.k + (int64_t)tile * kRecentTile * row;
+    const char* v0 = s.v + (int64_t)tile * kRecentTile * row;
+    constexpr int run = 8 * (int)sizeof(T);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t last = s.capacity - 1 - (int64_t)tile * kRecentTile;   // the slot may end within the tile
+      const char* p = k0 + min((int64_t)(s.key + 16 * h), last) * row;
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        const int w = s.b * STEPS + st;
+        k[h][st].load(p + (EXACT ? w : min(w, s.words - 1)) * run);
+        if (!EXACT && w >= s.words) k[h][st].clear();
+      }
+    }
+    const char* p = v0 + min(s.i, s.words - 1) * run;
+    const int64_t last = s.capacity - 1 - (int64_t)tile * kRecentTile;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j].load(p + min((int64_t)(4 * j + s.b), last) * row);
+  }
+  template <int H, int ST> __device__ __forceinline__ void key(Words (&w)[PIECES]) const {
+    uint32_t p[PIECES];
+    k[H][ST].template pair<0>(p);
+#pragma unroll
+    for (int n = 0; n < PIECES; ++n) w[n].x[0] = p[n];
+    k[H][ST].template pair<1>(p);
+#pragma unroll
+    for (int n = 0; n < PIECES; ++n) w[n].x[1] = p[n];
+    k[H][ST].template pair<2>(p);
+#pragma unroll
+    for (int n = 0; n < PIECES; ++n) w[n].x[2] = p[n];
+    k[H][ST].template pair<3>(p);
+#pragma unroll
+    for (int n = 0; n < PIECES; ++n) w[n].x[3] = p[n];
+  }
+  // Of a tile that some row does not see all of, values that are not finite become 0 too.
+  __device__ __forceinline__ bool prepare(int b, int end, bool whole) {
+    if (whole) return false;
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (4 * j + b >= end) v[j].clear();
+      any |= v[j].make_finite();
+    }
+    return any;
+  }
+  template <int I> __device__ __forceinline__ void value_pair(int j, uint32_t (&piece)[PIECES]) const { v[j].template pair<I>(piece); }
+};
+
+template <typename T, bool FOUR, int STEPS, bool EXACT> struct TileOf { typedef Plain<T, STEPS, EXACT> type; };
+template <typename T, int STEPS, bool EXACT> struct TileOf<T, true, STEPS, EXACT> { typedef Codes<STEPS, EXACT> type; };
+
+__device__ __forceinline__ float xor16_max(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+}  // namespace
+
+constexpr size_t recent_lds(int steps) { return sizeof(float) * (4 * 2 * 16 + 4 * 16 * (32 * (size_t)steps + 4)); }
+
+// cap, slopes: whether the call has them.
+template <typename T, bool FOUR, int STEPS, bool EXACT, int R>
+__global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, const T* __restrict__ qkv, int H, PlanAny plan, int B, RecentShape shape,
+                                                               int window, int sinks, ScoreArgs sc, RecentBuffers out, T* __restrict__ o) {
+  typedef typename TileOf<T, FOUR, STEPS, EXACT>::type Held;
+  constexpr int NQ = pieces_of<T>(), NK = Held::PIECES, LDO = 32 * STEPS + 4;
+  extern __shared__ __attribute__((aligned(16))) float lds_recent[];
+  // The row groups of a share run side by side on one XCD, whose L2 then has the share once.
+  const int units = B * c.KV * shape.parts;
+  int id = (int)blockIdx.x;
+  const int eights = units & ~7, span = 8 * shape.groups;
+  int group, unit;
+  if (id < eights * shape.groups) {
+    group = id % span / 8;
+    unit = id / span * 8 + id % 8;
+  } else {
+    id -= eights * shape.groups;
+    group = id / (units - eights);
+    unit = eights + id % (units - eights);
+  }
+  const int part = unit % shape.parts, kh = unit / shape.parts % c.KV, q = unit / shape.parts / c.KV, G = H / c.KV;
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G, group0 = group * 16 * R;
+  const int64_t slot = plan.at(B + 1 + q);
+  if (group0 >= rows) return;
+  const WindowTiles tiles = shape.tiles(group, n, G, len, window, sinks);
+  const int begin = part * shape.each, end = min(tiles.count, begin + shape.each);
+  if (begin >= end) return;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, b = lane >> 4;
+  const int words = c.dh / 8;
+  const int64_t head_of = slot * c.KV + kh, row_bytes = FOUR ? words * 4 : c.dh * (int)sizeof(T);
+  Source src;
+  src.k = c.k + head_of * c.capacity * row_bytes;
+  src.v = c.v + head_of * c.capacity * row_bytes;
+  src.ks = FOUR ? c.ks + head_of * c.groups * c.capacity : nullptr;
+  src.vs = FOUR ? c.vs + head_of * c.groups * c.capacity : nullptr;
+  src.capacity = c.capacity;
+  src.words = words;
+  src.key = 4 * (i16 & 3) + (i16 >> 2);
+  src.i = i16;
+  src.b = b;
+
+  const size_t ld = (size_t)(H + 2 * c.KV) * c.dh;
+  Words qf[R][STEPS][NQ];
+  int place[R];          // the row's token
+  float slope2[R];
+  constexpr float log2e = 1.44269504088896340736f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = min(group0 + 16 * r + i16, rows - 1), token = row / G, head = kh * G + row % G;
+    place[r] = len - n + token;
+    slope2[r] = sc.slopes ? sc.slopes[head] * log2e : 0.f;
+    const char* p = reinterpret_cast<const char*>(qkv + (size_t)(base + token) * ld + (size_t)head * c.dh);
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      const int w = b * STEPS + st;
+      Eight<T> x;
+      x.load(p + (EXACT ? w : min(w, words - 1)) * 8 * (int)sizeof(T));
+      if (!EXACT && w >= words) x.clear();
+      uint32_t piece[NQ];
+      x.template pair<0>(piece);
+#pragma unroll
+      for (int m = 0; m < NQ; ++m) qf[r][st][m].x[0] = piece[m];
+      x.template pair<1>(piece);
+#pragma unroll
+      for (int m = 0; m < NQ; ++m) qf[r][st][m].x[1] = piece[m];
+      x.template pair<2>(piece);
+#pragma unroll
+      for (int m = 0; m < NQ; ++m) qf[r][st][m].x[2] = piece[m];
+      x.template pair<3>(piece);
+#pragma unroll
+      for (int m = 0; m < NQ; ++m) qf[r][st][m].x[3] = piece[m];
+    }
+  }
+  // of the workgroup's rows: the first's and the last's token
+  const int p0 = len - n + group0 / G, p1 = len - n + min(group0 + 16 * R, rows) / G - (min(group0 + 16 * R, rows) % G == 0);
+  auto is_whole = [&](int k0) { return k0 + kRecentTile - 1 <= p0 && (k0 > p1 - window || k0 + kRecentTile <= sinks); };
+
+  floatx4 acc[R][8];
+  float m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) acc[r][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float factor = sc.cap > 0.f ? sc.scale / sc.cap : sc.scale * log2e, cap2 = sc.cap * log2e;
+  bool met = false;   // whether this wave took out values that are no numbers
+
+  Held next;
+  if (begin + wave < end) next.load(src, tiles.tile(begin + wave));
+  for (int at = begin + wave; at < end; at += 4) {
+    Held x = next;
+    if (at + 4 < end) next.load(src, tiles.tile(at + 4));
+    const int k0 = tiles.tile(at) * kRecentTile;
+    const bool whole = is_whole(k0);
+    floatx4 s[R][2];
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](auto st_) {
+      constexpr int st = decltype(st_)::value;
+      if constexpr (st < STEPS) {
+        auto half = [&](auto h_) {
+          constexpr int h = decltype(h_)::value;
+          Words kf[NK];
+          x.template key<h, st>(kf);
+#pragma unroll
+          for (int u = 0; u < NK; ++u)
+#pragma unroll
+            for (int w = 0; w < NQ; ++w)
+              if (u + w < 4) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) s[r][h] = product(kf[u], qf[r][st][w], s[r][h]);
+              }
+        };
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
+      }
+    };
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 3>{});
+    Words pf[R][NQ];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (sc.cap > 0.f) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[r][h][e] = cap2 * tanhf(s[r][h][e] * factor);
+      } else {
+        s[r][0] *= factor;
+        s[r][1] *= factor;
+      }
+      const int behind = place[r] - k0 - b;   // the row's distance from the lane's first key
+      if (sc.slopes) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[r][h][e] -= slope2[r] * fabsf((float)(behind - 16 * h - 4 * e));
+      }
+      if (!whole) {
+        const int left = sinks - k0 - b;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = 16 * h + 4 * e;
+            const bool see = (j <= behind) & ((behind - j < window) | (j < left));
+            s[r][h][e] = see ? s[r][h][e] : -INFINITY;
+          }
+      }
+      float mx = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])), fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3])));
+      if (__any(mx > m[r] + 8.f)) {   // a weight may be up to 2^8: no accuracy is lost in a floating format
+        const float top = fmaxf(m[r], xor16_max(xor32_max(mx)));
+        const float alpha = m[r] == top ? 1.f : __builtin_amdgcn_exp2f(m[r] - top);   // equal: also where both are -inf
+        m[r] = top;
+        l[r] *= alpha;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) acc[r][t] *= alpha;
+      }
+      const float top = m[r] == -INFINITY ? 0.f : m[r];   // nothing seen so far: all weights are 0
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[r][h][e] = __builtin_amdgcn_exp2f(s[r][h][e] - top);
+          l[r] += s[r][h][e];
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          if constexpr (NQ == 1) {
+            const bf16x2 v = {(bf16_t)s[r][h][e], (bf16_t)s[r][h][e + 1]};
+            __builtin_memcpy(&pf[r][0].x[2 * h + e / 2], &v, 4);
+          } else {
+            uint32_t piece[3];
+            cut(s[r][h][e], s[r][h][e + 1], piece);
+#pragma unroll
+            for (int w = 0; w < 3; ++w) pf[r][w].x[2 * h + e / 2] = piece[w];
+          }
+        }
+    }
+    met |= x.prepare(b, p1 + 1 - k0, whole);
+    auto column = [&](auto t_) {   // elements 2 t and 2 t + 1 of every eight
+      constexpr int t = decltype(t_)::value;
+      Words lo[NK], hi[NK];
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        uint32_t even[NK], odd[NK];
+        x.template value_pair<t>(j, even);
+        x.template value_pair<t>(j + 1, odd);
+#pragma unroll
+        for (int u = 0; u < NK; ++u) {
+          lo[u].x[j / 2] = lowers(even[u], odd[u]);
+          hi[u].x[j / 2] = uppers(even[u], odd[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < NK; ++u)
+#pragma unroll
+        for (int w = 0; w < NQ; ++w)
+          if (u + w < 4) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              acc[r][2 * t] = product(lo[u], pf[r][w], acc[r][2 * t]);
+              acc[r][2 * t + 1] = product(hi[u], pf[r][w], acc[r][2 * t + 1]);
+            }
+          }
+    };
+    column(std::integral_constant<int, 0>{});
+    column(std::integral_constant<int, 1>{});
+    column(std::integral_constant<int, 2>{});
+    column(std::integral_constant<int, 3>{});
+  }
+
+  if (__any(met)) {   // what was taken out goes to the rows that see it.  Lane b has elements 32 b .. 32 b + 31 of its rows
+    for (int at = begin + wave; at < end; at += 4) {
+      const int k0 = tiles.tile(at) * kRecentTile;
+      if (!FOUR && is_whole(k0)) continue;
+      for (int j = 0; j < kRecentTile && k0 + j <= p1; ++j) {
+        const int key = k0 + j;
+        if constexpr (FOUR) {
+          if (b >= c.groups || (uint8_t)src.vs[b * c.capacity + key] != kNoNumber) continue;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const bool see = key <= place[r] && (place[r] - key < window || key < sinks);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (FOUR) {
+#pragma unroll
+              for (int t = 0; t < 8; ++t) acc[r][t][e] = see ? __uint_as_float(0x7FC00000u) : acc[r][t][e];
+            } else if (4 * b + e < words) {
+              Eight<T> x;
+              x.load(src.v + key * row_bytes + (4 * b + e) * 8 * (int)sizeof(T));
+#pragma unroll
+              for (int t = 0; t < 8; ++t) {
+                const float f = x.element(t);
+                acc[r][t][e] += see && !__builtin_isfinite(f) ? f : 0.f;
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // The four waves' sums into one.
+  float* ml = lds_recent;           // [4][2][16]
+  float* osh = lds_recent + 128;    // [4][16][LDO]
+  const bool only = shape.parts_of(tiles) == 1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float sum = xor16_sum(xor32_sum(l[r]));
+    if (r > 0) __syncthreads();
+    if (b == 0) {
+      ml[wave * 32 + i16] = m[r];
+      ml[wave * 32 + 16 + i16] = sum;
+    }
+    __syncthreads();
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * 32 + i16]);
+    const float f = to_top(m[r], top);
+    float* mine = osh + (wave * 16 + i16) * LDO;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int d = 8 * (4 * b + e);
+      if (d < c.dh) {
+        *reinterpret_cast<floatx4*>(mine + d) = floatx4{acc[r][0][e] * f, acc[r][1][e] * f, acc[r][2][e] * f, acc[r][3][e] * f};
+        *reinterpret_cast<floatx4*>(mine + d + 4) = floatx4{acc[r][4][e] * f, acc[r][5][e] * f, acc[r][6][e] * f, acc[r][7][e] * f};
+      }
+    }
+    __syncthreads();
+    const int ri = tid >> 4, row = group0 + 16 * r + ri;
+    if (row >= rows) continue;
+    float most = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) most = fmaxf(most, ml[w * 32 + ri]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total += ml[w * 32 + 16 + ri] * to_top(ml[w * 32 + ri], most);
+    const int64_t to = (int64_t)(base + row / G) * H + kh * G + row % G;
+    for (int d = (tid & 15) * 4; d < c.dh; d += 64) {
+      floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) v += *reinterpret_cast<const floatx4*>(osh + (w * 16 + ri) * LDO + d);
+      if (only) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        Quad<T> y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y.x[e] = from_float<T>(total == 0.f ? 0.f : v[e] * inv);
+        *reinterpret_cast<Quad<T>*>(o + to * c.dh + d) = y;
+      } else {
+        *reinterpret_cast<floatx4*>(out.sums + ((int64_t)part * out.TH + to) * c.dh + d) = v;
+        if (d == 0) {
+          out.tops[2 * (part * out.TH + to)] = most;
+          out.tops[2 * (part * out.TH + to) + 1] = total;
+        }
+      }
+    }
+  }
+}
+
+// The parts of every row of several, a wave a row: lane d has elements 2 d and 2 d + 1.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan, int B, int H, int G, int dh, RecentShape shape, int window, int sinks,
+                                                                    RecentBuffers in, T* __restrict__ o) {
+  const int lane = (int)threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  if (at >= in.TH) return;
+  const int token = (int)(at / H), head = (int)(at % H);
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (plan.at(mid) <= token) lo = mid; else hi = mid;
+  }
+  const int base = plan.at(lo), n = plan.at(lo + 1) - base, row = (token - base) * G + head % G;
+  const int parts = shape.parts_of(shape.tiles(row / shape.rows, n, G, plan.at(2 * B + 1 + lo), window, sinks));
+  if (parts <= 1) return;   // written already
+  const bool mine = 2 * lane < dh;
+  float2 acc = {0.f, 0.f};
+  float top = -INFINITY, total = 0.f;
+  for (int p0 = 0; p0 < parts; p0 += 8) {   // eight at a time, so that their loads overlap
+    float2 t[8], v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t p = min(p0 + i, parts - 1) * in.TH + at;
+      t[i] = *reinterpret_cast<const float2*>(in.tops + 2 * p);
+      v[i] = *reinterpret_cast<const float2*>(in.sums + p * dh + (mine ? 2 * lane : 0));
+    }
+    float most = top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = fmaxf(most, t[i].x);
+    const float f = to_top(top, most);
+    acc.x *= f; acc.y *= f; total *= f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p0 + i < parts) {   // wave-uniform; also where the factor is 0: NaN stays
+        const float k = to_top(t[i].x, most);
+        total += k * t[i].y;
+        acc.x += k * v[i].x;
+        acc.y += k * v[i].y;
+      }
+    top = most;
+  }
+  if (!mine) return;
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  struct alignas(2 * sizeof(T)) Pair { T x[2]; } y;
+  y.x[0] = from_float<T>(total == 0.f ? 0.f : acc.x * inv);
+  y.x[1] = from_float<T>(total == 0.f ? 0.f : acc.y * inv);
+  *reinterpret_cast<Pair*>(o + at * dh + 2 * lane) = y;
+}
+
+template <typename T, bool FOUR>
+static hipError_t attention_recent(const Cache4Ref& c, const void* qkv, int H, const PlanAny& p, int B, int64_t TH, int window, int sinks, const ScoreArgs& sc,
+                                   const RecentShape& shape, const RecentBuffers& buf, void* o, hipStream_t s) {
+  const int64_t wgs = (int64_t)B * c.KV * shape.groups * shape.parts;
+  auto run = [&](auto steps, auto exact, auto r) {
+    constexpr int STEPS = decltype(steps)::value;
+    auto kern = attention_recent_kernel<T, FOUR, STEPS, decltype(exact)::value, decltype(r)::value>;
+    kern<<<dim3((unsigned)wgs), dim3(256), recent_lds(STEPS), s>>>(c, (const T*)qkv, H, p, B, shape, window, sinks, sc, buf, (T*)o);
+    return hipGetLastError();
+  };
+  auto by_rows = [&](auto steps, auto exact) {
+    if (shape.rows == 16) return run(steps, exact, std::integral_constant<int, 1>{});
+    if (shape.rows == 32) return run(steps, exact, std::integral_constant<int, 2>{});
+    if constexpr (sizeof(T) == 2) return run(steps, exact, std::integral_constant<int, 4>{});
+    return hipErrorInvalidValue;
+  };
+  auto by_width = [&](auto steps) { return c.dh == 32 * decltype(steps)::value ? by_rows(steps, std::true_type{}) : by_rows(steps, std::false_type{}); };
+  hipError_t e = hipErrorInvalidValue;
+  switch ((c.dh + 31) / 32) {
+    case 1: e = by_width(std::integral_constant<int, 1>{}); break;
+    case 2: e = by_width(std::integral_constant<int, 2>{}); break;
+    case 3: e = by_width(std::integral_constant<int, 3>{}); break;
+    case 4: e = by_width(std::integral_constant<int, 4>{}); break;
+  }
+  if (e != hipSuccess || shape.parts <= 1) return e;
+  attention_recent_join_kernel<T><<<dim3((unsigned)((TH + 3) / 4)), dim3(256), 0, s>>>(p, B, H, H / c.KV, c.dh, shape, window, sinks, buf, (T*)o);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention_recent(int dtype, bool four, const Cache4Ref& c, const void* qkv, int H, const int32_t* plan, size_t count,
+                                   const int32_t* d_plan, int B, int64_t T, int window, int sinks, const ScoreArgs& sc, const RecentShape& shape,
+                                   float* workspace, void* o, hipStream_t s) {
+  if (T <= 0) return hipSuccess;
+  const int64_t TH = T * H;
+  if ((int64_t)B * c.KV * shape.groups * shape.parts > kMostGroups || (TH + 3) / 4 > kMostGroups) return kTooManyGroups;
+  const PlanAny p = plan_any(plan, count, d_plan);
+  const RecentBuffers buf{workspace + recent_sums_at(shape, TH), workspace, TH};
+  if (dtype == 0)
+    return four ? attention_recent<float, true>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s)
+                : attention_recent<float, false>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s);
+  return four ? attention_recent<bf16_t, true>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s)
+              : attention_recent<bf16_t, false>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s);
+}
+
+}  // namespace otas

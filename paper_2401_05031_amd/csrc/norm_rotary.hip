@@ -1,0 +1,137 @@
+// Norms of query and key heads with rotary positions in the same pass: y = (x - c) r gain, r = 1 / sqrt(mean (x - c)^2 + eps), then the
+// pairs of y turned.  Every byte moves once: bound by HBM.
+//   A head has L lanes of a wave (a power of two), V elements each: sums over a head are exchanges within the wave, and so are
+// the partners of pairs that lie in halves, which go through LDS as floats (a lane's V partners are one run there where the
+// chunks divide the half).  The norm needs all of a head before any of it is stored, so that a call in place needs no more care.
+#include "rotary_angles.h"
+#include "window_kernels.h"
+
+namespace otas {
+
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {   // over every L lanes; all 64 active
+  if (L >= 64) v = xor32_sum(v);
+  if (L >= 32) v = xor16_sum(v);
+  if (L >= 16) {   // a rotation by half of the period that the values have reached is the butterfly's partner
+    v = dpp_sum<dpp_ror(8)>(v);
+    v = dpp_sum<dpp_ror(4)>(v);
+    v = dpp_sum<dpp_ror(2)>(v);
+    return dpp_sum<dpp_ror(1)>(v);
+  }
+  if (L >= 2) v = dpp_sum<kDppXor1>(v);
+  if (L >= 4) v = dpp_sum<kDppXor2>(v);
+  if (L >= 8) v = dpp_sum<kDppHalfMirror>(v);
+  return v;
+}
+
+template <typename T, int V, int L>
+__global__ __launch_bounds__(256) void norm_rotary_kernel(const T* qkv, T* out, const int32_t* __restrict__ positions, int64_t rows, int H, int KV,
+                                                          int dh, int tokens, HeadNormArgs n, RotaryArgs r) {
+  __shared__ float2 cs[8 * 64];
+  __shared__ __attribute__((aligned(16))) float turned[256 * V];
+  const int pairs = r.rot >> 1, all_heads = H + 2 * KV;
+  const int64_t t0 = (int64_t)blockIdx.x * tokens;
+  const int nt = (int)min((int64_t)tokens, rows - t0);
+  if (r.rot) rotary_angles(cs, positions, t0, nt, r);
+  const int lane_of = (int)threadIdx.x % L, own = (int)threadIdx.x / L, e = lane_of * V;
+  const bool there = e < dh;
+  const int heads = out != qkv ? all_heads : H + KV;   // values move only into another array
+  typedef Chunk<T, V> C;
+  float* mine = turned + own * (L * V);
+  const float inv = 1.f / (float)dh;
+  for (int i0 = 0; i0 < nt * heads; i0 += 256 / L) {
+    const int i = i0 + own, t = i / heads, h = i - t * heads;
+    const bool active = there && i < nt * heads;
+    const int64_t at = ((t0 + t) * all_heads + h) * dh + e;
+    C x;
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) y[j] = 0.f;
+    if (active) {
+      x = *reinterpret_cast<const C*>(qkv + at);
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[j] = to_float(x.x[j]);
+    }
+    if (n.center) {
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) s += y[j];
+      const float mean = lanes_sum<L>(s) * inv;
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[j] = there ? y[j] - mean : 0.f;
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s += y[j] * y[j];
+    const float scale = 1.f / sqrtf(fmaf(lanes_sum<L>(s), inv, n.eps));
+    const bool query = h < H, norm = active && h < H + KV;
+    if (norm) {
+      const T* g = (const T*)(query ? n.q_gain : n.k_gain);
+      C gain;
+      if (g) gain = *reinterpret_cast<const C*>(g + (n.per_head ? (int64_t)(query ? h : h - H) * dh : 0) + e);
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[j] = y[j] * scale * (g ? to_float(gain.x[j]) : 1.f);
+    }
+    if (r.rot && !r.interleaved) {   // partners: elements pairs away.  A head's lanes are one wave's, whose LDS operations keep their order
+#pragma unroll
+      for (int j = 0; j < V; j += 4) *reinterpret_cast<floatx4*>(mine + e + j) = floatx4{y[j], y[j + 1], y[j + 2], y[j + 3]};
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (norm && e < r.rot) {
+        const float2* a = cs + t * 64;
+        float z[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const int p = e + j;
+          const bool low = p < pairs;
+          const float2 w = a[low ? p : min(p - pairs, 63)];
+          const float other = mine[low ? p + pairs : p - pairs];
+          z[j] = p < r.rot ? y[j] * w.x + other * (low ? -w.y : w.y) : y[j];
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[j] = z[j];
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    } else if (r.rot && norm) {
+#pragma unroll
+      for (int j = 0; j < V; j += 2)
+        if (e + j < r.rot) {
+          const float2 w = cs[t * 64 + ((e + j) >> 1)];
+          const float lo = y[j], hi = y[j + 1];
+          y[j] = lo * w.x - hi * w.y;
+          y[j + 1] = lo * w.y + hi * w.x;
+        }
+    }
+    if (norm) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) x.x[j] = from_float<T>(y[j]);
+    }
+    if (active) *reinterpret_cast<C*>(out + at) = x;
+  }
+}
+
+hipError_t launch_norm_rotary(int dtype, const void* qkv, void* out, const int32_t* positions, int64_t T, int H, int KV, int dh,
+                              const HeadNormArgs& n, const RotaryArgs& r, hipStream_t s) {
+  if (T <= 0) return hipSuccess;
+  const int tokens = T >= 8192 ? 8 : T >= 2048 ? 4 : T >= 1024 ? 2 : 1;
+  const int64_t wgs = (T + tokens - 1) / tokens;
+  if (wgs > kMostGroups) return kTooManyGroups;
+  auto run = [&](auto zero, auto v, auto lanes) {
+    typedef decltype(zero) E;
+    norm_rotary_kernel<E, decltype(v)::value, decltype(lanes)::value>
+        <<<dim3((unsigned)wgs), dim3(256), 0, s>>>((const E*)qkv, (E*)out, positions, T, H, KV, dh, tokens, n, r);
+    return hipGetLastError();
+  };
+  auto by_lanes = [&](auto zero, auto v) {
+    const int lanes = (dh + decltype(v)::value - 1) / decltype(v)::value;
+    if (lanes <= 1) return run(zero, v, std::integral_constant<int, 1>{});
+    if (lanes <= 2) return run(zero, v, std::integral_constant<int, 2>{});
+    if (lanes <= 4) return run(zero, v, std::integral_constant<int, 4>{});
+    if (lanes <= 8) return run(zero, v, std::integral_constant<int, 8>{});
+    if (lanes <= 16) return run(zero, v, std::integral_constant<int, 16>{});
+    return run(zero, v, std::integral_constant<int, 32>{});
+  };
+  if (dtype == 0) return by_lanes(0.f, std::integral_constant<int, 4>{});
+  if (dh % 8) return by_lanes(bf16_t{}, std::integral_constant<int, 4>{});
+  return by_lanes(bf16_t{}, std::integral_constant<int, 8>{});
+}
+
+}  // namespace otas
