@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libotas.so")
 SOURCES = ["api.hip", "elementwise.hip", "gemm.hip", "attention.hip", "merge.hip", "launch_util.hip", "sched.cpp",
            "decode_api.hip", "rotary.hip", "attention_decode.hip", "attention_masked_bf16.hip",
            "attention_tree_bf16.hip", "evict.hip", "window_api.hip", "norm_rotary.hip", "attention_window.hip",
-           "attention_window_bf16.hip", "attention_recent.hip", "cache4.hip"]
+           "attention_rows_bf16.hip", "attention_recent.hip", "cache4.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]

@@ -21,10 +21,7 @@ namespace otas {
 
 namespace {
 
-struct RecentBuffers {
-  float *sums, *tops;
-  int64_t TH;
-};
+constexpr int kTile = 1 << kRecentShift;
 
 __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
 // The upper halves, or the lower ones, of two words as a pair, the first's in the lower half.
@@ -110,8 +107,8 @@ template <int STEPS, bool EXACT> struct Codes {
   uint4 vs[2];
   __device__ __forceinline__ void load(const Source& s, int tile) {
     const int64_t row = s.words * 4;
-    const char* k0 = s.k + (int64_t)tile * kRecentTile * row;
-    const char* v0 = s.v + (int64_t)tile * kRecentTile * row;
+    const char* k0 = s.k + (int64_t)tile * kTile * row;
+    const char* v0 = s.v + (int64_t)tile * kTile * row;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const char* p = k0 + (s.key + 16 * h) * (int)row + s.b * STEPS * 4;
@@ -128,14 +125,14 @@ template <int STEPS, bool EXACT> struct Codes {
 #pragma unroll
       for (int g = 0; g < SCALES; ++g) {
         const int group = min(s.b * STEPS + g, s.words - 1) >> 2;
-        ks[h][g] = (uint8_t)s.ks[group * s.capacity + tile * kRecentTile + s.key + 16 * h];
+        ks[h][g] = (uint8_t)s.ks[group * s.capacity + tile * kTile + s.key + 16 * h];
       }
     }
     const int word = min(s.i, s.words - 1);
     const char* p = v0 + s.b * (int)row + word * 4;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const uint32_t*>(p + 4 * j * (int)row);
-    const char* q = s.vs + (word >> 2) * s.capacity + tile * kRecentTile;
+    const char* q = s.vs + (word >> 2) * s.capacity + tile * kTile;
     vs[0] = *reinterpret_cast<const uint4*>(q);
     vs[1] = *reinterpret_cast<const uint4*>(q + 16);
   }
@@ -161,7 +158,7 @@ template <int STEPS, bool EXACT> struct Codes {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       vb[j] = value_byte(j, b);
-      if (end < kRecentTile) vb[j] = 4 * j + b < end ? vb[j] : 0;
+      if (end < kTile) vb[j] = 4 * j + b < end ? vb[j] : 0;
       most = max(most, vb[j]);
     }
     if (!__any(most == kNoNumber)) return false;
@@ -178,12 +175,12 @@ template <typename T, int STEPS, bool EXACT> struct Plain {
   Eight<T> k[2][STEPS], v[8];
   __device__ __forceinline__ void load(const Source& s, int tile) {
     const int row = s.words * 8 * (int)sizeof(T);
-    const char* k0 = s.k + (int64_t)tile * kRecentTile * row;
-    const char* v0 = s.v + (int64_t)tile * kRecentTile * row;
+    const char* k0 = s.k + (int64_t)tile * kTile * row;
+    const char* v0 = s.v + (int64_t)tile * kTile * row;
     constexpr int run = 8 * (int)sizeof(T);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t last = s.capacity - 1 - (int64_t)tile * kRecentTile;   // the slot may end within the tile
+      const int64_t last = s.capacity - 1 - (int64_t)tile * kTile;   // the slot may end within the tile
       const char* p = k0 + min((int64_t)(s.key + 16 * h), last) * row;
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
@@ -193,7 +190,7 @@ template <typename T, int STEPS, bool EXACT> struct Plain {
       }
     }
     const char* p = v0 + min(s.i, s.words - 1) * run;
-    const int64_t last = s.capacity - 1 - (int64_t)tile * kRecentTile;
+    const int64_t last = s.capacity - 1 - (int64_t)tile * kTile;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j].load(p + min((int64_t)(4 * j + s.b), last) * row);
   }
@@ -240,29 +237,18 @@ constexpr size_t recent_lds(int steps) { return sizeof(float) * (4 * 2 * 16 + 4 
 
 // cap, slopes: whether the call has them.
 template <typename T, bool FOUR, int STEPS, bool EXACT, int R>
-__global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, const T* __restrict__ qkv, int H, PlanAny plan, int B, RecentShape shape,
-                                                               int window, int sinks, ScoreArgs sc, RecentBuffers out, T* __restrict__ o) {
+__global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, const T* __restrict__ qkv, int H, PlanAny plan, int B, WindowShape shape,
+                                                               ScoreArgs sc, RecentBuffers out, T* __restrict__ o) {
   typedef typename TileOf<T, FOUR, STEPS, EXACT>::type Held;
   constexpr int NQ = pieces_of<T>(), NK = Held::PIECES, LDO = 32 * STEPS + 4;
   extern __shared__ __attribute__((aligned(16))) float lds_recent[];
-  // The row groups of a share run side by side on one XCD, whose L2 then has the share once.
-  const int units = B * c.KV * shape.parts;
-  int id = (int)blockIdx.x;
-  const int eights = units & ~7, span = 8 * shape.groups;
-  int group, unit;
-  if (id < eights * shape.groups) {
-    group = id % span / 8;
-    unit = id / span * 8 + id % 8;
-  } else {
-    id -= eights * shape.groups;
-    group = id / (units - eights);
-    unit = eights + id % (units - eights);
-  }
-  const int part = unit % shape.parts, kh = unit / shape.parts % c.KV, q = unit / shape.parts / c.KV, G = H / c.KV;
-  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G, group0 = group * 16 * R;
+  const WorkPlace work = shape.place((int)blockIdx.x, B * c.KV);
+  const int part = work.part, kh = work.unit % c.KV, q = work.unit / c.KV, G = H / c.KV;
+  const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G, group0 = work.group * 16 * R;
+  const int window = shape.window, sinks = shape.sinks;
   const int64_t slot = plan.at(B + 1 + q);
   if (group0 >= rows) return;
-  const WindowTiles tiles = shape.tiles(group, n, G, len, window, sinks);
+  const WindowTiles tiles = shape.tiles(work.group, n, G, len);
   const int begin = part * shape.each, end = min(tiles.count, begin + shape.each);
   if (begin >= end) return;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, b = lane >> 4;
@@ -313,7 +299,7 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
   }
   // of the workgroup's rows: the first's and the last's token
   const int p0 = len - n + group0 / G, p1 = len - n + min(group0 + 16 * R, rows) / G - (min(group0 + 16 * R, rows) % G == 0);
-  auto is_whole = [&](int k0) { return k0 + kRecentTile - 1 <= p0 && (k0 > p1 - window || k0 + kRecentTile <= sinks); };
+  auto is_whole = [&](int k0) { return k0 + kTile - 1 <= p0 && (k0 > p1 - window || k0 + kTile <= sinks); };
 
   floatx4 acc[R][8];
   float m[R], l[R];
@@ -332,7 +318,7 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
   for (int at = begin + wave; at < end; at += 4) {
     Held x = next;
     if (at + 4 < end) next.load(src, tiles.tile(at + 4));
-    const int k0 = tiles.tile(at) * kRecentTile;
+    const int k0 = tiles.tile(at) * kTile;
     const bool whole = is_whole(k0);
     floatx4 s[R][2];
 #pragma unroll
@@ -458,9 +444,9 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
 
   if (__any(met)) {   // what was taken out goes to the rows that see it.  Lane b has elements 32 b .. 32 b + 31 of its rows
     for (int at = begin + wave; at < end; at += 4) {
-      const int k0 = tiles.tile(at) * kRecentTile;
+      const int k0 = tiles.tile(at) * kTile;
       if (!FOUR && is_whole(k0)) continue;
-      for (int j = 0; j < kRecentTile && k0 + j <= p1; ++j) {
+      for (int j = 0; j < kTile && k0 + j <= p1; ++j) {
         const int key = k0 + j;
         if constexpr (FOUR) {
           if (b >= c.groups || (uint8_t)src.vs[b * c.capacity + key] != kNoNumber) continue;
@@ -546,7 +532,7 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
 
 // The parts of every row of several, a wave a row: lane d has elements 2 d and 2 d + 1.
 template <typename T>
-__global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan, int B, int H, int G, int dh, RecentShape shape, int window, int sinks,
+__global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan, int B, int H, int G, int dh, WindowShape shape,
                                                                     RecentBuffers in, T* __restrict__ o) {
   const int lane = (int)threadIdx.x & 63;
   const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -558,7 +544,7 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
     if (plan.at(mid) <= token) lo = mid; else hi = mid;
   }
   const int base = plan.at(lo), n = plan.at(lo + 1) - base, row = (token - base) * G + head % G;
-  const int parts = shape.parts_of(shape.tiles(row / shape.rows, n, G, plan.at(2 * B + 1 + lo), window, sinks));
+  const int parts = shape.parts_of(shape.tiles(row / shape.rows, n, G, plan.at(2 * B + 1 + lo)));
   if (parts <= 1) return;   // written already
   const bool mine = 2 * lane < dh;
   float2 acc = {0.f, 0.f};
@@ -595,47 +581,48 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
 }
 
 template <typename T, bool FOUR>
-static hipError_t attention_recent(const Cache4Ref& c, const void* qkv, int H, const PlanAny& p, int B, int64_t TH, int window, int sinks, const ScoreArgs& sc,
-                                   const RecentShape& shape, const RecentBuffers& buf, void* o, hipStream_t s) {
+static hipError_t attention_recent(const Cache4Ref& c, const void* qkv, int H, const PlanAny& p, int B, const ScoreArgs& sc, const WindowShape& shape,
+                                   const RecentBuffers& buf, void* o, hipStream_t s) {
   const int64_t wgs = (int64_t)B * c.KV * shape.groups * shape.parts;
   auto run = [&](auto steps, auto exact, auto r) {
     constexpr int STEPS = decltype(steps)::value;
     auto kern = attention_recent_kernel<T, FOUR, STEPS, decltype(exact)::value, decltype(r)::value>;
-    kern<<<dim3((unsigned)wgs), dim3(256), recent_lds(STEPS), s>>>(c, (const T*)qkv, H, p, B, shape, window, sinks, sc, buf, (T*)o);
+    kern<<<dim3((unsigned)wgs), dim3(256), recent_lds(STEPS), s>>>(c, (const T*)qkv, H, p, B, shape, sc, buf, (T*)o);
     return hipGetLastError();
   };
   auto by_rows = [&](auto steps, auto exact) {
-    if (shape.rows == 16) return run(steps, exact, std::integral_constant<int, 1>{});
-    if (shape.rows == 32) return run(steps, exact, std::integral_constant<int, 2>{});
-    if constexpr (sizeof(T) == 2) return run(steps, exact, std::integral_constant<int, 4>{});
-    return hipErrorInvalidValue;
+    return shape.rows == 16 ? run(steps, exact, std::integral_constant<int, 1>{}) : run(steps, exact, std::integral_constant<int, 2>{});
   };
   auto by_width = [&](auto steps) { return c.dh == 32 * decltype(steps)::value ? by_rows(steps, std::true_type{}) : by_rows(steps, std::false_type{}); };
-  hipError_t e = hipErrorInvalidValue;
   switch ((c.dh + 31) / 32) {
-    case 1: e = by_width(std::integral_constant<int, 1>{}); break;
-    case 2: e = by_width(std::integral_constant<int, 2>{}); break;
-    case 3: e = by_width(std::integral_constant<int, 3>{}); break;
-    case 4: e = by_width(std::integral_constant<int, 4>{}); break;
+    case 1: return by_width(std::integral_constant<int, 1>{});
+    case 2: return by_width(std::integral_constant<int, 2>{});
+    case 3: return by_width(std::integral_constant<int, 3>{});
+    case 4: return by_width(std::integral_constant<int, 4>{});
   }
-  if (e != hipSuccess || shape.parts <= 1) return e;
-  attention_recent_join_kernel<T><<<dim3((unsigned)((TH + 3) / 4)), dim3(256), 0, s>>>(p, B, H, H / c.KV, c.dh, shape, window, sinks, buf, (T*)o);
-  return hipGetLastError();
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_attention_recent(int dtype, bool four, const Cache4Ref& c, const void* qkv, int H, const int32_t* plan, size_t count,
-                                   const int32_t* d_plan, int B, int64_t T, int window, int sinks, const ScoreArgs& sc, const RecentShape& shape,
-                                   float* workspace, void* o, hipStream_t s) {
+                                   const int32_t* d_plan, int B, int64_t T, const ScoreArgs& sc, const WindowShape& shape, float* workspace, void* o,
+                                   hipStream_t s) {
   if (T <= 0) return hipSuccess;
   const int64_t TH = T * H;
   if ((int64_t)B * c.KV * shape.groups * shape.parts > kMostGroups || (TH + 3) / 4 > kMostGroups) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   const RecentBuffers buf{workspace + recent_sums_at(shape, TH), workspace, TH};
-  if (dtype == 0)
-    return four ? attention_recent<float, true>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s)
-                : attention_recent<float, false>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s);
-  return four ? attention_recent<bf16_t, true>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s)
-              : attention_recent<bf16_t, false>(c, qkv, H, p, B, TH, window, sinks, sc, shape, buf, o, s);
+  hipError_t e;
+  if (shape.rows == 128)
+    e = launch_attention_rows_bf16(four, c, qkv, H, plan, count, d_plan, B, sc, shape, buf, o, s);
+  else if (dtype == 0)
+    e = four ? attention_recent<float, true>(c, qkv, H, p, B, sc, shape, buf, o, s) : attention_recent<float, false>(c, qkv, H, p, B, sc, shape, buf, o, s);
+  else
+    e = four ? attention_recent<bf16_t, true>(c, qkv, H, p, B, sc, shape, buf, o, s) : attention_recent<bf16_t, false>(c, qkv, H, p, B, sc, shape, buf, o, s);
+  if (e != hipSuccess || shape.parts <= 1) return e;
+  const dim3 grid((unsigned)((TH + 3) / 4)), block(256);
+  if (dtype == 0) attention_recent_join_kernel<float><<<grid, block, 0, s>>>(p, B, H, H / c.KV, c.dh, shape, buf, (float*)o);
+  else attention_recent_join_kernel<bf16_t><<<grid, block, 0, s>>>(p, B, H, H / c.KV, c.dh, shape, buf, (bf16_t*)o);
+  return hipGetLastError();
 }
 
 }  // namespace otas

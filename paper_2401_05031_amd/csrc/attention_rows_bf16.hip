@@ -1,0 +1,290 @@
+// Attention through a window in bf16 for many rows: otas_attention_window, and otas_attention_recent and otas_attention_cache4 where a query
+// has more than 32 rows a key head.  Four waves of 32 rows each walk the keys that any of them sees in tiles of 64; while one LDS buffer
+// is worked on, the other is filled; one barrier a tile, as in attention_masked_bf16.hip.
+//   Rows are tokens x heads that share a key head, one after the other: what rows see moves with their tokens, and a workgroup
+// walks all that any of its rows sees.  With a window w, 128 rows of one head walk w + 128 keys, of which a wave sees w + 32; of eight heads they
+// walk w + 16 and a wave sees w + 4.
+//   Keys of the model's dtype travel from global memory straight into LDS.  Keys in 4 bits are asked for a tile ahead, 16 bytes of a
+// group a thread, and written to LDS as bf16, which holds them exactly, beneath the products of the tile before.
+#include "attention_tiles.h"
+#include "cache4.h"
+
+namespace otas {
+
+namespace {
+constexpr int kKeys = 1 << kRowsShift;
+}
+
+// A tile's groups of 32 elements in 4 bits, one of keys and one of values a thread.
+template <int DH> struct GroupLoader {
+  typedef TileRows<DH> R;
+  static constexpr int GROUPS = (DH + 31) / 32, TOTAL = kKeys * GROUPS;   // at most 256
+  static constexpr int LAST = DH % 32 / 8;                                // words of the last group, 0: all four
+  static_assert(TOTAL <= 256, "a group a thread");
+  const char *k, *v, *ks, *vs;   // the thread's
+  uint32_t kw[4], vw[4], kb, vb;
+  int64_t capacity;
+  int row, g;
+  bool mine;
+  __device__ __forceinline__ void begin(const char* k_, const char* v_, const char* ks_, const char* vs_, int64_t capacity_, int tid) {
+    capacity = capacity_;
+    mine = tid < TOTAL;
+    row = min(tid, TOTAL - 1) / GROUPS;
+    g = min(tid, TOTAL - 1) - row * GROUPS;
+    k = k_ + row * (DH / 2) + g * 16;
+    v = v_ + row * (DH / 2) + g * 16;
+    ks = ks_ + g * capacity + row;
+    vs = vs_ + g * capacity + row;
+  }
+  __device__ __forceinline__ void load(int tile) {   // the capacity is a multiple of 32: where the tile runs past it, its upper half is its lower
+    const int64_t at = (int64_t)tile * kKeys - ((int64_t)tile * kKeys + row < capacity ? 0 : 32);
+    auto words = [&](const char* p, uint32_t (&w)[4]) {
+      if (LAST == 0) {
+        __builtin_memcpy(w, p, 16);
+      } else {
+        __builtin_memcpy(w, p, 4 * LAST);
+        w[2] = w[3] = 0;
+        if (g < GROUPS - 1) __builtin_memcpy(w + LAST, p + 4 * LAST, 16 - 4 * LAST);
+      }
+    };
+    words(k + at * (DH / 2), kw);
+    words(v + at * (DH / 2), vw);
+    kb = *reinterpret_cast<const uint8_t*>(ks + at);
+    vb = *reinterpret_cast<const uint8_t*>(vs + at);
+  }
+  // Keys from `end` of the tile on, whose scales may be anything, count as 0, and so do groups of values that are no numbers.  Whether
+  // there were any of the latter before `end`.
+  __device__ __forceinline__ bool store(char* __restrict__ keys, char* __restrict__ values, int end) const {
+    if (!mine) return false;
+    const bool here = row < end, odd = here && vb == kNoNumber;
+    auto write = [&](char* to, const uint32_t (&w)[4], float f, uint32_t all, bool key) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (LAST != 0 && c >= LAST && g == GROUPS - 1) break;
+        const uint4 u = {pair4_bf16<0>(w[c], f) | all, pair4_bf16<1>(w[c], f) | all, pair4_bf16<2>(w[c], f) | all, pair4_bf16<3>(w[c], f) | all};
+        const int p = g * 4 + c;
+        *reinterpret_cast<uint4*>(to + row * R::ROW_BYTES + (key ? R::key_piece(row, p) : R::value_piece(row, p)) * 16) = u;
+      }
+    };
+    write(keys, kw, scale4(kb), kb == kNoNumber ? 0x7FC07FC0u : 0u, true);
+    const uint32_t none[4] = {0, 0, 0, 0};
+    if (!here || odd) write(values, none, 1.f, 0, false); else write(values, vw, scale4(vb), 0, false);
+    return odd;
+  }
+};
+
+template <int DH> constexpr size_t rows_buffer() { return 2 * TileRows<DH>::bytes(kKeys) + value_slack<DH>(); }
+template <int DH> constexpr size_t rows_lds() { return 2 * rows_buffer<DH>() + 16; }
+
+template <int DH, bool FOUR, int CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(Cache4Ref c, const bf16_t* __restrict__ qkv, int H, PlanAny plan, int B, WindowShape shape,
+                                                                     ScoreArgs sc, CapArgs cap, RecentBuffers out, bf16_t* __restrict__ o) {
+  typedef TileRows<DH> R;
+  constexpr size_t KB = R::bytes(kKeys), BUF = rows_buffer<DH>();   // keys | values | slack
+  constexpr int ROWS = 128;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const WorkPlace at = shape.place((int)blockIdx.x, B * c.KV);
+  const int kh = at.unit % c.KV, q = at.unit / c.KV, G = H / c.KV, group0 = at.group * ROWS;
+  const bool packed = !FOUR && c.k == nullptr;
+  const int base = plan.at(q), n = plan.at(q + 1) - base, rows = n * G;
+  if (group0 >= rows) return;
+  const int len = packed ? n : plan.at(2 * B + 1 + q), place0 = len - n;
+  const WindowTiles tiles = shape.tiles(at.group, n, G, len);
+  const int begin = at.part * shape.each, end = min(tiles.count, begin + shape.each);
+  if (begin >= end) return;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fk = lane >> 5;
+  const int wrow0 = group0 + wave * 32, row = min(wrow0 + fr, rows - 1), token = row / G, head = kh * G + row % G, place = place0 + token;
+  const bool active = wrow0 < rows;
+  const size_t ld = (size_t)(H + 2 * c.KV) * DH;
+  const bf16_t* first = qkv + (size_t)base * ld;
+  const int64_t slot_head = packed ? 0 : (int64_t)plan.at(B + 1 + q) * c.KV + kh;
+  const char *kbase, *vbase;
+  if (packed) {
+    kbase = reinterpret_cast<const char*>(first + (size_t)(H + kh) * DH);
+    vbase = reinterpret_cast<const char*>(first + (size_t)(H + c.KV + kh) * DH);
+  } else {
+    const int64_t bytes = slot_head * c.capacity * (FOUR ? DH / 2 : 2 * DH);
+    kbase = c.k + bytes;
+    vbase = c.v + bytes;
+  }
+  const uint32_t ldb = (uint32_t)((packed ? ld : DH) * sizeof(bf16_t));
+  // places of the workgroup's rows and of the wave's
+  const int p0 = place0 + group0 / G, p1 = place0 + (min(group0 + ROWS, rows) - 1) / G;
+  const int w0 = place0 + min(wrow0, rows - 1) / G, w1 = place0 + (min(wrow0 + 32, rows) - 1) / G;
+  const int window = shape.window, sinks = shape.sinks;
+
+  TileLoader<DH, kKeys, 4, false> key_loader;
+  TileLoader<DH, kKeys, 4, true> value_loader;
+  GroupLoader<DH> groups;
+  if constexpr (FOUR) {
+    const int64_t scales = slot_head * c.groups * c.capacity;
+    groups.begin(kbase, vbase, c.ks + scales, c.vs + scales, c.capacity, tid);
+  } else {
+    key_loader.begin(wave, lane);
+    value_loader.begin(wave, lane);
+  }
+  auto fetch = [&](int t, char* buf) {
+    const size_t from = (size_t)t * kKeys * ldb;
+    key_loader.load(kbase + from, ldb, len - 1 - t * kKeys, buf);
+    value_loader.load(vbase + from, ldb, len - 1 - t * kKeys, buf + KB);
+  };
+  const Score2 score = Score2::of(sc, BIAS ? sc.slopes[head] : 0.f, place);
+  // Whether rows at places a .. b all see all of the tile from kb on, and whether any of them sees any.
+  auto all_see = [&](int a, int b, int kb) { return kb + kKeys - 1 <= a && (kb > b - window || kb + kKeys <= sinks); };
+  auto some_see = [&](int a, int b, int kb) { return kb <= b && (kb + kKeys - 1 > a - window || kb < sinks); };
+  bool met = false;   // whether this thread took out a value that is not finite
+
+  if constexpr (FOUR) {
+    groups.load(tiles.tile(begin));
+    met |= groups.store(lds, lds + KB, p1 + 1 - tiles.tile(begin) * kKeys);
+    if (begin + 1 < end) groups.load(tiles.tile(begin + 1));
+  } else {
+    fetch(tiles.tile(begin), lds);
+  }
+  WaveRows<DH> w;
+  w.begin(first + (size_t)token * ld + (size_t)head * DH, fk, sc.scale < 0.f);
+  for (int i = begin; i < end; ++i) {
+    char* buf = lds + ((i - begin) & 1 ? BUF : 0);
+    char* other = lds + ((i - begin) & 1 ? 0 : BUF);
+    const int kb = tiles.tile(i) * kKeys;
+    if constexpr (FOUR) {
+      wait_lds_barrier();   // the tile is there, and nobody reads the other buffer any more
+      if (i + 1 < end) {
+        met |= groups.store(other, other + KB, p1 + 1 - tiles.tile(i + 1) * kKeys);
+        if (i + 2 < end) groups.load(tiles.tile(i + 2));
+      }
+    } else {
+      wait_all();   // this wave's part of the tile is there
+      // Of a tile that some row does not see all of, values that are not finite are taken out and come back at the end, to
+      // the rows that see them.
+      if (!all_see(p0, p1, kb)) met |= value_loader.make_finite(buf + KB, lane, [&](int r) { return kb + r <= p1; });
+      wait_lds_barrier();   // all of it, and nobody reads the other buffer any more
+      if (i + 1 < end) fetch(tiles.tile(i + 1), other);
+    }
+    if (active && some_see(w0, w1, kb)) {   // wave-uniform
+      __builtin_amdgcn_s_setprio(0);
+      floatx16 s[2];
+      tile_products<DH, 2>(s, w, buf, 0, fr, fk);
+      short8_t v[WaveRows<DH>::DT];
+      first_values<DH>(v, buf + KB, 0, lane);
+      __builtin_amdgcn_s_setprio(1);   // a wave that needs the vector ALU goes before one at its products, as in attention_masked_bf16.hip
+      const bool whole = all_see(w0, w1, kb);
+      bool done = false;
+      if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);
+      if (CAP && !done) tile_capped<CAP, 2>(s, score, cap);
+      const int behind = place - kb - 4 * fk;   // the row's distance from the lane's first key
+      if (BIAS) {
+        const float near = (float)behind;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float d = near - (float)(32 * b + 8 * (e >> 2) + (e & 3));
+            s[b][e] = fmaf(-score.slope2, fabsf(d), CAP ? s[b][e] : s[b][e] * score.scale2);
+          }
+      }
+      if (!whole) {
+        if (kb >= sinks) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[b][e] = (uint32_t)(behind - (32 * b + 8 * (e >> 2) + (e & 3))) < (uint32_t)window ? s[b][e] : -INFINITY;
+        } else {
+          const int left = sinks - kb - 4 * fk;
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int j = 32 * b + 8 * (e >> 2) + (e & 3);
+              const bool see = (j <= behind) & ((behind - j < window) | (j < left));
+              s[b][e] = see ? s[b][e] : -INFINITY;
+            }
+        }
+      }
+      if (!done) tile_weights<DH, 2>(w, s, CAP || BIAS ? 1.f : score.scale2);
+      __builtin_amdgcn_s_setprio(0);
+      tile_sums<DH, 2>(w, s, v, buf + KB, 0, lane);
+    }
+  }
+  if (any_wave(met, reinterpret_cast<int*>(lds + 2 * BUF), wave, lane)) {   // workgroup-uniform
+    for (int i = begin; i < end; ++i) {
+      const int kb = tiles.tile(i) * kKeys;
+      if (!FOUR && all_see(p0, p1, kb)) continue;
+      for (int j = kb; j < min(kb + kKeys, p1 + 1); ++j) {
+        const bool see = j <= place && (place - j < window || j < sinks);
+#pragma unroll
+        for (int t = 0; t < WaveRows<DH>::DT; ++t) {
+          if constexpr (FOUR) {
+            const bool odd = *reinterpret_cast<const uint8_t*>(c.vs + (slot_head * c.groups + t) * c.capacity + j) == kNoNumber;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w.o[t][e] = odd && see ? __uint_as_float(0x7FC00000u) : w.o[t][e];
+          } else {
+            const bf16_t* v = reinterpret_cast<const bf16_t*>(vbase + (size_t)j * ldb);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              if (t * 32 + g * 8 < DH) add_not_finite(w.o[t], g, v + t * 32 + g * 8 + fk * 4, see);
+          }
+        }
+      }
+    }
+  }
+  const float l = xor32_sum(w.l);
+  if (wrow0 + fr >= rows) return;
+  const int64_t to = (int64_t)(base + token) * H + head;
+  const bool only = shape.parts_of(tiles) == 1;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int t = 0; t < WaveRows<DH>::DT; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = t * 32 + g * 8 + fk * 4;
+      if (d < DH) {
+        const floatx4 x = {w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]};
+        if (only) {
+          bf16x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (bf16_t)(l == 0.f ? 0.f : x[e] * inv);
+          *reinterpret_cast<bf16x4*>(o + to * DH + d) = v;
+        } else {
+          *reinterpret_cast<floatx4*>(out.sums + ((int64_t)at.part * out.TH + to) * DH + d) = x;
+        }
+      }
+    }
+  if (!only && fk == 0) {
+    out.tops[2 * (at.part * out.TH + to)] = w.m;
+    out.tops[2 * (at.part * out.TH + to) + 1] = l;
+  }
+}
+
+hipError_t launch_attention_rows_bf16(bool four, const Cache4Ref& c, const void* qkv, int H, const int32_t* plan, size_t count, const int32_t* d_plan, int B,
+                                      const ScoreArgs& sc, const WindowShape& shape, const RecentBuffers& buf, void* o, hipStream_t s) {
+  const int64_t wgs = (int64_t)B * c.KV * shape.groups * shape.parts;
+  if (wgs > kMostGroups) return kTooManyGroups;
+  const PlanAny p = plan_any(plan, count, d_plan);
+  auto run = [&](auto width, auto four_, auto cap, auto bias) {
+    constexpr int DH = decltype(width)::value;
+    auto kern = attention_rows_bf16_kernel<DH, decltype(four_)::value, decltype(cap)::value, decltype(bias)::value>;
+    const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)rows_lds<DH>());
+    if (e != hipSuccess) return e;
+    kern<<<dim3((unsigned)wgs), dim3(256), rows_lds<DH>(), s>>>(c, (const bf16_t*)qkv, H, p, B, shape, sc, CapArgs::of(sc), buf, (bf16_t*)o);
+    return hipGetLastError();
+  };
+  auto pick = [&](auto width, auto four_) {
+    auto with_bias = [&](auto cap) { return sc.slopes ? run(width, four_, cap, std::true_type{}) : run(width, four_, cap, std::false_type{}); };
+    switch (Score2::cap_form(sc.cap)) {
+      case 0: return with_bias(std::integral_constant<int, 0>{});
+      case 1: return with_bias(std::integral_constant<int, 1>{});
+    }
+    return with_bias(std::integral_constant<int, 2>{});
+  };
+  auto either = [&](auto width) { return four ? pick(width, std::true_type{}) : pick(width, std::false_type{}); };
+  switch (c.dh) {
+    case 64: return either(std::integral_constant<int, 64>{});
+    case 80: return either(std::integral_constant<int, 80>{});
+    case 96: return either(std::integral_constant<int, 96>{});
+    case 128: return either(std::integral_constant<int, 128>{});
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace otas

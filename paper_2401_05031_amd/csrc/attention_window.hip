@@ -1,4 +1,4 @@
-// otas_attention_window with fp32 products (f32 models, and bf16 ones of head widths that attention_window_bf16.hip is not built for):
+// otas_attention_window with fp32 products (f32 models, and bf16 ones of head widths that attention_rows_bf16.hip is not built for):
 // row i sees row j of its query where j <= i and (i - j < window or j < sinks).  As attention_masked_f32_kernel, over the blocks of
 // 32 keys that any of a workgroup's 32 rows sees: first those of the sinks before its window, then the window's.
 #include "attention_rows_f32.h"
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_window_f32_ker
                            row0 + 1, max(0, last - window + 1), fk, RowScore::of(sc, h, row)};
   FloatRows<T, DT> r;
   rows_begin<T, DT>(r, first + (size_t)row * ld + (size_t)h * dh, dh, fk);
-  const WindowTiles tiles = window_tiles<32>(row0, last, window, sinks);
+  const WindowTiles tiles = window_tiles(5, row0, last, window, sinks);
   rows_stream<T, DT>(r, keys, dh, wave, tiles.sinks, 4, fr, fk);
   rows_stream<T, DT>(r, keys, dh, tiles.first + ((wave - tiles.sinks) & 3), tiles.first + tiles.count - tiles.sinks, 4, fr, fk);
   T* out = o + ((size_t)base + row0) * H * dh + (size_t)h * dh;
@@ -83,7 +83,12 @@ static hipError_t attention_window_f32(const void* qkv, const int32_t* plan, siz
 hipError_t launch_attention_window(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H,
                                    int KV, int dh, const ScoreArgs& sc, int window, int sinks, void* o, hipStream_t s) {
   if (max_n <= 0) return hipSuccess;
-  if (dtype != 0 && bf16_width(dh)) return launch_attention_window_bf16(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, window, sinks, o, s);
+  if (dtype != 0 && bf16_width(dh)) {
+    WindowShape shape{window, sinks, kRowsShift, 128, (int)(((int64_t)max_n * (H / KV) + 127) / 128), 0, 1};
+    shape.each = window_tiles(kRowsShift, 0, max_n - 1, window, sinks).count;   // all that a group can see
+    return launch_attention_rows_bf16(false, Cache4Ref{nullptr, nullptr, nullptr, nullptr, 0, KV, dh, 0}, qkv, H, plan, count, d_plan, B, sc, shape,
+                                      RecentBuffers{nullptr, nullptr, 0}, o, s);
+  }
   return dtype == 0 ? attention_window_f32<float>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, window, sinks, o, s)
                     : attention_window_f32<bf16_t>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, window, sinks, o, s);
 }

@@ -6,7 +6,7 @@
 
 using namespace otas;
 
-static_assert(OTAS_MAX_LONG_SEQ % kRecentTile == 0, "the last tile of a full cache");
+static_assert(OTAS_MAX_LONG_SEQ % (1 << kRowsShift) == 0, "the last tile of a full cache");
 
 namespace {
 
@@ -75,7 +75,7 @@ otas_status attention_last(otas_ctx* c, const Cache4Ref& cache, bool four, int s
   if (st != OTAS_OK) return st;
   if (cache.dh % 8 != 0) return OTAS_EUNSUPPORTED;
   const int64_t T = offsets[B];
-  const RecentShape shape = recent_shape(c->desc.dtype, four, c->desc.H, cache.KV, offsets, length, B, window, sinks);
+  const WindowShape shape = recent_shape(c->desc.dtype, four, cache.dh, c->desc.H, cache.KV, offsets, length, B, window, sinks);
   const size_t need = recent_workspace_floats(shape, T * c->desc.H, cache.dh) * sizeof(float);
   if (T > 0 && workspace_bytes < need) return OTAS_ENOMEM;
   const size_t in_bytes = qkv_bytes(c, T, cache.KV), out_bytes = rows_bytes(c, T);
@@ -91,8 +91,8 @@ otas_status attention_last(otas_ctx* c, const Cache4Ref& cache, bool four, int s
   if (!on.ok) return OTAS_EDEVICE;
   st = place_plan(c, plan);
   if (st != OTAS_OK) return st;
-  OTAS_LAUNCH_FITTING(K_ATTN, launch_attention_recent(c->desc.dtype, four, cache, qkv, c->desc.H, plan.data(), plan.size(), c->d_plan, B, T, window, sinks,
-                                              sc, shape, (float*)workspace, o, c->stream));
+  OTAS_LAUNCH_FITTING(K_ATTN, launch_attention_recent(c->desc.dtype, four, cache, qkv, c->desc.H, plan.data(), plan.size(), c->d_plan, B, T, sc,
+                                              shape, (float*)workspace, o, c->stream));
   return OTAS_OK;
 }
 
@@ -160,7 +160,7 @@ size_t otas_attention_recent_workspace_bytes(const otas_ctx* c, int32_t kv_heads
     if (recent_ok(offsets, length, B) != OTAS_OK) return 0;
     size_t floats = 1;
     for (bool four : {false, true}) {
-      const RecentShape shape = recent_shape(c->desc.dtype, four, c->desc.H, kv_heads, offsets, length, B, window, sinks);
+      const WindowShape shape = recent_shape(c->desc.dtype, four, c->desc.D / c->desc.H, c->desc.H, kv_heads, offsets, length, B, window, sinks);
       floats = std::max(floats, recent_workspace_floats(shape, (int64_t)offsets[B] * c->desc.H, c->desc.D / c->desc.H));
     }
     return align_up(floats * sizeof(float), kAlign);

@@ -17,23 +17,17 @@ struct HeadNormArgs {
 hipError_t launch_norm_rotary(int dtype, const void* qkv, void* out, const int32_t* positions, int64_t T, int H, int KV, int dh,
                               const HeadNormArgs& n, const RotaryArgs& r, hipStream_t s);
 
-// plan: off [B+1]
-hipError_t launch_attention_window(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H,
-                                   int KV, int dh, const ScoreArgs& sc, int window, int sinks, void* o, hipStream_t s);
-hipError_t launch_attention_window_bf16(const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H, int KV,
-                                        int dh, const ScoreArgs& sc, int window, int sinks, void* o, hipStream_t s);
-
-// Which tiles of TILE keys rows at places p0 .. p1 see through a window, counted through: those of the sinks that lie before the
+// Which tiles of 2^shift keys rows at places p0 .. p1 see through a window, counted through: those of the sinks that lie before the
 // window of the first row, then the window's.
 struct WindowTiles {
   int sinks, first, count;   // tiles 0 .. sinks - 1, then first .. first + count - sinks - 1
   __host__ __device__ int tile(int i) const { return i < sinks ? i : i - sinks + first; }
 };
-template <int TILE> __host__ __device__ inline WindowTiles window_tiles(int p0, int p1, int window, int sinks) {
+__host__ __device__ inline WindowTiles window_tiles(int shift, int p0, int p1, int window, int sinks) {
   const int far = p0 - window + 1 > 0 ? p0 - window + 1 : 0;
-  const int s = ((sinks < far ? sinks : far) + TILE - 1) / TILE;
-  const int first = s > far / TILE ? s : far / TILE;
-  return WindowTiles{s, first, s + p1 / TILE + 1 - first};
+  const int s = ((sinks < far ? sinks : far) + (1 << shift) - 1) >> shift;
+  const int first = s > far >> shift ? s : far >> shift;
+  return WindowTiles{s, first, s + (p1 >> shift) + 1 - first};
 }
 
 // A cache in 4 bits; a cache of the model's dtype has no scales.
@@ -49,46 +43,78 @@ hipError_t launch_cache4_append(int dtype, const Cache4Ref& c, const void* qkv, 
 hipError_t launch_cache4_read(int dtype, const Cache4Ref& c, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int64_t N, void* kv,
                               hipStream_t s);
 
-// How a call over the last tokens of caches is cut up (pure host).  A workgroup has `rows` of a query's n (H / KV) rows of a key head
-// and `each` of the tiles of kRecentTile entries that they see; `parts` = most such shares of a group of rows.
-constexpr int kRecentTile = 32;
-struct RecentShape {
-  int rows, groups, each, parts;
-  __host__ __device__ WindowTiles tiles(int group, int n, int G, int length, int window, int sinks) const {
+// How a call through a window is cut up (pure host).  A workgroup has `rows` of a query's n (H / KV) rows of a key head, and `each` of
+// the tiles of 2^shift keys that they see; `parts` = most such shares of a group of rows.
+constexpr int kRecentShift = 5, kRowsShift = 6;   // of attention_recent.hip, of attention_rows_bf16.hip
+struct WorkPlace { int unit, group, part; };      // unit: the query's and its key head's
+struct WindowShape {
+  int window, sinks, shift, rows, groups, each, parts;
+  __host__ __device__ WindowTiles tiles(int group, int n, int G, int length) const {
     const int last = (group + 1) * rows < n * G ? (group + 1) * rows - 1 : n * G - 1, at = length - n;
-    return window_tiles<kRecentTile>(at + group * rows / G, at + last / G, window, sinks);
+    return window_tiles(shift, at + group * rows / G, at + last / G, window, sinks);
   }
   __host__ __device__ int parts_of(const WindowTiles& t) const { return (t.count + each - 1) / each; }
+  // The row groups of a share run side by side on one XCD, whose L2 then has the share once.
+  __host__ __device__ WorkPlace place(int id, int units) const {
+    const int shares = units * parts, eights = shares & ~7, span = 8 * groups;
+    int group, share;
+    if (id < eights * groups) {
+      group = id % span / 8;
+      share = id / span * 8 + id % 8;
+    } else {
+      id -= eights * groups;
+      group = id / (shares - eights);
+      share = eights + id % (shares - eights);
+    }
+    return WorkPlace{share / parts, group, share % parts};
+  }
 };
-inline RecentShape recent_shape(int dtype, bool four, int H, int KV, const int32_t* off, const int32_t* length, int B, int window, int sinks) {
+// rows of a workgroup of attention_recent.hip, or 128 for attention_rows_bf16.hip
+inline int window_rows(int dtype, int dh, int64_t most) {
+  if (most <= 16) return 16;
+  return most > 32 && dtype != 0 && bf16_width(dh) ? 128 : 32;
+}
+inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, const int32_t* off, const int32_t* length, int B, int window, int sinks) {
   const int G = H / KV;
   int64_t most = 0;
   for (int q = 0; q < B; ++q) most = std::max<int64_t>(most, off[q + 1] - off[q]);
-  RecentShape t{16, 1, 1, 1};
+  WindowShape t{window, sinks, kRecentShift, 16, 1, 1, 1};
   if (most == 0) return t;
-  t.rows = most * G <= 16 ? 16 : most * G <= 32 || dtype == 0 ? 32 : 64;
+  t.rows = window_rows(dtype, dh, most * G);
+  if (t.rows == 128) t.shift = kRowsShift;
   t.groups = (int)((most * G + t.rows - 1) / t.rows);
   int64_t wgs = 0;
   int longest = 1;
   for (int q = 0; q < B; ++q) {
     const int n = off[q + 1] - off[q], mine = (int)(((int64_t)n * G + t.rows - 1) / t.rows);
     wgs += (int64_t)mine * KV;
-    for (int g = 0; g < mine; ++g) longest = std::max(longest, t.tiles(g, n, G, length[q], window, sinks).count);
+    for (int g = 0; g < mine; ++g) longest = std::max(longest, t.tiles(g, n, G, length[q]).count);
   }
-  const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(768 / wgs, (longest + 7) / 8));
+  const int64_t target = t.rows == 128 ? 512 : 768, least = t.rows == 128 ? 4 : 8;
+  const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(target / wgs, (longest + least - 1) / least));
   t.each = (int)((longest + wanted - 1) / wanted);
   t.parts = (longest + t.each - 1) / t.each;
   return t;
 }
 // Floats of workspace: of calls of several parts, for each largest logits and weight sums [T H][2] and sums [T H][dh], from a multiple
 // of four on.
-inline size_t recent_sums_at(const RecentShape& t, int64_t TH) { return ((size_t)TH * 2 * t.parts + 3) / 4 * 4; }
-inline size_t recent_workspace_floats(const RecentShape& t, int64_t TH, int dh) {
+inline size_t recent_sums_at(const WindowShape& t, int64_t TH) { return ((size_t)TH * 2 * t.parts + 3) / 4 * 4; }
+inline size_t recent_workspace_floats(const WindowShape& t, int64_t TH, int dh) {
   return t.parts > 1 ? recent_sums_at(t, TH) + (size_t)TH * t.parts * dh : 0;
 }
+struct RecentBuffers {
+  float *sums, *tops;
+  int64_t TH;
+};
 // plan: off [B+1] | slot [B] | length [B].  four: in 4 bits, else of the model's dtype.
 hipError_t launch_attention_recent(int dtype, bool four, const Cache4Ref& c, const void* qkv, int H, const int32_t* plan, size_t count,
-                                   const int32_t* d_plan, int B, int64_t T, int window, int sinks, const ScoreArgs& sc, const RecentShape& shape,
-                                   float* workspace, void* o, hipStream_t s);
+                                   const int32_t* d_plan, int B, int64_t T, const ScoreArgs& sc, const WindowShape& shape, float* workspace, void* o,
+                                   hipStream_t s);
+// Of several parts it leaves their sums in the buffers.  c.k NULL: packed rows' own keys, plan: off [B+1].
+hipError_t launch_attention_rows_bf16(bool four, const Cache4Ref& c, const void* qkv, int H, const int32_t* plan, size_t count, const int32_t* d_plan, int B,
+                                      const ScoreArgs& sc, const WindowShape& shape, const RecentBuffers& buf, void* o, hipStream_t s);
+// plan: off [B+1]
+hipError_t launch_attention_window(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H,
+                                   int KV, int dh, const ScoreArgs& sc, int window, int sinks, void* o, hipStream_t s);
 
 }  // namespace otas
