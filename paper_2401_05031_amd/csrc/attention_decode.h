@@ -1,6 +1,7 @@
 // What the fp32 and the bf16 attention of the decoder's operators share: which keys a row sees, how products become logits, the
 // lines of a tree of drafts.
 #pragma once
+#include <cstddef>
 #include <type_traits>
 
 #include "common.h"
@@ -24,6 +25,18 @@ inline PlanAny plan_any(const int32_t* plan, size_t count, const int32_t* d_plan
   if (!a.p) std::memcpy(a.v, plan, count * sizeof(int32_t));
   return a;
 }
+
+// The same for kernels whose first argument the plan is: both places by one pointer to constant memory, so that an index that the wave shares is
+// a scalar load (PlanAny::at is a vector's, through an address that may be either: a round trip more before a kernel's first load).
+typedef const __attribute__((address_space(4))) int32_t* PlanInts;
+struct PlanFirst {
+  PlanInts p;
+  static __device__ __forceinline__ PlanFirst of(const PlanAny& plan) {
+    return PlanFirst{plan.p ? (PlanInts)(uintptr_t)plan.p : (PlanInts)__builtin_amdgcn_kernarg_segment_ptr()};
+  }
+  __device__ __forceinline__ int32_t at(int i) const { return p[i]; }
+};
+static_assert(offsetof(PlanAny, v) == 0, "the kernel's first bytes");
 
 // Head i of XCD x where the heads of all queries, counted through, divide among the eight.
 __device__ inline int xcd_head(int x, int i, int H) {

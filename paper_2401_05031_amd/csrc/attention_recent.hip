@@ -7,9 +7,9 @@
 // lane (i = lane & 15, b = lane >> 4) supplying row i and k-slots 8 b .. 8 b + 7 of either operand.  Sums over k do not care which k
 // lies in which slot, nor the rows of a tile which d they are, so that operands are taken from memory as they lie:
 //   K: of a key's head lane b has the b-th run of STEPS words of eight elements (16 bytes at 4 bits and width 128); queries likewise.
-//   V: of the tile's 32 keys lane b has those of 4 j + b, and lane i the head's i-th eight elements of each: V^T's row i of product t is
+//   V: of the tile's 32 keys lane b has 8 b .. 8 b + 7, and lane i the head's i-th eight elements of each: V^T's row i of product t is
 //      element 8 i + t.  A pair of keys' elements change places between two registers (v_perm_b32), nothing leaves the lane.
-//   S: rows 4 b + e of the first and second product are keys 4 e + b and 16 + 4 e + b: what lane b needs of P for those keys is what it has.
+//   S: rows 4 b + e of the first and second product are keys 8 b + e and 8 b + 4 + e: what lane b needs of P for its keys is what it has.
 // bf16 models: queries, keys and values as they are, weights rounded to bf16 (by 2^-8 of themselves at most, as much as the output's own
 // rounding), their sum unrounded.  f32 models: every float operand x is cut into three bf16 pieces whose sum is x (8 bits each, by
 // truncation, so that none overflows), and the products of all pieces but the last two's are added up.  What is held in 4 bits is one
@@ -57,6 +57,7 @@ template <> struct Eight<bf16_t> {
   uint4 u;
   __device__ __forceinline__ void load(const char* p) { u = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void clear() { u = uint4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void negate() { u.x ^= 0x80008000u; u.y ^= 0x80008000u; u.z ^= 0x80008000u; u.w ^= 0x80008000u; }
   template <int I> __device__ __forceinline__ void pair(uint32_t (&piece)[1]) const { piece[0] = I == 0 ? u.x : I == 1 ? u.y : I == 2 ? u.z : u.w; }
   // Elements that are not finite become 0; whether there were any.
   __device__ __forceinline__ bool make_finite() {
@@ -76,6 +77,7 @@ template <> struct Eight<float> {
   floatx4 a, b;
   __device__ __forceinline__ void load(const char* p) { a = *reinterpret_cast<const floatx4*>(p); b = *reinterpret_cast<const floatx4*>(p + 16); }
   __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ void negate() { a = -a; b = -b; }
   template <int I> __device__ __forceinline__ void pair(uint32_t (&piece)[3]) const {
     if (I < 2) cut(a[2 * I & 3], a[(2 * I & 3) + 1], piece); else cut(b[2 * I & 3], b[(2 * I & 3) + 1], piece);
   }
@@ -94,49 +96,54 @@ template <> struct Eight<float> {
 // What a lane has loaded of a tile, and the operands it makes of that.  KeyPieces: pieces of a key's and a value's elements.
 template <typename T, bool FOUR, int STEPS, bool EXACT> struct Tile;
 
-// Where the heads of a slot lie, and which parts of a tile are a lane's.
+// Where the heads of a slot lie, and which parts of a tile are a lane's: bytes from the tile's first key on.
 struct Source {
-  const char *k, *v, *ks, *vs;   // the slot's key head; ks, vs: its scales
+  const char *k, *v, *ks, *vs;       // the slot's key head; ks, vs: its scales
   int64_t capacity;
-  int words, key, i, b;          // runs of eight elements a head; the lane's key of the first 16; its places
+  int words, b;                      // runs of eight elements a head; the lane's block
+  uint32_t row;                      // bytes of a key
+  uint32_t k_at, v_at, ks_at[3], vs_at;
 };
 
 template <int STEPS, bool EXACT> struct Codes {
   static constexpr int PIECES = 1, SCALES = STEPS == 3 ? 3 : 1;
   uint32_t k[2][STEPS], ks[2][SCALES], v[8];
-  uint4 vs[2];
+  uint2 vs;
+  static __device__ __forceinline__ void places(Source& s, int i16) {
+    s.row = s.words * 4;
+    s.k_at = (8 * (i16 >> 2) + (i16 & 3)) * s.row + s.b * STEPS * 4;
+    const int word = min(i16, s.words - 1);
+    s.v_at = 8 * s.b * s.row + word * 4;
+    s.vs_at = (uint32_t)((word >> 2) * s.capacity) + 8 * s.b;
+#pragma unroll
+    for (int g = 0; g < SCALES; ++g) s.ks_at[g] = (uint32_t)((min(s.b * STEPS + g, s.words - 1) >> 2) * s.capacity) + 8 * (i16 >> 2) + (i16 & 3);
+  }
   __device__ __forceinline__ void load(const Source& s, int tile) {
-    const int64_t row = s.words * 4;
-    const char* k0 = s.k + (int64_t)tile * kTile * row;
-    const char* v0 = s.v + (int64_t)tile * kTile * row;
+    const char* k0 = s.k + (size_t)tile * kTile * s.row;
+    const char* v0 = s.v + (size_t)tile * kTile * s.row;
+    const char* ks0 = s.ks + tile * kTile;
+    const char* vs0 = s.vs + tile * kTile;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const char* p = k0 + (s.key + 16 * h) * (int)row + s.b * STEPS * 4;
+      const uint32_t at = s.k_at + 4 * h * s.row;
       if (EXACT) {
-        __builtin_memcpy(k[h], p, STEPS * 4);
+        __builtin_memcpy(k[h], k0 + at, STEPS * 4);
       } else {
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
           const bool there = s.b * STEPS + st < s.words;
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(p + (there ? 4 * st : -s.b * STEPS * 4));
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(k0 + (there ? at + 4 * st : at - s.b * STEPS * 4));
           k[h][st] = there ? w : 0;
         }
       }
 #pragma unroll
-      for (int g = 0; g < SCALES; ++g) {
-        const int group = min(s.b * STEPS + g, s.words - 1) >> 2;
-        ks[h][g] = (uint8_t)s.ks[group * s.capacity + tile * kTile + s.key + 16 * h];
-      }
+      for (int g = 0; g < SCALES; ++g) ks[h][g] = *reinterpret_cast<const uint8_t*>(ks0 + (s.ks_at[g] + 4 * h));
     }
-    const int word = min(s.i, s.words - 1);
-    const char* p = v0 + s.b * (int)row + word * 4;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const uint32_t*>(p + 4 * j * (int)row);
-    const char* q = s.vs + (word >> 2) * s.capacity + tile * kTile;
-    vs[0] = *reinterpret_cast<const uint4*>(q);
-    vs[1] = *reinterpret_cast<const uint4*>(q + 16);
+    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const uint32_t*>(v0 + (s.v_at + j * s.row));
+    vs = *reinterpret_cast<const uint2*>(vs0 + s.vs_at);
   }
-  // The lane's key of the first (H = 0) or second 16: its words ST as operands.
+  // The lane's key of the first (H = 0) or second product: its words ST as operands.
   template <int H, int ST> __device__ __forceinline__ void key(Words (&w)[1]) const {
     const uint32_t byte = ks[H][SCALES == 1 ? 0 : ST];
     const float f = scale4(byte);
@@ -144,11 +151,7 @@ template <int STEPS, bool EXACT> struct Codes {
     w[0].x[1] = pair4_bf16<1>(k[H][ST], f);
     w[0].x[2] = pair4_bf16<2>(k[H][ST], f);
     w[0].x[3] = pair4_bf16<3>(k[H][ST], f);
-    if (byte == kNoNumber) w[0].x[0] = 0x7FC07FC0u;   // a product with it is NaN, whatever the others are
-  }
-  __device__ __forceinline__ uint32_t value_byte(int j, int b) const {
-    const uint32_t w = j == 0 ? vs[0].x : j == 1 ? vs[0].y : j == 2 ? vs[0].z : j == 3 ? vs[0].w : j == 4 ? vs[1].x : j == 5 ? vs[1].y : j == 6 ? vs[1].z : vs[1].w;
-    return w >> (8 * b) & 255;
+    if ((SCALES == 3 || ST == 0) && byte == kNoNumber) w[0].x[0] = 0x7FC07FC0u;   // a product with it is NaN, whatever the others are
   }
   uint32_t vb[8];   // scales of the lane's keys
   // Values ready for use: keys from `end` on of the tile (their scales may be anything) and groups that are no numbers become 0.
@@ -157,8 +160,8 @@ template <int STEPS, bool EXACT> struct Codes {
     uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      vb[j] = value_byte(j, b);
-      if (end < kTile) vb[j] = 4 * j + b < end ? vb[j] : 0;
+      vb[j] = (j < 4 ? vs.x : vs.y) >> (8 * (j & 3)) & 255;
+      if (end < kTile) vb[j] = 8 * b + j < end ? vb[j] : 0;
       most = max(most, vb[j]);
     }
     if (!__any(most == kNoNumber)) return false;
@@ -173,26 +176,28 @@ template <int STEPS, bool EXACT> struct Codes {
 template <typename T, int STEPS, bool EXACT> struct Plain {
   static constexpr int PIECES = pieces_of<T>();
   Eight<T> k[2][STEPS], v[8];
+  static constexpr uint32_t RUN = 8 * sizeof(T);
+  static __device__ __forceinline__ void places(Source& s, int i16) {
+    s.row = s.words * RUN;
+    s.k_at = 8 * (i16 >> 2) + (i16 & 3);   // the key: the slot may end within the tile
+    s.v_at = min(i16, s.words - 1) * RUN;
+  }
   __device__ __forceinline__ void load(const Source& s, int tile) {
-    const int row = s.words * 8 * (int)sizeof(T);
-    const char* k0 = s.k + (int64_t)tile * kTile * row;
-    const char* v0 = s.v + (int64_t)tile * kTile * row;
-    constexpr int run = 8 * (int)sizeof(T);
+    const char* k0 = s.k + (size_t)tile * kTile * s.row;
+    const char* v0 = s.v + (size_t)tile * kTile * s.row;
+    const int last = (int)min(s.capacity - 1 - (int64_t)tile * kTile, (int64_t)kTile - 1);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t last = s.capacity - 1 - (int64_t)tile * kTile;   // the slot may end within the tile
-      const char* p = k0 + min((int64_t)(s.key + 16 * h), last) * row;
+      const uint32_t at = min((int)s.k_at + 4 * h, last) * s.row;
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
         const int w = s.b * STEPS + st;
-        k[h][st].load(p + (EXACT ? w : min(w, s.words - 1)) * run);
+        k[h][st].load(k0 + (at + (EXACT ? w : min(w, s.words - 1)) * RUN));
         if (!EXACT && w >= s.words) k[h][st].clear();
       }
     }
-    const char* p = v0 + min(s.i, s.words - 1) * run;
-    const int64_t last = s.capacity - 1 - (int64_t)tile * kTile;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j].load(p + min((int64_t)(4 * j + s.b), last) * row);
+    for (int j = 0; j < 8; ++j) v[j].load(v0 + (min(8 * s.b + j, last) * s.row + s.v_at));
   }
   template <int H, int ST> __device__ __forceinline__ void key(Words (&w)[PIECES]) const {
     uint32_t p[PIECES];
@@ -215,7 +220,7 @@ template <typename T, int STEPS, bool EXACT> struct Plain {
     bool any = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if (4 * j + b >= end) v[j].clear();
+      if (8 * b + j >= end) v[j].clear();
       any |= v[j].make_finite();
     }
     return any;
@@ -237,11 +242,12 @@ constexpr size_t recent_lds(int steps) { return sizeof(float) * (4 * 2 * 16 + 4 
 
 // cap, slopes: whether the call has them.
 template <typename T, bool FOUR, int STEPS, bool EXACT, int R>
-__global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, const T* __restrict__ qkv, int H, PlanAny plan, int B, WindowShape shape,
+__global__ __launch_bounds__(256, R == 1 ? (FOUR && sizeof(T) == 2 ? 3 : 2) : 1) void attention_recent_kernel(PlanAny plan_, Cache4Ref c, const T* __restrict__ qkv, int H, int B, WindowShape shape,
                                                                ScoreArgs sc, RecentBuffers out, T* __restrict__ o) {
   typedef typename TileOf<T, FOUR, STEPS, EXACT>::type Held;
-  constexpr int NQ = pieces_of<T>(), NK = Held::PIECES, LDO = 32 * STEPS + 4;
+  constexpr int NQ = pieces_of<T>(), NK = Held::PIECES, DEPTH = FOUR ? 2 : 1, LDO = 32 * STEPS + 4;
   extern __shared__ __attribute__((aligned(16))) float lds_recent[];
+  const PlanFirst plan = PlanFirst::of(plan_);
   const WorkPlace work = shape.place((int)blockIdx.x, B * c.KV);
   const int part = work.part, kh = work.unit % c.KV, q = work.unit / c.KV, G = H / c.KV;
   const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G, group0 = work.group * 16 * R;
@@ -261,9 +267,8 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
   src.vs = FOUR ? c.vs + head_of * c.groups * c.capacity : nullptr;
   src.capacity = c.capacity;
   src.words = words;
-  src.key = 4 * (i16 & 3) + (i16 >> 2);
-  src.i = i16;
   src.b = b;
+  Held::places(src, i16);
 
   const size_t ld = (size_t)(H + 2 * c.KV) * c.dh;
   Words qf[R][STEPS][NQ];
@@ -282,6 +287,7 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
       Eight<T> x;
       x.load(p + (EXACT ? w : min(w, words - 1)) * 8 * (int)sizeof(T));
       if (!EXACT && w >= words) x.clear();
+      if (sc.scale < 0.f) x.negate();   // its size alone is applied later
       uint32_t piece[NQ];
       x.template pair<0>(piece);
 #pragma unroll
@@ -310,14 +316,12 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
 #pragma unroll
     for (int t = 0; t < 8; ++t) acc[r][t] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  const float factor = sc.cap > 0.f ? sc.scale / sc.cap : sc.scale * log2e, cap2 = sc.cap * log2e;
+  // Logits in units of ln 2.  Without cap and slopes products stay as they are and the exponent takes the factor.
+  const bool scaled = sc.cap > 0.f || sc.slopes;
+  const float scale = fabsf(sc.scale), factor = sc.cap > 0.f ? scale / sc.cap : scale * log2e, cap2 = sc.cap * log2e, last_factor = scaled ? 1.f : factor;
   bool met = false;   // whether this wave took out values that are no numbers
 
-  Held next;
-  if (begin + wave < end) next.load(src, tiles.tile(begin + wave));
-  for (int at = begin + wave; at < end; at += 4) {
-    Held x = next;
-    if (at + 4 < end) next.load(src, tiles.tile(at + 4));
+  auto consume = [&](Held& x, int at) {
     const int k0 = tiles.tile(at) * kTile;
     const bool whole = is_whole(k0);
     floatx4 s[R][2];
@@ -355,31 +359,31 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[r][h][e] = cap2 * tanhf(s[r][h][e] * factor);
-      } else {
+      } else if (scaled) {
         s[r][0] *= factor;
         s[r][1] *= factor;
       }
-      const int behind = place[r] - k0 - b;   // the row's distance from the lane's first key
+      const int behind = place[r] - k0 - 8 * b;   // the row's distance from the lane's first key
       if (sc.slopes) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[r][h][e] -= slope2[r] * fabsf((float)(behind - 16 * h - 4 * e));
+          for (int e = 0; e < 4; ++e) s[r][h][e] -= slope2[r] * fabsf((float)(behind - 4 * h - e));
       }
       if (!whole) {
-        const int left = sinks - k0 - b;
+        const int left = sinks - k0 - 8 * b;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int j = 16 * h + 4 * e;
+            const int j = 4 * h + e;
             const bool see = (j <= behind) & ((behind - j < window) | (j < left));
             s[r][h][e] = see ? s[r][h][e] : -INFINITY;
           }
       }
       float mx = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])), fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3])));
-      if (__any(mx > m[r] + 8.f)) {   // a weight may be up to 2^8: no accuracy is lost in a floating format
-        const float top = fmaxf(m[r], xor16_max(xor32_max(mx)));
+      if (__any(mx * last_factor > m[r] + 8.f)) {   // a weight may be up to 2^8: no accuracy is lost in a floating format
+        const float top = fmaxf(m[r], xor16_max(xor32_max(mx)) * last_factor);
         const float alpha = m[r] == top ? 1.f : __builtin_amdgcn_exp2f(m[r] - top);   // equal: also where both are -inf
         m[r] = top;
         l[r] *= alpha;
@@ -391,7 +395,7 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[r][h][e] = __builtin_amdgcn_exp2f(s[r][h][e] - top);
+          s[r][h][e] = __builtin_amdgcn_exp2f(fmaf(s[r][h][e], last_factor, -top));
           l[r] += s[r][h][e];
         }
 #pragma unroll
@@ -440,6 +444,21 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
     column(std::integral_constant<int, 1>{});
     column(std::integral_constant<int, 2>{});
     column(std::integral_constant<int, 3>{});
+  };
+  // Tiles are asked for DEPTH ahead.
+  Held held[DEPTH];
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i)
+    if (begin + wave + 4 * i < end) held[i].load(src, tiles.tile(begin + wave + 4 * i));
+  for (int at = begin + wave; at < end; at += 4 * DEPTH) {
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      const int mine = at + 4 * i;
+      if (mine < end) {
+        consume(held[i], mine);
+        if (mine + 4 * DEPTH < end) held[i].load(src, tiles.tile(mine + 4 * DEPTH));
+      }
+    }
   }
 
   if (__any(met)) {   // what was taken out goes to the rows that see it.  Lane b has elements 32 b .. 32 b + 31 of its rows
@@ -530,54 +549,84 @@ __global__ __launch_bounds__(256) void attention_recent_kernel(Cache4Ref c, cons
   }
 }
 
-// The parts of every row of several, a wave a row: lane d has elements 2 d and 2 d + 1.
-template <typename T>
-__global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan, int B, int H, int G, int dh, WindowShape shape,
+// The parts of every row of several, ROWS rows a wave (a head of a token each): lane d has elements 2 d and 2 d + 1.  Bound by latency, of many
+// rows by the parts' bytes: what the rows of a wave need is asked for together.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan_, int B, int H, int G, int dh, WindowShape shape,
                                                                     RecentBuffers in, T* __restrict__ o) {
+  const PlanFirst plan = PlanFirst::of(plan_);
   const int lane = (int)threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  if (at >= in.TH) return;
-  const int token = (int)(at / H), head = (int)(at % H);
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (plan.at(mid) <= token) lo = mid; else hi = mid;
-  }
-  const int base = plan.at(lo), n = plan.at(lo + 1) - base, row = (token - base) * G + head % G;
-  const int parts = shape.parts_of(shape.tiles(row / shape.rows, n, G, plan.at(2 * B + 1 + lo)));
-  if (parts <= 1) return;   // written already
-  const bool mine = 2 * lane < dh;
-  float2 acc = {0.f, 0.f};
-  float top = -INFINITY, total = 0.f;
-  for (int p0 = 0; p0 < parts; p0 += 8) {   // eight at a time, so that their loads overlap
-    float2 t[8], v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t p = min(p0 + i, parts - 1) * in.TH + at;
-      t[i] = *reinterpret_cast<const float2*>(in.tops + 2 * p);
-      v[i] = *reinterpret_cast<const float2*>(in.sums + p * dh + (mine ? 2 * lane : 0));
+  const int64_t first = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * ROWS;
+  if (first >= in.TH) return;
+  int parts[ROWS], most = 0;
+  int lo = 0;   // the query of the first row, then of the next
+  {
+    const int token = (int)(first / H);
+    int hi = B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (plan.at(mid) <= token) lo = mid; else hi = mid;
     }
-    float most = top;
+  }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = fmaxf(most, t[i].x);
-    const float f = to_top(top, most);
-    acc.x *= f; acc.y *= f; total *= f;
+  for (int r = 0; r < ROWS; ++r) {
+    const int64_t at = min(first + r, in.TH - 1);
+    const int token = (int)(at / H), head = (int)(at % H);
+    while (plan.at(lo + 1) <= token) ++lo;
+    const int base = plan.at(lo), n = plan.at(lo + 1) - base, row = (token - base) * G + head % G;
+    parts[r] = shape.parts_of(shape.tiles(row / shape.rows, n, G, plan.at(2 * B + 1 + lo)));
+    if (first + r >= in.TH || parts[r] <= 1) parts[r] = 0;   // none, or written already
+    most = max(most, parts[r]);
+  }
+  const bool mine = 2 * lane < dh;
+  constexpr int N = 8 / ROWS;
+  float2 acc[ROWS];
+  float top[ROWS], total[ROWS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (p0 + i < parts) {   // wave-uniform; also where the factor is 0: NaN stays
-        const float k = to_top(t[i].x, most);
-        total += k * t[i].y;
-        acc.x += k * v[i].x;
-        acc.y += k * v[i].y;
+  for (int r = 0; r < ROWS; ++r) {
+    acc[r] = float2{0.f, 0.f};
+    top[r] = -INFINITY;
+    total[r] = 0.f;
+  }
+  for (int p0 = 0; p0 < most; p0 += N) {
+    float2 t[ROWS][N], v[ROWS][N];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int64_t p = (int64_t)max(min(p0 + i, parts[r] - 1), 0) * in.TH + min(first + r, in.TH - 1);   // of a row of none: read, and not used
+        t[r][i] = *reinterpret_cast<const float2*>(in.tops + 2 * p);
+        v[r][i] = *reinterpret_cast<const float2*>(in.sums + p * dh + (mine ? 2 * lane : 0));
       }
-    top = most;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (p0 >= parts[r]) continue;   // wave-uniform
+      float m = top[r];
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = fmaxf(m, t[r][i].x);
+      const float f = to_top(top[r], m);
+      acc[r].x *= f; acc[r].y *= f; total[r] *= f;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (p0 + i < parts[r]) {   // wave-uniform; also where the factor is 0: NaN stays
+          const float k = to_top(t[r][i].x, m);
+          total[r] += k * t[r][i].y;
+          acc[r].x += k * v[r][i].x;
+          acc[r].y += k * v[r][i].y;
+        }
+      top[r] = m;
+    }
   }
   if (!mine) return;
-  const float inv = total == 0.f ? 0.f : 1.f / total;
-  struct alignas(2 * sizeof(T)) Pair { T x[2]; } y;
-  y.x[0] = from_float<T>(total == 0.f ? 0.f : acc.x * inv);
-  y.x[1] = from_float<T>(total == 0.f ? 0.f : acc.y * inv);
-  *reinterpret_cast<Pair*>(o + at * dh + 2 * lane) = y;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (parts[r] == 0) continue;
+    const float inv = total[r] == 0.f ? 0.f : 1.f / total[r];
+    struct alignas(2 * sizeof(T)) Pair { T x[2]; } y;
+    y.x[0] = from_float<T>(total[r] == 0.f ? 0.f : acc[r].x * inv);
+    y.x[1] = from_float<T>(total[r] == 0.f ? 0.f : acc[r].y * inv);
+    *reinterpret_cast<Pair*>(o + (first + r) * dh + 2 * lane) = y;
+  }
 }
 
 template <typename T, bool FOUR>
@@ -587,7 +636,7 @@ static hipError_t attention_recent(const Cache4Ref& c, const void* qkv, int H, c
   auto run = [&](auto steps, auto exact, auto r) {
     constexpr int STEPS = decltype(steps)::value;
     auto kern = attention_recent_kernel<T, FOUR, STEPS, decltype(exact)::value, decltype(r)::value>;
-    kern<<<dim3((unsigned)wgs), dim3(256), recent_lds(STEPS), s>>>(c, (const T*)qkv, H, p, B, shape, sc, buf, (T*)o);
+    kern<<<dim3((unsigned)wgs), dim3(256), recent_lds(STEPS), s>>>(p, c, (const T*)qkv, H, B, shape, sc, buf, (T*)o);
     return hipGetLastError();
   };
   auto by_rows = [&](auto steps, auto exact) {
@@ -612,17 +661,22 @@ hipError_t launch_attention_recent(int dtype, bool four, const Cache4Ref& c, con
   const PlanAny p = plan_any(plan, count, d_plan);
   const RecentBuffers buf{workspace + recent_sums_at(shape, TH), workspace, TH};
   hipError_t e;
-  if (shape.rows == 128)
+  if (shape.rows == kManyRows)
     e = launch_attention_rows_bf16(four, c, qkv, H, plan, count, d_plan, B, sc, shape, buf, o, s);
   else if (dtype == 0)
     e = four ? attention_recent<float, true>(c, qkv, H, p, B, sc, shape, buf, o, s) : attention_recent<float, false>(c, qkv, H, p, B, sc, shape, buf, o, s);
   else
     e = four ? attention_recent<bf16_t, true>(c, qkv, H, p, B, sc, shape, buf, o, s) : attention_recent<bf16_t, false>(c, qkv, H, p, B, sc, shape, buf, o, s);
   if (e != hipSuccess || shape.parts <= 1) return e;
-  const dim3 grid((unsigned)((TH + 3) / 4)), block(256);
-  if (dtype == 0) attention_recent_join_kernel<float><<<grid, block, 0, s>>>(p, B, H, H / c.KV, c.dh, shape, buf, (float*)o);
-  else attention_recent_join_kernel<bf16_t><<<grid, block, 0, s>>>(p, B, H, H / c.KV, c.dh, shape, buf, (bf16_t*)o);
-  return hipGetLastError();
+  auto join = [&](auto zero, auto rows) {
+    typedef decltype(zero) E;
+    constexpr int ROWS = decltype(rows)::value;
+    attention_recent_join_kernel<E, ROWS><<<dim3((unsigned)((TH + 4 * ROWS - 1) / (4 * ROWS))), dim3(256), 0, s>>>(p, B, H, H / c.KV, c.dh, shape, buf, (E*)o);
+    return hipGetLastError();
+  };
+  // Four rows a wave where that still leaves a wave for every SIMD.
+  auto by_rows = [&](auto zero) { return TH >= 4096 ? join(zero, std::integral_constant<int, 4>{}) : join(zero, std::integral_constant<int, 1>{}); };
+  return dtype == 0 ? by_rows(0.f) : by_rows(bf16_t{});
 }
 
 }  // namespace otas

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(Cache4Ref c
                                                                      ScoreArgs sc, CapArgs cap, RecentBuffers out, bf16_t* __restrict__ o) {
   typedef TileRows<DH> R;
   constexpr size_t KB = R::bytes(kKeys), BUF = rows_buffer<DH>();   // keys | values | slack
-  constexpr int ROWS = 128;
+  constexpr int ROWS = kManyRows;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const WorkPlace at = shape.place((int)blockIdx.x, B * c.KV);
   const int kh = at.unit % c.KV, q = at.unit / c.KV, G = H / c.KV, group0 = at.group * ROWS;

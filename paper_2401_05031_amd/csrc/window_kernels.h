@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <vector>
 
 #include "decode_kernels.h"
 
@@ -46,6 +47,7 @@ hipError_t launch_cache4_read(int dtype, const Cache4Ref& c, const int32_t* plan
 // How a call through a window is cut up (pure host).  A workgroup has `rows` of a query's n (H / KV) rows of a key head, and `each` of
 // the tiles of 2^shift keys that they see; `parts` = most such shares of a group of rows.
 constexpr int kRecentShift = 5, kRowsShift = 6;   // of attention_recent.hip, of attention_rows_bf16.hip
+constexpr int kManyRows = 128;                    // rows of a workgroup of the latter
 struct WorkPlace { int unit, group, part; };      // unit: the query's and its key head's
 struct WindowShape {
   int window, sinks, shift, rows, groups, each, parts;
@@ -69,11 +71,20 @@ struct WindowShape {
     return WorkPlace{share / parts, group, share % parts};
   }
 };
-// rows of a workgroup of attention_recent.hip, or 128 for attention_rows_bf16.hip
+// rows of a workgroup of attention_recent.hip, or kManyRows
 inline int window_rows(int dtype, int dh, int64_t most) {
   if (most <= 16) return 16;
-  return most > 32 && dtype != 0 && bf16_width(dh) ? 128 : 32;
+  return most > 32 && dtype != 0 && bf16_width(dh) ? kManyRows : 32;
 }
+// Workgroups of these kernels that the chip holds at once: by their registers, of the many rows' by LDS.
+inline int window_slots(int dtype, bool four, int rows) {
+  return 256 * (rows == 16 ? (four && dtype != 0 ? 3 : 2) : rows == kManyRows ? 2 : 1);
+}
+// The share of a workgroup is chosen by what a call should take: rounds of workgroups of so many steps (four tiles at once, one a wave; of many
+// rows one tile), a launch more and its join where there are several parts.  A step is latency, or the bytes of all workgroups at
+// once.  In us, measured: 6 before the first step, 3.5 and a tenth for each part for the join; 1 a step (f32 1.5), 1.3 a tile of many rows (4 bits 2.3) and 1.7 times that
+// where two workgroups share a CU; 6.5 TB/s.  Shares counted from every query's own length: one token of 32 queries over 5700 .. 8192 entries of 8 key heads of 128
+// in 4 bits 46 us, where shares of the longest query's length in 768 / 256 parts had every third query's last part empty.
 inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, const int32_t* off, const int32_t* length, int B, int window, int sinks) {
   const int G = H / KV;
   int64_t most = 0;
@@ -81,18 +92,33 @@ inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, con
   WindowShape t{window, sinks, kRecentShift, 16, 1, 1, 1};
   if (most == 0) return t;
   t.rows = window_rows(dtype, dh, most * G);
-  if (t.rows == 128) t.shift = kRowsShift;
+  const bool many = t.rows == kManyRows;
+  if (many) t.shift = kRowsShift;
   t.groups = (int)((most * G + t.rows - 1) / t.rows);
-  int64_t wgs = 0;
-  int longest = 1;
+  std::vector<int32_t> counts;   // tiles of every group of rows of a key head
   for (int q = 0; q < B; ++q) {
     const int n = off[q + 1] - off[q], mine = (int)(((int64_t)n * G + t.rows - 1) / t.rows);
-    wgs += (int64_t)mine * KV;
-    for (int g = 0; g < mine; ++g) longest = std::max(longest, t.tiles(g, n, G, length[q]).count);
+    for (int g = 0; g < mine; ++g) counts.push_back(t.tiles(g, n, G, length[q]).count);
   }
-  const int64_t target = t.rows == 128 ? 512 : 768, least = t.rows == 128 ? 4 : 8;
-  const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(target / wgs, (longest + least - 1) / least));
-  t.each = (int)((longest + wanted - 1) / wanted);
+  const int longest = *std::max_element(counts.begin(), counts.end()), slots = window_slots(dtype, four, t.rows), at_once = many ? 1 : 4;
+  const double bytes = at_once * (2 << t.shift) * (four ? dh / 2 + (dh + 31) / 32 : dh * (dtype == 0 ? 4.0 : 2.0));
+  const double latency = many ? (four ? 2.3 : 1.3) : dtype == 0 ? 1.5 : 1.0;
+  double best = 1e30;
+  t.each = longest;
+  for (int64_t steps = (longest + at_once - 1) / at_once; steps > 0; steps = counts.size() > 64 ? steps * 2 / 3 : steps * 7 / 8) {
+    const int each = (int)steps * at_once;
+    int64_t wgs = 0;
+    for (const int32_t c : counts) wgs += (c + each - 1) / each;
+    wgs *= KV;
+    const int64_t active = std::min<int64_t>(wgs, slots), rounds = (wgs + slots - 1) / slots;
+    const double step = std::max(many && active > slots / 2 ? 1.7 * latency : latency, active * bytes / 6.5e6);
+    const double us = rounds * (6 + steps * step) + (each < longest ? 3.5 + 0.1 * ((longest + each - 1) / each) : 0);
+    if (us < best) {
+      best = us;
+      t.each = each;
+    }
+    if (rounds > 4) break;   // more workgroups take longer from here on
+  }
   t.parts = (longest + t.each - 1) / t.each;
   return t;
 }
