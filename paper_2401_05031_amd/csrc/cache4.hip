@@ -5,12 +5,17 @@
 
 namespace otas {
 
-// Code of one element, scaled to at most 7: the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6, of two as near the one of even code.
-__device__ __forceinline__ uint32_t code4(float x) {
-  const float y = fabsf(x);
-  const uint32_t c = (uint32_t)(y > 0.25f) + (y >= 0.75f) + (y > 1.25f) + (y >= 1.75f) + (y > 2.5f) + (y >= 3.5f) + (y > 5.f);
-  return c | (__float_as_uint(x) >> 31) << 3;
+// Eight elements as codes: v_cvt_scalef32_pk_fp4_f32 divides by the scale, rounds to the nearest (of two as near to the one of even code)
+// and holds what is larger at 6.
+template <typename T> __device__ __forceinline__ uint32_t codes4(const Oct<T>& x, float scale) {
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, to_float(x.x[0]), to_float(x.x[1]), scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, to_float(x.x[2]), to_float(x.x[3]), scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, to_float(x.x[4]), to_float(x.x[5]), scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, to_float(x.x[6]), to_float(x.x[7]), scale, 3);
 }
+
+// Row of a workgroup: runs of rows to each XCD, whose L2 then puts together the scales of entries side by side.
+__device__ __forceinline__ int row_of(int id, int each) { return (id & 7) * each + (id >> 3); }
 
 template <typename P> __device__ __forceinline__ int query_of(const P& plan, int B, int i) {   // the last one that begins at or before row i
   int lo = 0, hi = B;
@@ -24,8 +29,10 @@ template <typename P> __device__ __forceinline__ int query_of(const P& plan, int
 // A workgroup has one row.  A thread has eight elements of a head, four threads a group, whose largest element goes round them in
 // registers.
 template <typename T, typename P>
-__global__ __launch_bounds__(256) void cache4_append_kernel(Cache4Ref c, const T* __restrict__ qkv, int H, P plan, int B, bool has_rows) {
-  const int i = (int)blockIdx.x, q = query_of(plan, B, i);
+__global__ __launch_bounds__(256) void cache4_append_kernel(Cache4Ref c, const T* __restrict__ qkv, int H, P plan, int B, int N, bool has_rows) {
+  const int i = row_of((int)blockIdx.x, (N + 7) >> 3);
+  if (i >= N) return;
+  const int q = query_of(plan, B, i);
   const int64_t slot = plan[B + 1 + q], entry = plan[2 * B + 1 + q] + (i - plan[q]);
   const int64_t row = has_rows ? plan[3 * B + 1 + i] : i;
   const int words = c.dh / 8, per_head = 4 * c.groups, total = 2 * c.KV * per_head;
@@ -43,12 +50,7 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(Cache4Ref c, const T
     largest = max(largest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)largest, kDppXor1, 0xF, 0xF, true));
     largest = max(largest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)largest, kDppXor2, 0xF, 0xF, true));
     if (!there) continue;
-    const uint32_t byte = scale4_byte(largest);
-    const float f = scale4(254 - min(byte, 252u));
-    uint32_t word = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) word |= code4(to_float(x.x[j]) * f) << (4 * j);
-    if (byte == kNoNumber) word = 0;
+    const uint32_t byte = scale4_byte(largest), word = byte == kNoNumber ? 0 : codes4(x, scale4(byte));
     const int64_t head = slot * c.KV + kh;
     *reinterpret_cast<uint32_t*>((h < c.KV ? c.k : c.v) + (head * c.capacity + entry) * (c.dh / 2) + w * 4) = word;
     if (w % 4 == 0) (h < c.KV ? c.ks : c.vs)[(head * c.groups + w / 4) * c.capacity + entry] = (char)byte;
@@ -60,17 +62,19 @@ hipError_t launch_cache4_append(int dtype, const Cache4Ref& c, const void* qkv, 
   if (N <= 0) return hipSuccess;
   return with_plan(plan, count, d_plan, [&](auto p) {
     typedef decltype(p) P;
-    const dim3 grid((unsigned)N), block(256);
-    if (dtype == 0) cache4_append_kernel<float, P><<<grid, block, 0, s>>>(c, (const float*)qkv, H, p, B, has_rows);
-    else cache4_append_kernel<bf16_t, P><<<grid, block, 0, s>>>(c, (const bf16_t*)qkv, H, p, B, has_rows);
+    const dim3 grid((unsigned)((N + 7) / 8 * 8)), block(256);
+    if (dtype == 0) cache4_append_kernel<float, P><<<grid, block, 0, s>>>(c, (const float*)qkv, H, p, B, (int)N, has_rows);
+    else cache4_append_kernel<bf16_t, P><<<grid, block, 0, s>>>(c, (const bf16_t*)qkv, H, p, B, (int)N, has_rows);
     return hipGetLastError();
   });
 }
 
 // A workgroup has one row, a thread eight elements of a head.
 template <typename T, typename P>
-__global__ __launch_bounds__(256) void cache4_read_kernel(Cache4Ref c, P plan, int B, T* __restrict__ kv) {
-  const int i = (int)blockIdx.x, q = query_of(plan, B, i);
+__global__ __launch_bounds__(256) void cache4_read_kernel(Cache4Ref c, P plan, int B, int N, T* __restrict__ kv) {
+  const int i = row_of((int)blockIdx.x, (N + 7) >> 3);
+  if (i >= N) return;
+  const int q = query_of(plan, B, i);
   const int64_t slot = plan[B + 1 + q], entry = plan[2 * B + 1 + q] + (i - plan[q]);
   const int words = c.dh / 8, total = 2 * c.KV * words;
   for (int u = (int)threadIdx.x; u < total; u += 256) {
@@ -93,9 +97,9 @@ hipError_t launch_cache4_read(int dtype, const Cache4Ref& c, const int32_t* plan
   if (N <= 0) return hipSuccess;
   return with_plan(plan, count, d_plan, [&](auto p) {
     typedef decltype(p) P;
-    const dim3 grid((unsigned)N), block(256);
-    if (dtype == 0) cache4_read_kernel<float, P><<<grid, block, 0, s>>>(c, p, B, (float*)kv);
-    else cache4_read_kernel<bf16_t, P><<<grid, block, 0, s>>>(c, p, B, (bf16_t*)kv);
+    const dim3 grid((unsigned)((N + 7) / 8 * 8)), block(256);
+    if (dtype == 0) cache4_read_kernel<float, P><<<grid, block, 0, s>>>(c, p, B, (int)N, (float*)kv);
+    else cache4_read_kernel<bf16_t, P><<<grid, block, 0, s>>>(c, p, B, (int)N, (bf16_t*)kv);
     return hipGetLastError();
   });
 }

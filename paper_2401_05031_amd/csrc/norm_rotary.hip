@@ -26,7 +26,7 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v) {   // over
 template <typename T, int V, int L>
 __global__ __launch_bounds__(256) void norm_rotary_kernel(const T* qkv, T* out, const int32_t* __restrict__ positions, int64_t rows, int H, int KV,
                                                           int dh, int tokens, HeadNormArgs n, RotaryArgs r) {
-  __shared__ float2 cs[8 * 64];
+  __shared__ __attribute__((aligned(16))) float2 cs[4 * 64];
   __shared__ __attribute__((aligned(16))) float turned[256 * V];
   const int pairs = r.rot >> 1, all_heads = H + 2 * KV;
   const int64_t t0 = (int64_t)blockIdx.x * tokens;
@@ -38,19 +38,29 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(const T* qkv, T* out, 
   typedef Chunk<T, V> C;
   float* mine = turned + own * (L * V);
   const float inv = 1.f / (float)dh;
+  const bool whole_halves = pairs % V == 0;   // a chunk's partners are one run
+  C gains[2];                                 // shared by all heads
+  const bool shared = !n.per_head;
+  if (shared && there) {
+    if (n.q_gain) gains[0] = *reinterpret_cast<const C*>((const T*)n.q_gain + e);
+    if (n.k_gain) gains[1] = *reinterpret_cast<const C*>((const T*)n.k_gain + e);
+  }
+  // Where head i of the workgroup's lies: its row and its place there move on by so many a round.
+  const int step_t = 256 / L / heads, step_h = 256 / L % heads;
+  int t = own / heads, h = own - t * heads;
+  auto where = [&](int t, int h) { return ((t0 + t) * all_heads + h) * dh + e; };
+  C next;
+  if (there && t < nt) next = *reinterpret_cast<const C*>(qkv + where(t, h));
   for (int i0 = 0; i0 < nt * heads; i0 += 256 / L) {
-    const int i = i0 + own, t = i / heads, h = i - t * heads;
-    const bool active = there && i < nt * heads;
-    const int64_t at = ((t0 + t) * all_heads + h) * dh + e;
-    C x;
+    const bool active = there && t < nt;
+    const int64_t at = where(t, h);
+    C x = next;
+    int t_next = t + step_t, h_next = h + step_h;
+    if (h_next >= heads) { h_next -= heads; ++t_next; }
+    if (there && t_next < nt) next = *reinterpret_cast<const C*>(qkv + where(t_next, h_next));
     float y[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) y[j] = 0.f;
-    if (active) {
-      x = *reinterpret_cast<const C*>(qkv + at);
-#pragma unroll
-      for (int j = 0; j < V; ++j) y[j] = to_float(x.x[j]);
-    }
+    for (int j = 0; j < V; ++j) y[j] = active ? to_float(x.x[j]) : 0.f;
     if (n.center) {
       float s = 0.f;
 #pragma unroll
@@ -66,8 +76,8 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(const T* qkv, T* out, 
     const bool query = h < H, norm = active && h < H + KV;
     if (norm) {
       const T* g = (const T*)(query ? n.q_gain : n.k_gain);
-      C gain;
-      if (g) gain = *reinterpret_cast<const C*>(g + (n.per_head ? (int64_t)(query ? h : h - H) * dh : 0) + e);
+      C gain = query ? gains[0] : gains[1];
+      if (g && !shared) gain = *reinterpret_cast<const C*>(g + (int64_t)(query ? h : h - H) * dh + e);
 #pragma unroll
       for (int j = 0; j < V; ++j) y[j] = y[j] * scale * (g ? to_float(gain.x[j]) : 1.f);
     }
@@ -78,6 +88,21 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(const T* qkv, T* out, 
       if (norm && e < r.rot) {
         const float2* a = cs + t * 64;
         float z[V];
+        if (whole_halves) {
+          const bool low = e < pairs;
+          const float* other = mine + (low ? e + pairs : e - pairs);
+          const float4* w = reinterpret_cast<const float4*>(a + (low ? e : e - pairs));   // cosine and sine of two pairs
+          const float sign = low ? -1.f : 1.f;
+#pragma unroll
+          for (int j = 0; j < V; j += 4) {
+            const floatx4 p = *reinterpret_cast<const floatx4*>(other + j);
+            const float4 w0 = w[j / 2], w1 = w[j / 2 + 1];
+            z[j] = y[j] * w0.x + p[0] * (sign * w0.y);
+            z[j + 1] = y[j + 1] * w0.z + p[1] * (sign * w0.w);
+            z[j + 2] = y[j + 2] * w1.x + p[2] * (sign * w1.y);
+            z[j + 3] = y[j + 3] * w1.z + p[3] * (sign * w1.w);
+          }
+        } else
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const int p = e + j;
@@ -105,13 +130,16 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(const T* qkv, T* out, 
       for (int j = 0; j < V; ++j) x.x[j] = from_float<T>(y[j]);
     }
     if (active) *reinterpret_cast<C*>(out + at) = x;
+    t = t_next;
+    h = h_next;
   }
 }
 
 hipError_t launch_norm_rotary(int dtype, const void* qkv, void* out, const int32_t* positions, int64_t T, int H, int KV, int dh,
                               const HeadNormArgs& n, const RotaryArgs& r, hipStream_t s) {
   if (T <= 0) return hipSuccess;
-  const int tokens = T >= 8192 ? 8 : T >= 2048 ? 4 : T >= 1024 ? 2 : 1;
+  // Rows per workgroup: angles of several keep all threads busy (16384 rows: 2 55 us, 4 52, 8 55), but a small call wants its rows on many CUs.
+  const int tokens = T >= 2048 ? 4 : T >= 1024 ? 2 : 1;
   const int64_t wgs = (T + tokens - 1) / tokens;
   if (wgs > kMostGroups) return kTooManyGroups;
   auto run = [&](auto zero, auto v, auto lanes) {
