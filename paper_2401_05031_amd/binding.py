@@ -292,9 +292,10 @@ class KVCache4:
         small = (self.slots, self.kv_heads, -(-self.head_width // OTAS_CACHE4_GROUP), self.capacity)
         if k_scales.shape != small or v_scales.shape != small:
             raise ValueError(f"k_scales and v_scales must be {small}")
-        self.device_index = k.get_device()
+        self.device_index = device = k.get_device()
+        byte = torch.uint8
         for t in (k, v, k_scales, v_scales):
-            if t.dtype != torch.uint8 or t.get_device() != self.device_index or self.device_index < 0 or not t.is_contiguous():
+            if t.dtype is not byte or t.get_device() != device or device < 0 or not t.is_contiguous():
                 raise ValueError("k, v, k_scales and v_scales must be contiguous uint8 tensors on one GPU")
         self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
         self.desc = _KVCache4(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), self.slots, self.kv_heads, self.capacity)

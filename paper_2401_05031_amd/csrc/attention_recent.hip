@@ -549,14 +549,16 @@ __global__ __launch_bounds__(256, R == 1 ? (FOUR && sizeof(T) == 2 ? 3 : 2) : 1)
   }
 }
 
-// The parts of every row of several, ROWS rows a wave (a head of a token each): lane d has elements 2 d and 2 d + 1.  Bound by latency, of many
-// rows by the parts' bytes: what the rows of a wave need is asked for together.
-template <typename T, int ROWS>
+// The parts of every row (a head of a token) of several: ROWS rows a wave, or where there are few, one a workgroup, whose waves share its parts
+// (SHARED).  Lane d has elements 2 d and 2 d + 1.  Bound by latency, of many rows by the parts' bytes: what a wave needs is asked for together.
+template <typename T, int ROWS, bool SHARED>
 __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan_, int B, int H, int G, int dh, WindowShape shape,
                                                                     RecentBuffers in, T* __restrict__ o) {
+  static_assert(!SHARED || ROWS == 1, "a row a workgroup");
+  __shared__ float shares[4][2 + 128];
   const PlanFirst plan = PlanFirst::of(plan_);
-  const int lane = (int)threadIdx.x & 63;
-  const int64_t first = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * ROWS;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int64_t first = SHARED ? blockIdx.x : ((int64_t)blockIdx.x * 4 + wave) * ROWS;
   if (first >= in.TH) return;
   int parts[ROWS], most = 0;
   int lo = 0;   // the query of the first row, then of the next
@@ -578,8 +580,9 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
     if (first + r >= in.TH || parts[r] <= 1) parts[r] = 0;   // none, or written already
     most = max(most, parts[r]);
   }
+  if (SHARED && most == 0) return;   // workgroup-uniform
   const bool mine = 2 * lane < dh;
-  constexpr int N = 8 / ROWS;
+  constexpr int N = 8 / ROWS, STEP = SHARED ? 4 : 1;
   float2 acc[ROWS];
   float top[ROWS], total[ROWS];
 #pragma unroll
@@ -588,13 +591,13 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
     top[r] = -INFINITY;
     total[r] = 0.f;
   }
-  for (int p0 = 0; p0 < most; p0 += N) {
+  for (int p0 = SHARED ? wave : 0; p0 < most; p0 += N * STEP) {
     float2 t[ROWS][N], v[ROWS][N];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int64_t p = (int64_t)max(min(p0 + i, parts[r] - 1), 0) * in.TH + min(first + r, in.TH - 1);   // of a row of none: read, and not used
+        const int64_t p = (int64_t)max(min(p0 + i * STEP, parts[r] - 1), 0) * in.TH + min(first + r, in.TH - 1);   // of a row of none: read, and not used
         t[r][i] = *reinterpret_cast<const float2*>(in.tops + 2 * p);
         v[r][i] = *reinterpret_cast<const float2*>(in.sums + p * dh + (mine ? 2 * lane : 0));
       }
@@ -608,13 +611,34 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
       acc[r].x *= f; acc[r].y *= f; total[r] *= f;
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        if (p0 + i < parts[r]) {   // wave-uniform; also where the factor is 0: NaN stays
+        if (p0 + i * STEP < parts[r]) {   // wave-uniform; also where the factor is 0: NaN stays
           const float k = to_top(t[r][i].x, m);
           total[r] += k * t[r][i].y;
           acc[r].x += k * v[r][i].x;
           acc[r].y += k * v[r][i].y;
         }
       top[r] = m;
+    }
+  }
+  if constexpr (SHARED) {   // in the order of the waves
+    if (lane == 0) {
+      shares[wave][0] = top[0];
+      shares[wave][1] = total[0];
+    }
+    *reinterpret_cast<float2*>(&shares[wave][2 + 2 * lane]) = acc[0];
+    __syncthreads();
+    if (wave > 0) return;
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, shares[w][0]);
+    acc[0] = float2{0.f, 0.f};
+    total[0] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float k = to_top(shares[w][0], m);
+      total[0] += k * shares[w][1];
+      acc[0].x += k * shares[w][2 + 2 * lane];
+      acc[0].y += k * shares[w][3 + 2 * lane];
     }
   }
   if (!mine) return;
@@ -668,14 +692,18 @@ hipError_t launch_attention_recent(int dtype, bool four, const Cache4Ref& c, con
   else
     e = four ? attention_recent<bf16_t, true>(c, qkv, H, p, B, sc, shape, buf, o, s) : attention_recent<bf16_t, false>(c, qkv, H, p, B, sc, shape, buf, o, s);
   if (e != hipSuccess || shape.parts <= 1) return e;
-  auto join = [&](auto zero, auto rows) {
+  auto join = [&](auto zero, auto rows, auto shared) {
     typedef decltype(zero) E;
     constexpr int ROWS = decltype(rows)::value;
-    attention_recent_join_kernel<E, ROWS><<<dim3((unsigned)((TH + 4 * ROWS - 1) / (4 * ROWS))), dim3(256), 0, s>>>(p, B, H, H / c.KV, c.dh, shape, buf, (E*)o);
+    const int64_t groups = decltype(shared)::value ? TH : (TH + 4 * ROWS - 1) / (4 * ROWS);
+    attention_recent_join_kernel<E, ROWS, decltype(shared)::value><<<dim3((unsigned)groups), dim3(256), 0, s>>>(p, B, H, H / c.KV, c.dh, shape, buf, (E*)o);
     return hipGetLastError();
   };
-  // Four rows a wave where that still leaves a wave for every SIMD.
-  auto by_rows = [&](auto zero) { return TH >= 4096 ? join(zero, std::integral_constant<int, 4>{}) : join(zero, std::integral_constant<int, 1>{}); };
+  // Four rows a wave where that still leaves a wave for every SIMD; a row's parts shared where one wave would take them in several turns.
+  auto by_rows = [&](auto zero) {
+    if (TH >= 4096) return join(zero, std::integral_constant<int, 4>{}, std::false_type{});
+    return shape.parts > 8 ? join(zero, std::integral_constant<int, 1>{}, std::true_type{}) : join(zero, std::integral_constant<int, 1>{}, std::false_type{});
+  };
   return dtype == 0 ? by_rows(0.f) : by_rows(bf16_t{});
 }
 

@@ -77,12 +77,13 @@ template <int DH> constexpr size_t rows_buffer() { return 2 * TileRows<DH>::byte
 template <int DH> constexpr size_t rows_lds() { return 2 * rows_buffer<DH>() + 16; }
 
 template <int DH, bool FOUR, int CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(Cache4Ref c, const bf16_t* __restrict__ qkv, int H, PlanAny plan, int B, WindowShape shape,
+__global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny plan_, Cache4Ref c, const bf16_t* __restrict__ qkv, int H, int B, WindowShape shape,
                                                                      ScoreArgs sc, CapArgs cap, RecentBuffers out, bf16_t* __restrict__ o) {
   typedef TileRows<DH> R;
   constexpr size_t KB = R::bytes(kKeys), BUF = rows_buffer<DH>();   // keys | values | slack
   constexpr int ROWS = kManyRows;
   extern __shared__ __attribute__((aligned(16))) char lds[];
+  const PlanFirst plan = PlanFirst::of(plan_);
   const WorkPlace at = shape.place((int)blockIdx.x, B * c.KV);
   const int kh = at.unit % c.KV, q = at.unit / c.KV, G = H / c.KV, group0 = at.group * ROWS;
   const bool packed = !FOUR && c.k == nullptr;
@@ -266,7 +267,7 @@ hipError_t launch_attention_rows_bf16(bool four, const Cache4Ref& c, const void*
     auto kern = attention_rows_bf16_kernel<DH, decltype(four_)::value, decltype(cap)::value, decltype(bias)::value>;
     const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)rows_lds<DH>());
     if (e != hipSuccess) return e;
-    kern<<<dim3((unsigned)wgs), dim3(256), rows_lds<DH>(), s>>>(c, (const bf16_t*)qkv, H, p, B, shape, sc, CapArgs::of(sc), buf, (bf16_t*)o);
+    kern<<<dim3((unsigned)wgs), dim3(256), rows_lds<DH>(), s>>>(p, c, (const bf16_t*)qkv, H, B, shape, sc, CapArgs::of(sc), buf, (bf16_t*)o);
     return hipGetLastError();
   };
   auto pick = [&](auto width, auto four_) {

@@ -28,9 +28,10 @@ template <typename T> struct WindowKeys {
 };
 
 template <typename T, int DT, bool WHOLE>
-__global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_window_f32_kernel(const T* __restrict__ qkv, PlanAny plan, int B, int H, int KV, int width, int xblks,
+__global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_window_f32_kernel(PlanAny plan_, const T* __restrict__ qkv, int B, int H, int KV, int width, int xblks,
                                                                    ScoreArgs sc, int window, int sinks, T* __restrict__ o) {
   extern __shared__ __attribute__((aligned(16))) float f32_lds[];
+  const PlanFirst plan = PlanFirst::of(plan_);
   // The row blocks of a head on one XCD where heads divide so.
   const int id = (int)blockIdx.x, pairs = B * H;
   int pair, xblk;
@@ -75,7 +76,7 @@ static hipError_t attention_window_f32(const void* qkv, const int32_t* plan, siz
     auto kern = attention_window_f32_kernel<T, DT, decltype(whole)::value>;
     const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
     if (e != hipSuccess) return e;
-    kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>((const T*)qkv, p, B, H, KV, dh, xblks, sc, window, sinks, (T*)o);
+    kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>(p, (const T*)qkv, B, H, KV, dh, xblks, sc, window, sinks, (T*)o);
     return hipGetLastError();
   });
 }

@@ -200,7 +200,7 @@ otas_status otas_cache4_append(otas_ctx* c, const otas_kv_cache4* cache, const v
     } else if (N > T) {
       return OTAS_EINVAL;
     }
-    if (N > kMostGroups - 7) return OTAS_EUNSUPPORTED;   // a workgroup a row
+    if (N > kMostGroups) return OTAS_EUNSUPPORTED;   // as otas_cache_append
     const size_t count = 3 * (size_t)B + 1 + (rows ? (size_t)N : 0);
     if (count > kPlanInts) return OTAS_ENOMEM;
     std::vector<int32_t> plan(count);   // row offsets [B+1] | slot [B] | length [B] | rows [N]
@@ -234,7 +234,7 @@ otas_status otas_cache4_read(otas_ctx* c, const otas_kv_cache4* cache, const int
     if (st != OTAS_OK) return st;
     for (int q = 0; q < B; ++q)
       if (row_offsets[q + 1] - row_offsets[q] > cache->capacity - first[q]) return OTAS_EINVAL;
-    if (N > kMostGroups - 7) return OTAS_EUNSUPPORTED;   // a workgroup a row
+    if (N > kMostGroups) return OTAS_EUNSUPPORTED;   // as otas_cache_append
     if (N == 0) return OTAS_OK;
     std::vector<int32_t> plan(3 * (size_t)B + 1);   // row offsets [B+1] | slot [B] | first [B]
     std::copy(row_offsets, row_offsets + B + 1, plan.begin());
