@@ -173,9 +173,10 @@ otas_status otas_attention_window(otas_ctx *ctx, const void *qkv, int32_t kv_hea
  *   are a run of drafts or a prompt taken in pieces.
  *   offsets, slot, length host: 0 <= rows of a query <= length[q] (EINVAL); slots may repeat
  *   score NULL = all defaults; the distance for slopes is t - j.  Neither the cache's positions nor its mass are touched.
- *   workspace dev >= otas_attention_recent_workspace_bytes for the same kv_heads, offsets, length, window and sinks, 256-byte aligned
+ *   workspace dev >= otas_attention_recent_workspace_bytes for the same kv_heads, offsets, length, window and sinks, 256-byte aligned;
+ *   the bytes grow with the lengths
  *   o dev [T, D]; o and the workspace overlap no other array.   Host numbers: 3 B + 1.
- * d_h a multiple of 8 up to 128 (EUNSUPPORTED).  Keys and values that a row does not see do not reach it.  A row that sees a key or value
+ * d_h a multiple of 8 up to 128, length[q] (H / kv_heads) < 2^30 (EUNSUPPORTED).  Keys and values that a row does not see do not reach it.  A row that sees a key or value
  * that is not finite is not finite where it counts, or all NaN.  f32 models form products from operands cut into three
  * bf16 pieces each, without loss but for the product of the two last (2^-30 of the product): sums are float.  bf16 models round
  * weights as otas_attention_masked does.  The split of a long window between workgroups, and with it the last bits of o, depends on the whole

@@ -85,7 +85,7 @@ hipError_t launch_attention_window(int dtype, const void* qkv, const int32_t* pl
                                    int KV, int dh, const ScoreArgs& sc, int window, int sinks, void* o, hipStream_t s) {
   if (max_n <= 0) return hipSuccess;
   if (dtype != 0 && bf16_width(dh)) {
-    WindowShape shape{window, sinks, kRowsShift, kManyRows, (int)(((int64_t)max_n * (H / KV) + kManyRows - 1) / kManyRows), 0, 1};
+    WindowShape shape{window, sinks, kRowsShift, kManyRows, (int)(((int64_t)max_n * (H / KV) + kManyRows - 1) / kManyRows), 0, 1, 1};
     shape.each = window_tiles(kRowsShift, 0, max_n - 1, window, sinks).count;   // all that a group can see
     return launch_attention_rows_bf16(false, Cache4Ref{nullptr, nullptr, nullptr, nullptr, 0, KV, dh, 0}, qkv, H, plan, count, d_plan, B, sc, shape,
                                       RecentBuffers{nullptr, nullptr, 0}, o, s);

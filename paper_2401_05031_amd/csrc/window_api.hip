@@ -60,6 +60,8 @@ otas_status recent_ok(const int32_t* offsets, const int32_t* length, int B) {
     if (offsets[q + 1] - offsets[q] > length[q]) return OTAS_EINVAL;
   return OTAS_OK;
 }
+// Rows of a query x heads that share a key head are counted in 32 bits.
+bool rows_fit(const otas_ctx* c, int kv, int64_t n) { return n * (c->desc.H / kv) <= INT32_MAX / 2; }
 
 // Either attention of the last tokens; apart(array, bytes): whether it is clear of the cache.
 template <typename Apart>
@@ -74,6 +76,8 @@ otas_status attention_last(otas_ctx* c, const Cache4Ref& cache, bool four, int s
   if (st == OTAS_OK) st = recent_ok(offsets, length, B);
   if (st != OTAS_OK) return st;
   if (cache.dh % 8 != 0) return OTAS_EUNSUPPORTED;
+  for (int q = 0; q < B; ++q)
+    if (!rows_fit(c, cache.KV, length[q])) return OTAS_EUNSUPPORTED;
   const int64_t T = offsets[B];
   const WindowShape shape = recent_shape(c->desc.dtype, four, cache.dh, c->desc.H, cache.KV, offsets, length, B, window, sinks);
   const size_t need = recent_workspace_floats(shape, T * c->desc.H, cache.dh) * sizeof(float);
@@ -138,7 +142,7 @@ otas_status otas_attention_window(otas_ctx* c, const void* qkv, int32_t kv_heads
     if (overlap(qkv, qkv_bytes(c, T, kv_heads), o, rows_bytes(c, T))) return OTAS_EINVAL;
     int max_n = 0;
     for (int q = 0; q < B; ++q) max_n = std::max(max_n, offsets[q + 1] - offsets[q]);
-    if (max_n > OTAS_MAX_LONG_SEQ) return OTAS_EUNSUPPORTED;
+    if (max_n > OTAS_MAX_LONG_SEQ || !rows_fit(c, kv_heads, max_n)) return OTAS_EUNSUPPORTED;
     if (T == 0) return OTAS_OK;
     const std::vector<int32_t> plan(offsets, offsets + B + 1);
     OnDevice on(c);
@@ -156,12 +160,12 @@ size_t otas_attention_recent_workspace_bytes(const otas_ctx* c, int32_t kv_heads
   return guarded_size([&]() -> size_t {
     if (!c || !offsets || !length || B <= 0 || !kv_heads_ok(c, kv_heads) || !offsets_ok(offsets, B) || !window_ok(window, sinks)) return 0;
     for (int q = 0; q < B; ++q)
-      if (length[q] < 0 || length[q] > OTAS_MAX_LONG_SEQ) return 0;
+      if (length[q] < 0 || length[q] > OTAS_MAX_LONG_SEQ || !rows_fit(c, kv_heads, length[q])) return 0;
     if (recent_ok(offsets, length, B) != OTAS_OK) return 0;
     size_t floats = 1;
     for (bool four : {false, true}) {
       const WindowShape shape = recent_shape(c->desc.dtype, four, c->desc.D / c->desc.H, c->desc.H, kv_heads, offsets, length, B, window, sinks);
-      floats = std::max(floats, recent_workspace_floats(shape, (int64_t)offsets[B] * c->desc.H, c->desc.D / c->desc.H));
+      floats = std::max(floats, recent_room_floats(shape, (int64_t)offsets[B] * c->desc.H, c->desc.D / c->desc.H));
     }
     return align_up(floats * sizeof(float), kAlign);
   });

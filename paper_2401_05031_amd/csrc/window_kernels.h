@@ -51,6 +51,7 @@ constexpr int kManyRows = 128;                    // rows of a workgroup of the 
 struct WorkPlace { int unit, group, part; };      // unit: the query's and its key head's
 struct WindowShape {
   int window, sinks, shift, rows, groups, each, parts;
+  int room;   // parts that the workspace has place for; >= parts, and grows with the lengths
   __host__ __device__ WindowTiles tiles(int group, int n, int G, int length) const {
     const int last = (group + 1) * rows < n * G ? (group + 1) * rows - 1 : n * G - 1, at = length - n;
     return window_tiles(shift, at + group * rows / G, at + last / G, window, sinks);
@@ -89,16 +90,20 @@ inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, con
   const int G = H / KV;
   int64_t most = 0;
   for (int q = 0; q < B; ++q) most = std::max<int64_t>(most, off[q + 1] - off[q]);
-  WindowShape t{window, sinks, kRecentShift, 16, 1, 1, 1};
+  WindowShape t{window, sinks, kRecentShift, 16, 1, 1, 1, 1};
   if (most == 0) return t;
   t.rows = window_rows(dtype, dh, most * G);
   const bool many = t.rows == kManyRows;
   if (many) t.shift = kRowsShift;
   t.groups = (int)((most * G + t.rows - 1) / t.rows);
   std::vector<int32_t> counts;   // tiles of every group of rows of a key head
+  int64_t reach = 1;             // as many and more, whatever multiple a window begins at: grows with the lengths
+  auto whole = [&](int64_t keys) { return (keys + (1 << t.shift) - 1) >> t.shift; };
   for (int q = 0; q < B; ++q) {
     const int n = off[q + 1] - off[q], mine = (int)(((int64_t)n * G + t.rows - 1) / t.rows);
     for (int g = 0; g < mine; ++g) counts.push_back(t.tiles(g, n, G, length[q]).count);
+    if (n > 0)
+      reach = std::max(reach, std::min(whole(length[q]), whole(std::min(sinks, length[q])) + whole((int64_t)std::min(window, length[q]) + t.rows / G + 1) + 1));
   }
   const int longest = *std::max_element(counts.begin(), counts.end()), slots = window_slots(dtype, four, t.rows), at_once = many ? 1 : 4;
   const double bytes = at_once * (2 << t.shift) * (four ? dh / 2 + (dh + 31) / 32 : dh * (dtype == 0 ? 4.0 : 2.0));
@@ -111,15 +116,18 @@ inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, con
     for (const int32_t c : counts) wgs += (c + each - 1) / each;
     wgs *= KV;
     const int64_t active = std::min<int64_t>(wgs, slots), rounds = (wgs + slots - 1) / slots;
+    if (each < longest && rounds > 2) break;   // more workgroups take longer from here on
     const double step = std::max(many && active > slots / 2 ? 1.7 * latency : latency, active * bytes / 6.5e6);
     const double us = rounds * (6 + steps * step) + (each < longest ? 3.5 + 0.1 * ((longest + each - 1) / each) : 0);
     if (us < best) {
       best = us;
       t.each = each;
     }
-    if (rounds > 4) break;   // more workgroups take longer from here on
   }
   t.parts = (longest + t.each - 1) / t.each;
+  // Every group of rows has a workgroup of each key head, and no more than two rounds are chosen.
+  const int64_t most_parts = std::max<int64_t>(1, 2 * slots / KV - ((int64_t)counts.size() - 1));
+  t.room = (int)std::min(most_parts, (reach + at_once - 1) / at_once);
   return t;
 }
 // Floats of workspace: of calls of several parts, for each largest logits and weight sums [T H][2] and sums [T H][dh], from a multiple
@@ -128,6 +136,7 @@ inline size_t recent_sums_at(const WindowShape& t, int64_t TH) { return ((size_t
 inline size_t recent_workspace_floats(const WindowShape& t, int64_t TH, int dh) {
   return t.parts > 1 ? recent_sums_at(t, TH) + (size_t)TH * t.parts * dh : 0;
 }
+inline size_t recent_room_floats(const WindowShape& t, int64_t TH, int dh) { return t.room > 1 ? (size_t)TH * t.room * (dh + 2) + 3 : 0; }
 struct RecentBuffers {
   float *sums, *tops;
   int64_t TH;
