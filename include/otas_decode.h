@@ -15,7 +15,7 @@
  *     entry point says how many it has), else through the context's plan buffer.  Calls of the first kind may be captured into a
  *     HIP graph (their host numbers are part of it); of the second kind they are refused under capture (EUNSUPPORTED), and
  *     limited to 1048576 entries (ENOMEM).
- *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, 2^24 of
+ *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, 2^26 of otas_norm_rotary, 2^24 of
  *     otas_cache_append, attention over very many queries of which one is very long (all are given as many workgroups as the longest).
  *     otas_cache_evict has a limit of its own.
  *   - Results do not depend on the order in which the device happens to run anything.
@@ -149,7 +149,7 @@ otas_status otas_cache_evict(otas_ctx *ctx, const otas_kv_cache *cache, const in
  *   eps finite, > 0 (EINVAL).  Means, norms and rotation are float, rounded once; heads of elements beyond 1e18, whose squares' sum
  *   is no float, are not for this entry point.
  *   positions may be NULL where rot_dim is 0.  out may be qkv (then only query and key heads are written), else no overlap; the gains overlap
- *   no part of out (EINVAL).  No host numbers.  Up to 2^27 rows, as otas_rotary. */
+ *   no part of out (EINVAL).  No host numbers. */
 typedef struct {
   const void *q_gain, *k_gain;
   float eps;

@@ -248,7 +248,7 @@ __global__ __launch_bounds__(256, R == 1 ? (FOUR && sizeof(T) == 2 ? 3 : 2) : 1)
   constexpr int NQ = pieces_of<T>(), NK = Held::PIECES, DEPTH = FOUR ? 2 : 1, LDO = 32 * STEPS + 4;
   extern __shared__ __attribute__((aligned(16))) float lds_recent[];
   const PlanFirst plan = PlanFirst::of(plan_);
-  const WorkPlace work = shape.place((int)blockIdx.x, B * c.KV);
+  const WorkPlace work = shape.work(plan, (int)blockIdx.x, B, c.KV);
   const int part = work.part, kh = work.unit % c.KV, q = work.unit / c.KV, G = H / c.KV;
   const int base = plan.at(q), n = plan.at(q + 1) - base, len = plan.at(2 * B + 1 + q), rows = n * G, group0 = work.group * 16 * R;
   const int window = shape.window, sinks = shape.sinks;
@@ -654,9 +654,8 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
 }
 
 template <typename T, bool FOUR>
-static hipError_t attention_recent(const Cache4Ref& c, const void* qkv, int H, const PlanAny& p, int B, const ScoreArgs& sc, const WindowShape& shape,
+static hipError_t attention_recent(const Cache4Ref& c, const void* qkv, int H, const PlanAny& p, int B, int64_t wgs, const ScoreArgs& sc, const WindowShape& shape,
                                    const RecentBuffers& buf, void* o, hipStream_t s) {
-  const int64_t wgs = (int64_t)B * c.KV * shape.groups * shape.parts;
   auto run = [&](auto steps, auto exact, auto r) {
     constexpr int STEPS = decltype(steps)::value;
     auto kern = attention_recent_kernel<T, FOUR, STEPS, decltype(exact)::value, decltype(r)::value>;
@@ -681,16 +680,17 @@ hipError_t launch_attention_recent(int dtype, bool four, const Cache4Ref& c, con
                                    hipStream_t s) {
   if (T <= 0) return hipSuccess;
   const int64_t TH = T * H;
-  if ((int64_t)B * c.KV * shape.groups * shape.parts > kMostGroups || (TH + 3) / 4 > kMostGroups) return kTooManyGroups;
+  const int64_t wgs = shape.workgroups(plan, B, c.KV);
+  if (wgs > kMostGroups || (TH + 3) / 4 > kMostGroups) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   const RecentBuffers buf{workspace + recent_sums_at(shape, TH), workspace, TH};
   hipError_t e;
   if (shape.rows == kManyRows)
     e = launch_attention_rows_bf16(four, c, qkv, H, plan, count, d_plan, B, sc, shape, buf, o, s);
   else if (dtype == 0)
-    e = four ? attention_recent<float, true>(c, qkv, H, p, B, sc, shape, buf, o, s) : attention_recent<float, false>(c, qkv, H, p, B, sc, shape, buf, o, s);
+    e = four ? attention_recent<float, true>(c, qkv, H, p, B, wgs, sc, shape, buf, o, s) : attention_recent<float, false>(c, qkv, H, p, B, wgs, sc, shape, buf, o, s);
   else
-    e = four ? attention_recent<bf16_t, true>(c, qkv, H, p, B, sc, shape, buf, o, s) : attention_recent<bf16_t, false>(c, qkv, H, p, B, sc, shape, buf, o, s);
+    e = four ? attention_recent<bf16_t, true>(c, qkv, H, p, B, wgs, sc, shape, buf, o, s) : attention_recent<bf16_t, false>(c, qkv, H, p, B, wgs, sc, shape, buf, o, s);
   if (e != hipSuccess || shape.parts <= 1) return e;
   auto join = [&](auto zero, auto rows, auto shared) {
     typedef decltype(zero) E;

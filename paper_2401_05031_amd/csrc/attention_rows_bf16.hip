@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
   constexpr int ROWS = kManyRows;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const PlanFirst plan = PlanFirst::of(plan_);
-  const WorkPlace at = shape.place((int)blockIdx.x, B * c.KV);
+  const WorkPlace at = shape.work(plan, (int)blockIdx.x, B, c.KV);
   const int kh = at.unit % c.KV, q = at.unit / c.KV, G = H / c.KV, group0 = at.group * ROWS;
   const bool packed = !FOUR && c.k == nullptr;
   const int base = plan.at(q), n = plan.at(q + 1) - base, rows = n * G;
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
 
 hipError_t launch_attention_rows_bf16(bool four, const Cache4Ref& c, const void* qkv, int H, const int32_t* plan, size_t count, const int32_t* d_plan, int B,
                                       const ScoreArgs& sc, const WindowShape& shape, const RecentBuffers& buf, void* o, hipStream_t s) {
-  const int64_t wgs = (int64_t)B * c.KV * shape.groups * shape.parts;
+  const int64_t wgs = shape.workgroups(plan, B, c.KV);
   if (wgs > kMostGroups) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   auto run = [&](auto width, auto four_, auto cap, auto bias) {

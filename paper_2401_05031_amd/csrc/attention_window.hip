@@ -28,22 +28,32 @@ template <typename T> struct WindowKeys {
 };
 
 template <typename T, int DT, bool WHOLE>
-__global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_window_f32_kernel(PlanAny plan_, const T* __restrict__ qkv, int B, int H, int KV, int width, int xblks,
-                                                                   ScoreArgs sc, int window, int sinks, T* __restrict__ o) {
+__global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_window_f32_kernel(PlanAny plan_, const T* __restrict__ qkv, int B, int H, int KV, int width,
+                                                                   ScoreArgs sc, WindowShape shape, T* __restrict__ o) {
   extern __shared__ __attribute__((aligned(16))) float f32_lds[];
   const PlanFirst plan = PlanFirst::of(plan_);
   // The row blocks of a head on one XCD where heads divide so.
-  const int id = (int)blockIdx.x, pairs = B * H;
-  int pair, xblk;
-  if (pairs % 8 == 0) {
-    const int mine = pairs >> 3, k = id >> 3;
-    pair = xcd_head(id & 7, k % mine, H);
-    xblk = xblks - 1 - k / mine;
+  int q, h, xblk;
+  if (shape.firsts) {
+    const WorkPlace at = shape.work(plan, (int)blockIdx.x, B, H);
+    q = at.unit / H;
+    h = at.unit % H;
+    xblk = plan.at(shape.firsts + q + 1) - plan.at(shape.firsts + q) - 1 - at.group;
   } else {
-    pair = id % pairs;
-    xblk = xblks - 1 - id / pairs;
+    const int id = (int)blockIdx.x, pairs = B * H, xblks = shape.groups;
+    int pair;
+    if (pairs % 8 == 0) {
+      const int mine = pairs >> 3, k = id >> 3;
+      pair = xcd_head(id & 7, k % mine, H);
+      xblk = xblks - 1 - k / mine;
+    } else {
+      pair = id % pairs;
+      xblk = xblks - 1 - id / pairs;
+    }
+    h = pair % H;
+    q = pair / H;
   }
-  const int h = pair % H, q = pair / H, dh = WHOLE ? 32 * DT : width;
+  const int dh = WHOLE ? 32 * DT : width, window = shape.window, sinks = shape.sinks;
   const int base = plan.at(q), n = plan.at(q + 1) - base, row0 = xblk * 32;
   if (row0 >= n) return;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), fr = lane & 31, fk = lane >> 5;
@@ -65,10 +75,9 @@ __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_window_f32_ker
 }
 
 template <typename T>
-static hipError_t attention_window_f32(const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H, int KV,
-                                       int dh, const ScoreArgs& sc, int window, int sinks, void* o, hipStream_t s) {
-  const int xblks = (max_n + 31) / 32;
-  const int64_t wgs = (int64_t)xblks * H * B;
+static hipError_t attention_window_f32(const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int H, int KV, int dh,
+                                       const ScoreArgs& sc, const WindowShape& shape, void* o, hipStream_t s) {
+  const int64_t wgs = shape.workgroups(plan, B, H);
   if (wgs > kMostGroups) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   return with_tiles(dh, [&](auto dt, auto whole) {
@@ -76,22 +85,19 @@ static hipError_t attention_window_f32(const void* qkv, const int32_t* plan, siz
     auto kern = attention_window_f32_kernel<T, DT, decltype(whole)::value>;
     const hipError_t e = set_max_dynamic_lds((const void*)kern, (int)float_rows_lds<DT>());
     if (e != hipSuccess) return e;
-    kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>(p, (const T*)qkv, B, H, KV, dh, xblks, sc, window, sinks, (T*)o);
+    kern<<<dim3((unsigned)wgs), dim3(256), float_rows_lds<DT>(), s>>>(p, (const T*)qkv, B, H, KV, dh, sc, shape, (T*)o);
     return hipGetLastError();
   });
 }
 
-hipError_t launch_attention_window(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int max_n, int H,
-                                   int KV, int dh, const ScoreArgs& sc, int window, int sinks, void* o, hipStream_t s) {
-  if (max_n <= 0) return hipSuccess;
-  if (dtype != 0 && bf16_width(dh)) {
-    WindowShape shape{window, sinks, kRowsShift, kManyRows, (int)(((int64_t)max_n * (H / KV) + kManyRows - 1) / kManyRows), 0, 1, 1};
-    shape.each = window_tiles(kRowsShift, 0, max_n - 1, window, sinks).count;   // all that a group can see
+hipError_t launch_attention_window(int dtype, const void* qkv, const int32_t* plan, size_t count, const int32_t* d_plan, int B, int H, int KV, int dh,
+                                   const ScoreArgs& sc, const WindowShape& shape, void* o, hipStream_t s) {
+  if (shape.groups <= 0) return hipSuccess;
+  if (shape.rows == kManyRows)
     return launch_attention_rows_bf16(false, Cache4Ref{nullptr, nullptr, nullptr, nullptr, 0, KV, dh, 0}, qkv, H, plan, count, d_plan, B, sc, shape,
                                       RecentBuffers{nullptr, nullptr, 0}, o, s);
-  }
-  return dtype == 0 ? attention_window_f32<float>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, window, sinks, o, s)
-                    : attention_window_f32<bf16_t>(qkv, plan, count, d_plan, B, max_n, H, KV, dh, sc, window, sinks, o, s);
+  return dtype == 0 ? attention_window_f32<float>(qkv, plan, count, d_plan, B, H, KV, dh, sc, shape, o, s)
+                    : attention_window_f32<bf16_t>(qkv, plan, count, d_plan, B, H, KV, dh, sc, shape, o, s);
 }
 
 }  // namespace otas

@@ -79,7 +79,7 @@ otas_status attention_last(otas_ctx* c, const Cache4Ref& cache, bool four, int s
   for (int q = 0; q < B; ++q)
     if (!rows_fit(c, cache.KV, length[q])) return OTAS_EUNSUPPORTED;
   const int64_t T = offsets[B];
-  const WindowShape shape = recent_shape(c->desc.dtype, four, cache.dh, c->desc.H, cache.KV, offsets, length, B, window, sinks);
+  WindowShape shape = recent_shape(c->desc.dtype, four, cache.dh, c->desc.H, cache.KV, offsets, length, B, window, sinks);
   const size_t need = recent_workspace_floats(shape, T * c->desc.H, cache.dh) * sizeof(float);
   if (T > 0 && workspace_bytes < need) return OTAS_ENOMEM;
   const size_t in_bytes = qkv_bytes(c, T, cache.KV), out_bytes = rows_bytes(c, T);
@@ -91,6 +91,7 @@ otas_status attention_last(otas_ctx* c, const Cache4Ref& cache, bool four, int s
   std::copy(slot, slot + B, plan.begin() + B + 1);
   std::copy(length, length + B, plan.begin() + 2 * B + 1);
   if (T == 0) return OTAS_OK;
+  shape.count_groups(plan, offsets, B, c->desc.H / cache.KV, kArgInts, kPlanInts);
   OnDevice on(c);
   if (!on.ok) return OTAS_EDEVICE;
   st = place_plan(c, plan);
@@ -144,13 +145,16 @@ otas_status otas_attention_window(otas_ctx* c, const void* qkv, int32_t kv_heads
     for (int q = 0; q < B; ++q) max_n = std::max(max_n, offsets[q + 1] - offsets[q]);
     if (max_n > OTAS_MAX_LONG_SEQ || !rows_fit(c, kv_heads, max_n)) return OTAS_EUNSUPPORTED;
     if (T == 0) return OTAS_OK;
-    const std::vector<int32_t> plan(offsets, offsets + B + 1);
+    const int dh = c->desc.D / c->desc.H;
+    WindowShape shape = packed_shape(c->desc.dtype, dh, c->desc.H, kv_heads, max_n, window, sinks);
+    std::vector<int32_t> plan(offsets, offsets + B + 1);
+    shape.count_groups(plan, offsets, B, shape.rows == kManyRows ? c->desc.H / kv_heads : 1, kArgInts, kPlanInts);
     OnDevice on(c);
     if (!on.ok) return OTAS_EDEVICE;
     const otas_status placed = place_plan(c, plan);
     if (placed != OTAS_OK) return placed;
-    OTAS_LAUNCH_FITTING(K_ATTN, launch_attention_window(c->desc.dtype, qkv, plan.data(), plan.size(), c->d_plan, B, max_n, c->desc.H, kv_heads,
-                                                c->desc.D / c->desc.H, sc, window, sinks, o, c->stream));
+    OTAS_LAUNCH_FITTING(K_ATTN, launch_attention_window(c->desc.dtype, qkv, plan.data(), plan.size(), c->d_plan, B, c->desc.H, kv_heads, dh,
+                                                        sc, shape, o, c->stream));
     return OTAS_OK;
   });
 }

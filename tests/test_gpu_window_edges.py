@@ -171,6 +171,27 @@ def test_a_slot_past_four_gigabytes(lib, four):
         assert torch.equal(back.double(), torch.cat([t[0, :, -3:].transpose(0, 1).reshape(3, -1) for t in values], dim=1))
 
 
+@pytest.mark.parametrize("dtype,H,KV,dh", [("bf16", 8, 2, 64), ("bf16", 4, 4, 80), ("bf16", 6, 2, 48), ("f32", 4, 1, 64)])
+@pytest.mark.parametrize("singles", [5, 70, 500])
+def test_a_long_run_among_single_rows(lib, dtype, H, KV, dh, singles):
+    """Calls whose queries differ so much in rows that they are counted one by one (with 500 of them, in memory), also empty ones."""
+    import torch
+    ctx, g = context(dtype, H, dh), gen(singles)
+    rows = [1] * (singles // 2) + [0, 700, 0] + [1] * (singles // 2) + [290, 0]
+    off = offsets_of(rows)
+    qkv = normal(g, (off[-1], (H + 2 * KV) * dh), dtype)
+    o = torch.empty((off[-1], H * dh), dtype=qkv.dtype, device="cuda")
+    ctx.otas_attention_window(qkv, KV, off, o, 100, 3)
+    within(o, *plain.window(qkv, H, KV, off, 100, 3), "window")
+    slots, lengths, capacity = [(7 * q) % 9 for q in range(len(rows))], [max(n, (13 * q) % 800) for q, n in enumerate(rows)], 800
+    k, v = normal(g, (9, KV, capacity, dh), dtype), normal(g, (9, KV, capacity, dh), dtype)
+    for four in (False, True):
+        cache, (a, b) = packed_cache(lib, k, v) if four else (lib.KVCache(k, v, torch.zeros((9, capacity), dtype=torch.int32, device="cuda")), (k, v))
+        for window, sinks in ((100, 3), (ALL, 0)):
+            want, bound = plain.recent(qkv, H, a, b, off, slots, lengths, window, sinks)
+            within(run_recent(lib, ctx, four, cache, qkv, off, slots, lengths, window, sinks), want, bound, "cached")
+
+
 def decoder(lib, ctx, stream_tokens, H, KV, dh, dtype, window, sinks):
     """What a decoder's layer does with a token of each request, on buffers that it keeps."""
     import torch

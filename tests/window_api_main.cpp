@@ -73,6 +73,40 @@ static int shapes() {
           c = 1;
         }
       }
+  // and of a call whose queries are counted one by one
+  struct Plan {
+    std::vector<int32_t> v;
+    int at(int i) const { return v[i]; }
+  };
+  for (int G : {1, 4})
+    for (int KV : {1, 3, 8})
+      for (int parts : {1, 2}) {
+        const int32_t off[] = {0, 0, 300, 301, 301, 301, 306, 500, 500};
+        const int B = 8;
+        WindowShape t{1, 0, 5, 32, (300 * G + 31) / 32, 1, parts, parts};
+        Plan plan{std::vector<int32_t>(off, off + B + 1)};
+        WindowShape none = t;
+        none.count_groups(plan.v, off, B, G, 17, 1000);   // 18 numbers would not fit
+        CHECK(none.firsts == 0 && plan.v.size() == 9 && none.workgroups(plan.v.data(), B, KV) == (int64_t)B * t.groups * KV * parts);
+        t.count_groups(plan.v, off, B, G, 18, 18);
+        CHECK(t.firsts == 9 && plan.v.size() == 18);
+        std::vector<int> seen(B * KV * t.groups * parts, 0);
+        const int64_t wgs = t.workgroups(plan.v.data(), B, KV);
+        int64_t rows = 0;
+        for (int q = 0; q < B; ++q) rows += ((off[q + 1] - off[q]) * G + 31) / 32;
+        CHECK(wgs == rows * KV * parts);
+        for (int id = 0; id < wgs; ++id) {
+          const WorkPlace p = t.work(plan, id, B, KV);
+          const int q = p.unit / KV;
+          CHECK(p.unit >= 0 && q < B && p.group >= 0 && p.group * 32 < (off[q + 1] - off[q]) * G && p.part >= 0 && p.part < parts);
+          CHECK(!seen[(p.unit * t.groups + p.group) * parts + p.part]++);
+        }
+        Plan even{{0, 300, 580, 870}};
+        WindowShape same = t;
+        same.firsts = 0;
+        same.count_groups(even.v, even.v.data(), 3, G, 960, 2000);
+        CHECK(same.firsts == 0 && even.v.size() == 4);
+      }
   return 0;
 }
 
