@@ -81,7 +81,10 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
                                                                      ScoreArgs sc, CapArgs cap, RecentBuffers out, bf16_t* __restrict__ o) {
   typedef TileRows<DH> R;
   constexpr size_t KB = R::bytes(kKeys), BUF = rows_buffer<DH>();   // keys | values | slack
-  constexpr int ROWS = kManyRows;
+  // Blocks of 32 keys at a time.  One by one, halves of a tile that no row of the wave sees are left out; two at once cover each other's latencies.
+  // Width 64 (4 x 1500 rows, window 300 / 2 x 6000, 1000 / 8192, all), one 27 / 87 / 219 us, two 29 / 89 / 216; 80: 42 / 115 / 264 and 43 / 115 / 238;
+  // 128: 49 / 149 / 337 and 50 / 140 / 312.
+  constexpr int ROWS = kManyRows, NB = DH == 64 ? 1 : 2;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const PlanFirst plan = PlanFirst::of(plan_);
   const WorkPlace at = shape.work(plan, (int)blockIdx.x, B, c.KV);
@@ -130,9 +133,9 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
     value_loader.load(vbase + from, ldb, len - 1 - t * kKeys, buf + KB);
   };
   const Score2 score = Score2::of(sc, BIAS ? sc.slopes[head] : 0.f, place);
-  // Whether rows at places a .. b all see all of the tile from kb on, and whether any of them sees any.
-  auto all_see = [&](int a, int b, int kb) { return kb + kKeys - 1 <= a && (kb > b - window || kb + kKeys <= sinks); };
-  auto some_see = [&](int a, int b, int kb) { return kb <= b && (kb + kKeys - 1 > a - window || kb < sinks); };
+  // Whether rows at places a .. b all see all of the `keys` keys from kb on, and whether any of them sees any.
+  auto all_see = [&](int a, int b, int kb, int keys) { return kb + keys - 1 <= a && (kb > b - window || kb + keys <= sinks); };
+  auto some_see = [&](int a, int b, int kb, int keys) { return kb <= b && (kb + keys - 1 > a - window || kb < sinks); };
   bool met = false;   // whether this thread took out a value that is not finite
 
   if constexpr (FOUR) {
@@ -158,26 +161,31 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
       wait_all();   // this wave's part of the tile is there
       // Of a tile that some row does not see all of, values that are not finite are taken out and come back at the end, to
       // the rows that see them.
-      if (!all_see(p0, p1, kb)) met |= value_loader.make_finite(buf + KB, lane, [&](int r) { return kb + r <= p1; });
+      if (!all_see(p0, p1, kb, kKeys)) met |= value_loader.make_finite(buf + KB, lane, [&](int r) { return kb + r <= p1; });
       wait_lds_barrier();   // all of it, and nobody reads the other buffer any more
       if (i + 1 < end) fetch(tiles.tile(i + 1), other);
     }
-    if (active && some_see(w0, w1, kb)) {   // wave-uniform
+    if (!active) continue;
+#pragma unroll 1
+    for (int b0 = 0; b0 < 2; b0 += NB) {
+      const int from = kb + 32 * b0;
+      if (!some_see(w0, w1, from, 32 * NB)) continue;   // wave-uniform
+      const char* keys = buf + b0 * 32 * R::ROW_BYTES;
       __builtin_amdgcn_s_setprio(0);
-      floatx16 s[2];
-      tile_products<DH, 2>(s, w, buf, 0, fr, fk);
+      floatx16 s[NB];
+      tile_products<DH, NB>(s, w, keys, 0, fr, fk);
       short8_t v[WaveRows<DH>::DT];
-      first_values<DH>(v, buf + KB, 0, lane);
+      first_values<DH>(v, keys + KB, 0, lane);
       __builtin_amdgcn_s_setprio(1);   // a wave that needs the vector ALU goes before one at its products, as in attention_masked_bf16.hip
-      const bool whole = all_see(w0, w1, kb);
+      const bool whole = all_see(w0, w1, from, 32 * NB);
       bool done = false;
-      if (CAP && !BIAS && whole) done = tile_weights_capped<DH, 2>(w, s, cap);
-      if (CAP && !done) tile_capped<CAP, 2>(s, score, cap);
-      const int behind = place - kb - 4 * fk;   // the row's distance from the lane's first key
+      if (CAP && !BIAS && whole) done = tile_weights_capped<DH, NB>(w, s, cap);
+      if (CAP && !done) tile_capped<CAP, NB>(s, score, cap);
+      const int behind = place - from - 4 * fk;   // the row's distance from the lane's first key
       if (BIAS) {
         const float near = (float)behind;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float d = near - (float)(32 * b + 8 * (e >> 2) + (e & 3));
@@ -185,15 +193,15 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
           }
       }
       if (!whole) {
-        if (kb >= sinks) {
+        if (from >= sinks) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[b][e] = (uint32_t)(behind - (32 * b + 8 * (e >> 2) + (e & 3))) < (uint32_t)window ? s[b][e] : -INFINITY;
         } else {
-          const int left = sinks - kb - 4 * fk;
+          const int left = sinks - from - 4 * fk;
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const int j = 32 * b + 8 * (e >> 2) + (e & 3);
@@ -202,15 +210,15 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
             }
         }
       }
-      if (!done) tile_weights<DH, 2>(w, s, CAP || BIAS ? 1.f : score.scale2);
+      if (!done) tile_weights<DH, NB>(w, s, CAP || BIAS ? 1.f : score.scale2);
       __builtin_amdgcn_s_setprio(0);
-      tile_sums<DH, 2>(w, s, v, buf + KB, 0, lane);
+      tile_sums<DH, NB>(w, s, v, keys + KB, 0, lane);
     }
   }
   if (any_wave(met, reinterpret_cast<int*>(lds + 2 * BUF), wave, lane)) {   // workgroup-uniform
     for (int i = begin; i < end; ++i) {
       const int kb = tiles.tile(i) * kKeys;
-      if (!FOUR && all_see(p0, p1, kb)) continue;
+      if (!FOUR && all_see(p0, p1, kb, kKeys)) continue;
       for (int j = kb; j < min(kb + kKeys, p1 + 1); ++j) {
         const bool see = j <= place && (place - j < window || j < sinks);
 #pragma unroll

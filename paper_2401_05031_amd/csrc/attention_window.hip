@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256, DT <= 2 ? 3 : 2) void attention_window_f32_ker
     const WorkPlace at = shape.work(plan, (int)blockIdx.x, B, H);
     q = at.unit / H;
     h = at.unit % H;
-    xblk = plan.at(shape.firsts + q + 1) - plan.at(shape.firsts + q) - 1 - at.group;
+    xblk = at.group;
   } else {
     const int id = (int)blockIdx.x, pairs = B * H, xblks = shape.groups;
     int pair;
