@@ -238,28 +238,36 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
     }
   }
   const float l = xor32_sum(w.l);
-  if (wrow0 + fr >= rows) return;
+  if (!active) return;
+  const bool mine = wrow0 + fr < rows;   // both lanes of a row
   const int64_t to = (int64_t)(base + token) * H + head;
   const bool only = shape.parts_of(tiles) == 1;
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int t = 0; t < WaveRows<DH>::DT; ++t)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d = t * 32 + g * 8 + fk * 4;
-      if (d < DH) {
-        const floatx4 x = {w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]};
-        if (only) {
-          bf16x4 v;
+    for (int g = 0; g < 4; g += 2)
+      if (t * 32 + g * 8 < DH) {
+        if (only) {   // the lane's halves of two eights change places with the other half's: whole eights are stored
+          uint32_t x[2][2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (bf16_t)(l == 0.f ? 0.f : x[e] * inv);
-          *reinterpret_cast<bf16x4*>(o + to * DH + d) = v;
-        } else {
-          *reinterpret_cast<floatx4*>(out.sums + ((int64_t)at.part * out.TH + to) * DH + d) = x;
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int at = 4 * (g + i) + 2 * e;
+              const bf16x2 v = {(bf16_t)(l == 0.f ? 0.f : w.o[t][at] * inv), (bf16_t)(l == 0.f ? 0.f : w.o[t][at + 1] * inv)};
+              __builtin_memcpy(&x[i][e], &v, 4);
+            }
+          const auto lo = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false), hi = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+          if (mine) *reinterpret_cast<uint4*>(o + to * DH + t * 32 + (g + fk) * 8) = uint4{lo[0], hi[0], lo[1], hi[1]};
+        } else if (mine) {
+#pragma unroll
+          for (int i = g; i < g + 2; ++i)
+            *reinterpret_cast<floatx4*>(out.sums + ((int64_t)at.part * out.TH + to) * DH + t * 32 + i * 8 + fk * 4) =
+                floatx4{w.o[t][4 * i], w.o[t][4 * i + 1], w.o[t][4 * i + 2], w.o[t][4 * i + 3]};
         }
       }
-    }
-  if (!only && fk == 0) {
+  if (!only && mine && fk == 0) {
     out.tops[2 * (at.part * out.TH + to)] = w.m;
     out.tops[2 * (at.part * out.TH + to) + 1] = l;
   }
