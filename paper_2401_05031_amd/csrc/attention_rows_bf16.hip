@@ -52,24 +52,30 @@ template <int DH> struct GroupLoader {
     kb = *reinterpret_cast<const uint8_t*>(ks + at);
     vb = *reinterpret_cast<const uint8_t*>(vs + at);
   }
-  // Keys from `end` of the tile on, whose scales may be anything, count as 0, and so do groups of values that are no numbers.  Whether
-  // there were any of the latter before `end`.
-  __device__ __forceinline__ bool store(char* __restrict__ keys, char* __restrict__ values, int end) const {
-    if (!mine) return false;
+  // What was loaded made ready for LDS: keys from `end` of the tile on, whose scales may be anything, have no values, and neither have groups
+  // that are no numbers.  Whether there were any of the latter before `end`.
+  __device__ __forceinline__ bool prepare(int end) {
     const bool here = row < end, odd = here && vb == kNoNumber;
-    auto write = [&](char* to, const uint32_t (&w)[4], float f, uint32_t all, bool key) {
+    if (!here || odd) {
+      vb = 0;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        if (LAST != 0 && c >= LAST && g == GROUPS - 1) break;
-        const uint4 u = {pair4_bf16<0>(w[c], f) | all, pair4_bf16<1>(w[c], f) | all, pair4_bf16<2>(w[c], f) | all, pair4_bf16<3>(w[c], f) | all};
-        const int p = g * 4 + c;
-        *reinterpret_cast<uint4*>(to + row * R::ROW_BYTES + (key ? R::key_piece(row, p) : R::value_piece(row, p)) * 16) = u;
-      }
-    };
-    write(keys, kw, scale4(kb), kb == kNoNumber ? 0x7FC07FC0u : 0u, true);
-    const uint32_t none[4] = {0, 0, 0, 0};
-    if (!here || odd) write(values, none, 1.f, 0, false); else write(values, vw, scale4(vb), 0, false);
-    return odd;
+      for (int c = 0; c < 4; ++c) vw[c] = 0;
+    }
+    return mine && odd;
+  }
+  static constexpr int PIECES = 8;
+  // Piece c of these: eight keys' elements (c < 4), or values'.  A key's group that is no number has elements that are none.
+  __device__ __forceinline__ void store(int c, char* __restrict__ keys, char* __restrict__ values) const {
+    const int p = g * 4 + (c & 3);
+    if (!mine || (LAST != 0 && (c & 3) >= LAST && g == GROUPS - 1)) return;
+    const uint32_t word = c < 4 ? kw[c & 3] : vw[c & 3], all = c < 4 && kb == kNoNumber ? 0x7FC07FC0u : 0u;
+    const float f = scale4(c < 4 ? kb : vb);
+    const uint4 u = {pair4_bf16<0>(word, f) | all, pair4_bf16<1>(word, f) | all, pair4_bf16<2>(word, f) | all, pair4_bf16<3>(word, f) | all};
+    *reinterpret_cast<uint4*>((c < 4 ? keys : values) + row * R::ROW_BYTES + (c < 4 ? R::key_piece(row, p) : R::value_piece(row, p)) * 16) = u;
+  }
+  __device__ __forceinline__ void store_all(char* __restrict__ keys, char* __restrict__ values) const {
+#pragma unroll
+    for (int c = 0; c < PIECES; ++c) store(c, keys, values);
   }
 };
 
@@ -84,7 +90,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
   // Blocks of 32 keys at a time.  One by one, halves of a tile that no row of the wave sees are left out; two at once cover each other's latencies.
   // Width 64 (4 x 1500 rows, window 300 / 2 x 6000, 1000 / 8192, all), one 27 / 87 / 219 us, two 29 / 89 / 216; 80: 42 / 115 / 264 and 43 / 115 / 238;
   // 128: 49 / 149 / 337 and 50 / 140 / 312.
-  constexpr int ROWS = kManyRows, NB = DH == 64 ? 1 : 2;
+  constexpr int ROWS = kManyRows, NB = DH == 64 && !FOUR ? 1 : 2;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const PlanFirst plan = PlanFirst::of(plan_);
   const WorkPlace at = shape.work(plan, (int)blockIdx.x, B, c.KV);
@@ -140,7 +146,8 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
 
   if constexpr (FOUR) {
     groups.load(tiles.tile(begin));
-    met |= groups.store(lds, lds + KB, p1 + 1 - tiles.tile(begin) * kKeys);
+    met |= groups.prepare(p1 + 1 - tiles.tile(begin) * kKeys);
+    groups.store_all(lds, lds + KB);
     if (begin + 1 < end) groups.load(tiles.tile(begin + 1));
   } else {
     fetch(tiles.tile(begin), lds);
@@ -153,10 +160,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
     const int kb = tiles.tile(i) * kKeys;
     if constexpr (FOUR) {
       wait_lds_barrier();   // the tile is there, and nobody reads the other buffer any more
-      if (i + 1 < end) {
-        met |= groups.store(other, other + KB, p1 + 1 - tiles.tile(i + 1) * kKeys);
-        if (i + 2 < end) groups.load(tiles.tile(i + 2));
-      }
+      if (i + 1 < end) met |= groups.prepare(p1 + 1 - tiles.tile(i + 1) * kKeys);
     } else {
       wait_all();   // this wave's part of the tile is there
       // Of a tile that some row does not see all of, values that are not finite are taken out and come back at the end, to
@@ -165,15 +169,25 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
       wait_lds_barrier();   // all of it, and nobody reads the other buffer any more
       if (i + 1 < end) fetch(tiles.tile(i + 1), other);
     }
-    if (!active) continue;
+    bool stored = !FOUR;   // the next tile in 4 bits; behind the last one what is there once more, where nobody reads it
 #pragma unroll 1
     for (int b0 = 0; b0 < 2; b0 += NB) {
       const int from = kb + 32 * b0;
-      if (!some_see(w0, w1, from, 32 * NB)) continue;   // wave-uniform
+      if (!active || !some_see(w0, w1, from, 32 * NB)) continue;   // wave-uniform
       const char* keys = buf + b0 * 32 * R::ROW_BYTES;
       __builtin_amdgcn_s_setprio(0);
       floatx16 s[NB];
-      tile_products<DH, NB>(s, w, keys, 0, fr, fk);
+      if constexpr (FOUR && NB == 2) {
+        tile_products<DH, NB>(s, w, keys, 0, fr, fk, [&](int j) {
+#pragma unroll
+          for (int c = 0; c < groups.PIECES; ++c)
+            if (c * (WaveRows<DH>::KS * NB) / groups.PIECES == j) groups.store(c, other, other + KB);
+        });
+        stored = true;
+        if (i + 2 < end) groups.load(tiles.tile(i + 2));
+      } else {
+        tile_products<DH, NB>(s, w, keys, 0, fr, fk);
+      }
       short8_t v[WaveRows<DH>::DT];
       first_values<DH>(v, keys + KB, 0, lane);
       __builtin_amdgcn_s_setprio(1);   // a wave that needs the vector ALU goes before one at its products, as in attention_masked_bf16.hip
@@ -213,6 +227,10 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
       if (!done) tile_weights<DH, NB>(w, s, CAP || BIAS ? 1.f : score.scale2);
       __builtin_amdgcn_s_setprio(0);
       tile_sums<DH, NB>(w, s, v, keys + KB, 0, lane);
+    }
+    if (!stored) {
+      groups.store_all(other, other + KB);
+      if (i + 2 < end) groups.load(tiles.tile(i + 2));
     }
   }
   if (any_wave(met, reinterpret_cast<int*>(lds + 2 * BUF), wave, lane)) {   // workgroup-uniform

@@ -152,9 +152,11 @@ template <int DH> struct WaveRows {   // a wave's 32 rows
 };
 
 // Products of the rows with NB blocks of 32 keys of the tile, from block b0 on.  The keys of a block are read while the products of
-// the one before it run (left alone the compiler reads each piece just before its product, and waits for it there).
-template <int DH, int NB>
-__device__ __forceinline__ void tile_products(floatx16 (&s)[NB], const WaveRows<DH>& w, const char* __restrict__ lds_k, int b0, int fr, int fk) {
+// the one before it run (left alone the compiler reads each piece just before its product, and waits for it there).  beneath(i): other work,
+// behind product i.
+struct NoWork { __device__ __forceinline__ void operator()(int) const {} };
+template <int DH, int NB, class F = NoWork>
+__device__ __forceinline__ void tile_products(floatx16 (&s)[NB], const WaveRows<DH>& w, const char* __restrict__ lds_k, int b0, int fr, int fk, F beneath = F()) {
   typedef TileRows<DH> R;
   constexpr int KS = WaveRows<DH>::KS;
   auto piece = [&](int b, int ks) {   // 32 b does not change the rule
@@ -172,6 +174,7 @@ __device__ __forceinline__ void tile_products(floatx16 (&s)[NB], const WaveRows<
     for (int ks = 0; ks < KS; ++ks) {
       s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b & 1][ks], w.q[ks], s[b], 0, 0, 0);
       if (b + 1 < NB) kf[(b + 1) & 1][ks] = piece(b + 1, ks);
+      beneath(b * KS + ks);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
