@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
   if (group0 >= rows) return;
   const int len = packed ? n : plan.at(2 * B + 1 + q), place0 = len - n;
   const WindowTiles tiles = shape.tiles(at.group, n, G, len);
-  const int begin = at.part * shape.each, end = min(tiles.count, begin + shape.each);
+  const int each = shape.each_of(tiles), begin = at.part * each, end = min(tiles.count, begin + each);
   if (begin >= end) return;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fk = lane >> 5;
   const int wrow0 = group0 + wave * 32, row = min(wrow0 + fr, rows - 1), token = row / G, head = kh * G + row % G, place = place0 + token;

@@ -57,7 +57,17 @@ struct WindowShape {
     const int last = (group + 1) * rows < n * G ? (group + 1) * rows - 1 : n * G - 1, at = length - n;
     return window_tiles(shift, at + group * rows / G, at + last / G, window, sinks);
   }
-  __host__ __device__ int parts_of(const WindowTiles& t) const { return (t.count + each - 1) / each; }
+  // Tiles that go side by side: one for each wave, or one that all waves have in LDS.
+  __host__ __device__ int at_once() const { return rows == kManyRows ? 1 : 4; }
+  // Tiles of a part of these: as many parts as shares of `each` would be, or fewer, but alike.
+  __host__ __device__ int each_of(const WindowTiles& t) const {
+    const int unit = at_once(), steps = (t.count + unit - 1) / unit, p = (t.count + each - 1) / each;
+    return (steps + p - 1) / p * unit;
+  }
+  __host__ __device__ int parts_of(const WindowTiles& t) const {
+    const int e = each_of(t);
+    return (t.count + e - 1) / e;
+  }
   // The row groups of a share run side by side on one XCD, whose L2 then has the share once.
   __host__ __device__ WorkPlace place(int id, int units) const { return place(id, units, groups); }
   __host__ __device__ WorkPlace place(int id, int units, int groups) const {
@@ -115,7 +125,7 @@ inline int window_slots(int dtype, bool four, int rows) {
 }
 // The share of a workgroup is chosen by what a call should take: rounds of workgroups of so many steps (four tiles at once, one a wave; of many
 // rows one tile), a launch more and its join where there are several parts.  A step is latency, or the bytes of all workgroups at
-// once.  In us, measured: 6 before the first step, 3.5 and a tenth for each part for the join; 1 a step (f32 1.5), 1.3 a tile of many rows (4 bits 2.3) and 1.7 times that
+// once.  In us, measured: 6 before the first step, 3.5 and a tenth for each part for the join; 1 a step (f32 1.5 at width 64, 3 at 128), 1.3 a tile of many rows (4 bits 2.3) and 1.7 times that
 // where two workgroups share a CU; 6.5 TB/s.  Shares counted from every query's own length: one token of 32 queries over 5700 .. 8192 entries of 8 key heads of 128
 // in 4 bits 46 us, where shares of the longest query's length in 768 / 256 parts had every third query's last part empty.
 inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, const int32_t* off, const int32_t* length, int B, int window, int sinks) {
@@ -137,13 +147,13 @@ inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, con
     if (n > 0)
       reach = std::max(reach, std::min(whole(length[q]), whole(std::min(sinks, length[q])) + whole((int64_t)std::min(window, length[q]) + t.rows / G + 1) + 1));
   }
-  const int longest = *std::max_element(counts.begin(), counts.end()), slots = window_slots(dtype, four, t.rows), at_once = many ? 1 : 4;
+  const int longest = *std::max_element(counts.begin(), counts.end()), slots = window_slots(dtype, four, t.rows), at_once = t.at_once();
   const double bytes = at_once * (2 << t.shift) * (four ? dh / 2 + (dh + 31) / 32 : dh * (dtype == 0 ? 4.0 : 2.0));
-  const double latency = many ? (four ? 2.3 : 1.3) : dtype == 0 ? 1.5 : 1.0;
+  const double latency = many ? (four ? 2.3 : 1.3) : dtype == 0 ? dh / 43.0 : 1.0;
   double best = 1e30;
   t.each = longest;
-  for (int64_t steps = (longest + at_once - 1) / at_once; steps > 0; steps = counts.size() > 64 ? steps * 2 / 3 : steps * 7 / 8) {
-    const int each = (int)steps * at_once;
+  for (int steps = (longest + at_once - 1) / at_once; steps > 0; steps -= std::max(1, steps / 12)) {
+    const int each = steps * at_once;
     int64_t wgs = 0;
     for (const int32_t c : counts) wgs += (c + each - 1) / each;
     wgs *= KV;
@@ -156,7 +166,8 @@ inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, con
       t.each = each;
     }
   }
-  t.parts = (longest + t.each - 1) / t.each;
+  t.parts = t.parts_of(WindowTiles{0, 0, longest});
+  for (const int32_t c : counts) t.parts = std::max(t.parts, t.parts_of(WindowTiles{0, 0, c}));
   // Every group of rows has a workgroup of each key head, and no more than two rounds are chosen.
   const int64_t most_parts = std::max<int64_t>(1, 2 * slots / KV - ((int64_t)counts.size() - 1));
   t.room = (int)std::min(most_parts, (reach + at_once - 1) / at_once);

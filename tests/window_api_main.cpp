@@ -50,6 +50,17 @@ static int shapes() {
                   before = x;
                   have[x] = 1;
                 }
+                int next = 0;
+                for (int p = 0; p < t.parts + 1; ++p) {
+                  const int each = t.each_of(w), begin = p * each, end = std::min(w.count, begin + each);
+                  if (p < t.parts_of(w)) {
+                    CHECK(begin == next && end > begin && each <= t.each && each % t.at_once() == 0);
+                    next = end;
+                  } else {
+                    CHECK(begin >= end);
+                  }
+                }
+                CHECK(next == w.count);
                 for (int r = g * t.rows; r < std::min((g + 1) * t.rows, n * G); ++r) {
                   const int place = length - n + r / G;
                   for (int j = 0; j <= place; ++j)
