@@ -89,8 +89,9 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
   constexpr size_t KB = R::bytes(kKeys), BUF = rows_buffer<DH>();   // keys | values | slack
   // Blocks of 32 keys at a time.  One by one, halves of a tile that no row of the wave sees are left out; two at once cover each other's latencies.
   // Width 64 (4 x 1500 rows, window 300 / 2 x 6000, 1000 / 8192, all), one 27 / 87 / 219 us, two 29 / 89 / 216; 80: 42 / 115 / 264 and 43 / 115 / 238;
-  // 128: 49 / 149 / 337 and 50 / 140 / 312.
-  constexpr int ROWS = kManyRows, NB = DH == 64 && !FOUR ? 1 : 2;
+  // 128: 49 / 149 / 337 and 50 / 140 / 312.  In 4 bits at width 64 (4 x 2000 rows over 4096 entries, window 1024) 121 and 144 us, with which three waves
+  // a SIMD have the registers.
+  constexpr int ROWS = kManyRows, NB = DH == 64 ? 1 : 2;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const PlanFirst plan = PlanFirst::of(plan_);
   const WorkPlace at = shape.work(plan, (int)blockIdx.x, B, c.KV);

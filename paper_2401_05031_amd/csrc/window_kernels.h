@@ -119,7 +119,8 @@ inline int window_rows(int dtype, int dh, int64_t most) {
   if (most <= 16) return 16;
   return most > 32 && dtype != 0 && bf16_width(dh) ? kManyRows : 32;
 }
-// Workgroups of these kernels that the chip holds at once: by their registers, of the many rows' by LDS.
+// Workgroups of these kernels that the chip holds at once: by their registers, of the many rows' by LDS (at width 64 it holds three a CU; shares
+// for that many took 2 to 5 us longer: 64 rows of 8 queries over 2000 entries, 32 heads on 8, 35.5 and 38.5 us).
 inline int window_slots(int dtype, bool four, int rows) {
   return 256 * (rows == 16 ? (four && dtype != 0 ? 3 : 2) : rows == kManyRows ? 2 : 1);
 }
