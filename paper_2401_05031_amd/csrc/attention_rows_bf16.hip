@@ -61,12 +61,26 @@ template <int DH> struct GroupLoader {
 #pragma unroll
       for (int c = 0; c < 4; ++c) vw[c] = 0;
     }
+    if (TURNS) {
+      auto swap_if = [](bool b, uint32_t& x, uint32_t& y) {
+        const uint32_t t = b ? y : x;
+        y = b ? x : y;
+        x = t;
+      };
+      swap_if(turn() & 1, vw[0], vw[1]);
+      swap_if(turn() & 1, vw[2], vw[3]);
+      swap_if(turn() & 2, vw[0], vw[2]);
+      swap_if(turn() & 2, vw[1], vw[3]);
+    }
     return mine && odd;
   }
+  // Values' pieces of four rows (eight of width 64) would lie on the same banks: every thread begins with another of its four.
+  static constexpr bool TURNS = DH % 64 == 0;
+  __device__ __forceinline__ int turn() const { return TURNS ? (DH == 128 ? row : row >> 1) & 3 : 0; }
   static constexpr int PIECES = 8;
   // Piece c of these: eight keys' elements (c < 4), or values'.  A key's group that is no number has elements that are none.
   __device__ __forceinline__ void store(int c, char* __restrict__ keys, char* __restrict__ values) const {
-    const int p = g * 4 + (c & 3);
+    const int p = g * 4 + (c < 4 ? c : (c & 3) ^ turn());
     if (!mine || (LAST != 0 && (c & 3) >= LAST && g == GROUPS - 1)) return;
     const uint32_t word = c < 4 ? kw[c & 3] : vw[c & 3], all = c < 4 && kb == kNoNumber ? 0x7FC07FC0u : 0u;
     const float f = scale4(c < 4 ? kb : vb);
