@@ -34,7 +34,9 @@ template <typename P> __device__ __forceinline__ RowPlace row_place(const P& pla
   return RowPlace{plan[B + 1 + lo], (int64_t)plan[2 * B + 1 + lo] + (i - plan[lo])};
 }
 
-// A thread has eight elements of a head, four threads a group, whose largest element goes round them in registers.  Memory-bound.
+// A thread has eight elements of a head, four threads a group, whose largest element goes round them in registers.  Memory-bound: 12700 rows of
+// 8 + 8 heads of 128 bf16 (66 MB with what is written, part of it from and to the last-level cache) 14.5 us, 32 rows 3.9 us.  A row a workgroup 18 us;
+// with conversions in plain arithmetic and no runs of rows to each XCD, whose scales then go out byte by byte, 24.
 template <typename T, int ROWS, typename P>
 __global__ __launch_bounds__(256) void cache4_append_kernel(Cache4Ref c, const T* __restrict__ qkv, int H, P plan, int B, int N, bool has_rows) {
   const int i0 = first_row((int)blockIdx.x, N, ROWS);
@@ -75,7 +77,7 @@ __global__ __launch_bounds__(256) void cache4_append_kernel(Cache4Ref c, const T
   }
 }
 
-// A thread has eight elements of a head.
+// A thread has eight elements of a head.  Memory-bound: 12700 rows 14.3 us (a row a workgroup 16), 32 rows 3.7 us.
 template <typename T, int ROWS, typename P>
 __global__ __launch_bounds__(256) void cache4_read_kernel(Cache4Ref c, P plan, int B, int N, T* __restrict__ kv) {
   const int i0 = first_row((int)blockIdx.x, N, ROWS);
