@@ -565,24 +565,33 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
   const int64_t first = SHARED ? blockIdx.x : ((int64_t)blockIdx.x * 4 + wave) * ROWS;
   if (first >= in.TH) return;
   int parts[ROWS], most = 0;
+  int token = (int)first / H, head = (int)first - token * H, of_key = head % G;   // TH is below 2^26
   int lo = 0;   // the query of the first row, then of the next
   {
-    const int token = (int)(first / H);
     int hi = B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (plan.at(mid) <= token) lo = mid; else hi = mid;
     }
   }
+  int known = -1, of_group = 0;   // a group of rows and its parts: rows side by side mostly are of one, and counting is a chain of divisions
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
-    const int64_t at = min(first + r, in.TH - 1);
-    const int token = (int)(at / H), head = (int)(at % H);
-    while (plan.at(lo + 1) <= token) ++lo;
-    const int base = plan.at(lo), n = plan.at(lo + 1) - base, row = (token - base) * G + head % G;
-    parts[r] = shape.parts_of(shape.tiles(row / shape.rows, n, G, plan.at(2 * B + 1 + lo)));
-    if (first + r >= in.TH || parts[r] <= 1) parts[r] = 0;   // none, or written already
+    parts[r] = 0;   // none, or written already
+    if (first + r >= in.TH) continue;
+    for (; plan.at(lo + 1) <= token; ++lo) known = -1;
+    const int base = plan.at(lo), n = plan.at(lo + 1) - base, group = ((token - base) * G + of_key) >> __builtin_ctz(shape.rows);
+    if (group != known) {
+      of_group = shape.parts_of(shape.tiles(group, n, G, plan.at(2 * B + 1 + lo)));
+      known = group;
+    }
+    if (of_group > 1) parts[r] = of_group;
     most = max(most, parts[r]);
+    if (++of_key == G) of_key = 0;
+    if (++head == H) {
+      head = 0;
+      ++token;
+    }
   }
   if (SHARED && most == 0) return;   // workgroup-uniform
   const bool mine = 2 * lane < dh;

@@ -35,7 +35,8 @@ def run_recent(lib, ctx, four, cache, qkv, off, slots, lengths, window, sinks, s
 @pytest.mark.parametrize("dtype,H,KV,dh,rows,lengths,window,sinks", [
     ("bf16", 16, 8, 128, [1], [9001], ALL, 0), ("bf16", 4, 1, 64, [1, 1], [20000, 40], 15000, 70), ("f32", 4, 2, 64, [1], [9001], ALL, 0),
     ("f32", 2, 1, 80, [3, 1], [5003, 17], 4000, 5), ("bf16", 16, 2, 128, [256, 256, 1, 200], [4000, 3001, 900, 200], 2500, 4),
-    ("bf16", 8, 4, 80, [300], [2049], ALL, 0), ("f32", 8, 2, 32, [600], [1500], 300, 33)])
+    ("bf16", 8, 4, 80, [300], [2049], ALL, 0), ("f32", 8, 2, 32, [600], [1500], 300, 33),
+    ("bf16", 4, 2, 96, [150, 40], [1500, 700], 600, 40), ("bf16", 8, 2, 64, [100, 33, 1], [2500, 500, 64], ALL, 0), ("bf16", 6, 2, 128, [700, 3, 300], [3000, 2900, 2000], ALL, 0)])
 def test_long_windows_in_parts(lib, dtype, H, KV, dh, rows, lengths, window, sinks, four):
     """Calls cut into several parts, of few rows and of many, joined by every form of the join."""
     ctx, g, B = context(dtype, H, dh), gen(lengths[0]), len(rows)

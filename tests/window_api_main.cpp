@@ -70,6 +70,26 @@ static int shapes() {
               CHECK(recent_sums_at(t, n * 4 * G) % 4 == 0);
               CHECK(recent_workspace_floats(t, n * 4 * G, 128) <= recent_room_floats(t, n * 4 * G, 128));
             }
+  // the workspace of long queries is enough for shorter ones
+  uint32_t seed = 1;
+  auto draw = [&](int n) { seed = seed * 1664525u + 1013904223u; return (int)((uint64_t)(seed >> 8) * n >> 24); };
+  for (int round = 0; round < 400; ++round) {
+    const int B = 1 + draw(6), G = 1 << draw(4), KV = 1 + draw(8), dh = 8 * (1 + draw(16)), dtype = draw(2), window = draw(3) ? 1 + draw(3000) : INT32_MAX,
+              sinks = draw(2) * draw(200);
+    std::vector<int32_t> off{0}, before, after;
+    for (int q = 0; q < B; ++q) {
+      off.push_back(off.back() + draw(draw(2) ? 3 : 300));
+      before.push_back(off[q + 1] - off[q] + draw(9000));
+      after.push_back(before[q] + draw(draw(2) ? 40 : 30000));
+    }
+    for (bool four : {false, true}) {
+      const WindowShape small = recent_shape(dtype, four, dh, G * KV, KV, off.data(), before.data(), B, window, sinks);
+      const WindowShape large = recent_shape(dtype, four, dh, G * KV, KV, off.data(), after.data(), B, window, sinks);
+      const int64_t TH = (int64_t)off[B] * G * KV;
+      CHECK(recent_workspace_floats(small, TH, dh) <= recent_room_floats(small, TH, dh));
+      CHECK(recent_room_floats(small, TH, dh) <= recent_room_floats(large, TH, dh));
+    }
+  }
   // every share of a call has a place of its own
   for (int groups : {1, 2, 7})
     for (int parts : {1, 3})
