@@ -118,7 +118,8 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
   if (group0 >= rows) return;
   const int len = packed ? n : plan.at(2 * B + 1 + q), place0 = len - n;
   const WindowTiles tiles = shape.tiles(at.group, n, G, len);
-  const int each = shape.each_of(tiles), begin = at.part * each, end = min(tiles.count, begin + each);
+  // a division is a tenth of a microsecond before the first load: none without parts
+  const int each = shape.parts == 1 ? tiles.count : shape.each_of(tiles), begin = at.part * each, end = min(tiles.count, begin + each);
   if (begin >= end) return;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fk = lane >> 5;
   const int wrow0 = group0 + wave * 32, row = min(wrow0 + fr, rows - 1), token = row / G, head = kh * G + row % G, place = place0 + token;
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
   if (!active) return;
   const bool mine = wrow0 + fr < rows;   // both lanes of a row
   const int64_t to = (int64_t)(base + token) * H + head;
-  const bool only = shape.parts_of(tiles) == 1;
+  const bool only = shape.parts == 1 || shape.parts_of(tiles) == 1;
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int t = 0; t < WaveRows<DH>::DT; ++t)
