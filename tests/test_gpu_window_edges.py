@@ -316,6 +316,35 @@ def test_captured_steps_and_a_workspace_that_two_graphs_share(lib):
             ctx.close()
 
 
+def test_two_contexts_at_once(lib):
+    """Two contexts on streams of their own, without a wait between their calls: each has its own plan (in memory: more numbers than arguments hold),
+    workspace and results."""
+    import torch
+    H, KV, dh, B = 4, 2, 64, 400
+    cfg = synth.Config("two", L=1, D=H * dh, H=H, F=64, dtype="bf16", B=1, n0=4, strategies=[(0, 0)], seed=5)
+    state = []
+    for seed in (1, 2):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            ctx, g = hz.make_context(cfg)[0], gen(seed)
+            rows = [(q * seed) % 3 for q in range(B)]
+            off, capacity = offsets_of(rows), 320
+            qkv = normal(g, (off[-1], (H + 2 * KV) * dh), "bf16")
+            cache, (k, v) = packed_cache(lib, normal(g, (B, KV, capacity, dh), "bf16"), normal(g, (B, KV, capacity, dh), "bf16"))
+            lengths = [max(n, (q * 7 * seed) % capacity) for q, n in enumerate(rows)]
+            ws = torch.empty(ctx.otas_attention_recent_workspace_bytes(KV, off, lengths, 50, 3), dtype=torch.uint8, device="cuda")
+            state.append((stream, ctx, qkv, off, cache, lengths, ws, torch.empty((off[-1], H * dh), dtype=qkv.dtype, device="cuda"), k, v))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for stream, ctx, qkv, off, cache, lengths, ws, o, k, v in state:
+            with torch.cuda.stream(stream):
+                ctx.otas_attention_cache4(cache, qkv, off, list(range(B)), lengths, ws, o, 50, 3)
+    torch.cuda.synchronize()
+    for stream, ctx, qkv, off, cache, lengths, ws, o, k, v in state:
+        within(o, *plain.recent(qkv, H, k, v, off, range(B), lengths, 50, 3), "its own")
+        ctx.close()
+
+
 def test_rows_behind_the_last_entry_and_other_slots_stay(lib):
     """Neither attention writes anything but o and its workspace."""
     import torch
