@@ -128,7 +128,7 @@ inline int window_slots(int dtype, bool four, int rows) {
 // rows one tile), a launch more and its join where there are several parts.  A step is latency, or the bytes of all workgroups at
 // once.  In us, measured: 6 before the first step, 3.5 and a tenth for each part for the join; 1 a step (f32 1.5 at width 64, 3 at 128), 1.3 a tile of many rows (4 bits 2.3) and 1.7 times that
 // where two workgroups share a CU; 6.5 TB/s.  Shares counted from every query's own length: one token of 32 queries over 5700 .. 8192 entries of 8 key heads of 128
-// in 4 bits 46 us, where shares of the longest query's length in 768 / 256 parts had every third query's last part empty.
+// in 4 bits 48 us, where shares of the longest query's length in 768 / 256 parts had every third query's last part empty.
 inline WindowShape recent_shape(int dtype, bool four, int dh, int H, int KV, const int32_t* off, const int32_t* length, int B, int window, int sinks) {
   const int G = H / KV;
   int64_t most = 0;
