@@ -31,14 +31,11 @@ __device__ __forceinline__ void rows_begin(FloatRows<T, DT>& r, const T* q, int 
   r.l = 0.f;
 }
 
-// No instruction: a value that the compiler then forms where it is used.  From offsets that it knows to be the same in every
-// iteration it forms the 64-bit addresses of all loads ahead of the loop, 60 registers a lane.
-__device__ __forceinline__ void keep_here(uint32_t& x) { asm volatile("" : "+v"(x)); }
-
 // keys: kp, vp the first key's head, ld elements between keys, end their number; logits(s, kb), in place, of the
 // products of a block (in units of ln 2, -inf where the lane's row does not see the key); sees(j); partial(kb) whether block kb
 // has a pair that does not see each other.  Values are asked for when the first products are under way: one set of registers does
-// for keys and values.  Three waves fit a SIMD at widths up to 64 and two beyond, which is what the loop lives on: it waits for L2, then
+// for keys and values.  From offsets that the compiler knows to be the same in every iteration it forms the 64-bit addresses of all loads ahead of
+// the loop, 60 registers a lane: keep_here.  Three waves fit a SIMD at widths up to 64 and two beyond, which is what the loop lives on: it waits for L2, then
 // for the matrix cores (fp32, 2 queries of 1500 with 12 heads of 64: 94 -> 83 us from two waves to three; 16 heads of 128: 269 ->
 // 215 us from one to two, 76 of 153 TFLOP/s).
 template <typename T, int DT, class Keys>

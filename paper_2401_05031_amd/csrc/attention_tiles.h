@@ -297,7 +297,7 @@ struct CapArgs {
 };
 
 // Products into capped logits, in units of ln 2, where slopes or masks come between them and the weights: by the polynomial if all
-// of the wave's are small enough, keys that no row sees among them.
+// of the wave's are small enough, those of keys that no row sees among them where the caller has not taken them out.
 template <int CAP, int NB> __device__ __forceinline__ void tile_capped(floatx16 (&s)[NB], const Score2& score, const CapArgs& cap) {
   float most = 0.f;   // NaN is passed over here and stays one in either form
 #pragma unroll

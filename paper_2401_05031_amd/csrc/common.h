@@ -47,6 +47,9 @@ template <typename T> __device__ inline T from_float(float x);
 template <> __device__ inline float from_float<float>(float x) { return x; }
 template <> __device__ inline bf16_t from_float<bf16_t>(float x) { return (bf16_t)x; }
 
+// No instruction: a value that the compiler takes for another one behind it, so that what hangs on it is formed there, where it is used.
+__device__ __forceinline__ void keep_here(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
 // Exchanges between the lanes of a wave in registers.  A __shfl is a round trip through the LDS pipe (over 100 clocks),
 // and the reductions below are chains of them that nothing covers; these take a VALU instruction each.  All 64 lanes active.
 // Same bits; ViT-B pass of one query with r = 16 540 -> 529 us, of 64 1.992 -> 1.974 ms (MI355X).
