@@ -507,7 +507,10 @@ class Context:
         T, W = len(qkv), (self.H + 2 * kv_heads) * (self.D // self.H)
         return T, W, self._need("qkv", qkv, (T, W), self.torch_dtype)
 
+    # The two kinds of cache have descriptions of one size, so that the library could not tell one from the other.
     def _need_cache(self, cache) -> int:
+        if not isinstance(cache, KVCache):
+            raise ValueError(f"cache: want a KVCache, got {type(cache).__name__}")
         if cache.dtype != self.torch_dtype or cache.head_width != self.D // self.H or cache.device_index != self.device_index:
             raise ValueError(f"cache: want {self.torch_dtype}, head width {self.D // self.H} on GPU {self.device_index}, got "
                              f"{cache.dtype}, {cache.head_width} on GPU {cache.device_index}")
@@ -652,6 +655,8 @@ class Context:
         self._attention_last("otas_attention_cache4", self._need_cache4(cache), cache, qkv, offsets, slots, lengths, workspace, o, window, sinks, score)
 
     def _need_cache4(self, cache) -> int:
+        if not isinstance(cache, KVCache4):
+            raise ValueError(f"cache: want a KVCache4, got {type(cache).__name__}")
         if cache.head_width != self.D // self.H or cache.device_index != self.device_index:
             raise ValueError(f"cache: want head width {self.D // self.H} on GPU {self.device_index}, got {cache.head_width} on GPU {cache.device_index}")
         return cache.address
