@@ -520,8 +520,8 @@ class Context:
         import torch
         if score is None:
             return None
-        if score.slopes is not None:
-            self._need("score.slopes", score.slopes, (self.H,), torch.float32)
+        slopes = score.slopes   # what is checked is what the library gets, also where it was assigned after the description was made
+        score.desc.slopes = None if slopes is None else self._need("score.slopes", slopes, (self.H,), torch.float32)
         return score.address
 
     def _need_workspace(self, workspace) -> Tuple[int, int]:
@@ -613,10 +613,10 @@ class Context:
         import torch
         T, W, at = self._need_rows(qkv, kv_heads)
         to = at if out is qkv else self._need("out", out, (T, W), self.torch_dtype)
-        dh = self.D // self.H
-        for name, gain, heads in (("norm.q_gain", norm.q_gain, self.H), ("norm.k_gain", norm.k_gain, kv_heads)):
-            if gain is not None:
-                self._need(name, gain, (heads, dh) if norm.per_head else (dh,), self.torch_dtype)
+        d, dh, q_gain, k_gain, per_head = norm.desc, self.D // self.H, norm.q_gain, norm.k_gain, norm.per_head   # as in _need_score
+        d.q_gain = None if q_gain is None else self._need("norm.q_gain", q_gain, (self.H, dh) if per_head else (dh,), self.torch_dtype)
+        d.k_gain = None if k_gain is None else self._need("norm.k_gain", k_gain, (kv_heads, dh) if per_head else (dh,), self.torch_dtype)
+        d.per_head = 1 if per_head else 0
         _check(self._lib.otas_norm_rotary(self._h, at, T, kv_heads, norm.address,
                                           None if positions is None else self._need("positions", positions, (T,), torch.int32), rope.address, to),
                "otas_norm_rotary")

@@ -61,3 +61,77 @@ def test_a_cache_of_the_other_kind_is_refused(four):
         for call in calls(ctx, c, four):
             with pytest.raises(ValueError, match="cache"):
                 call()
+
+
+class Tensor:
+    """As much of a tensor as the binding looks at."""
+
+    def __init__(self, address, shape, dtype=torch.bfloat16, device=0):
+        self.address, self.shape, self.dtype, self.device = address, torch.Size(shape), dtype, device
+
+    def data_ptr(self):
+        return self.address
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return True
+
+    def __len__(self):
+        return self.shape[0]
+
+
+class Recorder:
+    """A library that keeps the arguments of its last call and returns success."""
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.last = name, args
+            return 0
+        return call
+
+
+def recording():
+    ctx = context()
+    del ctx._need
+    ctx._lib = Recorder()
+    return ctx, Tensor(4096, (3, (H + 2 * KV) * DH)), Tensor(1 << 20, (3,), torch.int32)
+
+
+def described(kind, address):
+    return kind.from_address(address)
+
+
+def test_the_gains_that_a_call_checks_are_those_that_it_passes():
+    """Tensors assigned to a description after it was made."""
+    ctx, qkv, pos = recording()
+    norm, rope = binding.HeadNorm(Tensor(1 << 24, (DH,)), Tensor(2 << 24, (DH,))), binding.Rotary(DH)
+
+    def passed():
+        ctx.otas_norm_rotary(qkv, KV, norm, pos, rope, qkv)
+        name, args = ctx._lib.last
+        d = described(binding._HeadNormDesc, args[4])
+        return d.q_gain, d.k_gain, d.eps, d.center, d.per_head
+    first = passed()
+    assert first[:2] == (1 << 24, 2 << 24) and first[4] == 0
+    norm.q_gain, norm.k_gain, norm.per_head = Tensor(3 << 24, (H, DH)), None, True
+    assert passed() == (3 << 24, None, *first[2:4], 1)
+    norm.q_gain = Tensor(3 << 24, (DH,))
+    with pytest.raises(ValueError):
+        passed()
+
+
+def test_the_slopes_that_a_call_checks_are_those_that_it_passes():
+    ctx, qkv, _ = recording()
+    score, o = binding.Score(0.5, 2.0, Tensor(1 << 24, (H,), torch.float32)), Tensor(8192, (3, H * DH))
+
+    def passed():
+        ctx.otas_attention_window(qkv, KV, [0, 3], o, 5, 0, score)
+        name, args = ctx._lib.last
+        return described(binding._ScoreDesc, args[7]).slopes
+    assert passed() == 1 << 24
+    score.slopes = Tensor(2 << 24, (H,), torch.float32)
+    assert passed() == 2 << 24
+    score.slopes = None
+    assert passed() is None
