@@ -520,9 +520,17 @@ class Context:
         import torch
         if score is None:
             return None
+        if not isinstance(score, Score):
+            raise ValueError(f"score: want a Score, got {type(score).__name__}")
         slopes = score.slopes   # what is checked is what the library gets, also where it was assigned after the description was made
         score.desc.slopes = None if slopes is None else self._need("score.slopes", slopes, (self.H,), torch.float32)
         return score.address
+
+    @staticmethod
+    def _need_rope(rope) -> int:
+        if not isinstance(rope, Rotary):
+            raise ValueError(f"rope: want a Rotary, got {type(rope).__name__}")
+        return rope.address
 
     def _need_workspace(self, workspace) -> Tuple[int, int]:
         import torch
@@ -534,7 +542,7 @@ class Context:
         import torch
         T, W, at = self._need_rows(qkv, kv_heads)
         to = at if out is qkv else self._need("out", out, (T, W), self.torch_dtype)
-        _check(self._lib.otas_rotary(self._h, at, T, kv_heads, self._need("positions", positions, (T,), torch.int32), rope.address, to),
+        _check(self._lib.otas_rotary(self._h, at, T, kv_heads, self._need("positions", positions, (T,), torch.int32), self._need_rope(rope), to),
                "otas_rotary")
 
     def otas_attention_masked(self, qkv, kv_heads, offsets, o, causal=True, prefix=None, documents=None, positions=None,
@@ -613,12 +621,14 @@ class Context:
         import torch
         T, W, at = self._need_rows(qkv, kv_heads)
         to = at if out is qkv else self._need("out", out, (T, W), self.torch_dtype)
+        if not isinstance(norm, HeadNorm):
+            raise ValueError(f"norm: want a HeadNorm, got {type(norm).__name__}")
         d, dh, q_gain, k_gain, per_head = norm.desc, self.D // self.H, norm.q_gain, norm.k_gain, norm.per_head   # as in _need_score
         d.q_gain = None if q_gain is None else self._need("norm.q_gain", q_gain, (self.H, dh) if per_head else (dh,), self.torch_dtype)
         d.k_gain = None if k_gain is None else self._need("norm.k_gain", k_gain, (kv_heads, dh) if per_head else (dh,), self.torch_dtype)
         d.per_head = 1 if per_head else 0
         _check(self._lib.otas_norm_rotary(self._h, at, T, kv_heads, norm.address,
-                                          None if positions is None else self._need("positions", positions, (T,), torch.int32), rope.address, to),
+                                          None if positions is None else self._need("positions", positions, (T,), torch.int32), self._need_rope(rope), to),
                "otas_norm_rotary")
 
     def otas_attention_window(self, qkv, kv_heads, offsets, o, window, sinks=0, score=None) -> None:

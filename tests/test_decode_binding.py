@@ -84,6 +84,7 @@ class Tensor:
 
 class Recorder:
     """A library that keeps the arguments of its last call and returns success."""
+    last = None
 
     def __getattr__(self, name):
         def call(*args):
@@ -135,3 +136,22 @@ def test_the_slopes_that_a_call_checks_are_those_that_it_passes():
     assert passed() == 2 << 24
     score.slopes = None
     assert passed() is None
+
+
+def test_a_description_of_another_kind_is_refused():
+    """The library reads as many bytes as the description that it expects has."""
+    ctx, qkv, pos = recording()
+    norm, rope, score, o = binding.HeadNorm(), binding.Rotary(DH), binding.Score(), Tensor(8192, (3, H * DH))
+    four = cache(binding.KVCache4)
+    for other in (norm, score, four, None):
+        with pytest.raises(ValueError, match="rope"):
+            ctx.otas_rotary(qkv, KV, pos, other, qkv)
+        with pytest.raises(ValueError, match="rope"):
+            ctx.otas_norm_rotary(qkv, KV, norm, pos, other, qkv)
+    for other in (rope, score, four, None):
+        with pytest.raises(ValueError, match="norm"):
+            ctx.otas_norm_rotary(qkv, KV, other, pos, rope, qkv)
+    for other in (rope, norm, four):
+        with pytest.raises(ValueError, match="score"):
+            ctx.otas_attention_window(qkv, KV, [0, 3], o, 5, 0, other)
+    assert ctx._lib.last is None
