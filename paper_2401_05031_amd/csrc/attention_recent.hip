@@ -566,7 +566,7 @@ __global__ __launch_bounds__(256) void attention_recent_join_kernel(PlanAny plan
   const int64_t first = SHARED ? blockIdx.x : ((int64_t)blockIdx.x * 4 + wave) * ROWS;
   if (first >= in.TH) return;
   int parts[ROWS], most = 0;
-  int token = (int)first / H, head = (int)first - token * H, of_key = head % G;   // TH is below 2^26
+  int token = (int)first / H, head = (int)first - token * H, of_key = head % G;   // TH is below 2^24
   int lo = 0;   // the query of the first row, then of the next
   {
     int hi = B;
@@ -695,7 +695,8 @@ hipError_t launch_attention_recent(int dtype, bool four, const Cache4Ref& c, con
   if (T <= 0) return hipSuccess;
   const int64_t TH = T * H;
   const int64_t wgs = shape.workgroups(plan, B, c.KV);
-  if (wgs > kMostGroups || (TH + 3) / 4 > kMostGroups) return kTooManyGroups;
+  // The join counts rows in 32 bits, and has no more workgroups than there are rows.
+  if (wgs > kMostGroups || (shape.parts > 1 && TH > kMostGroups)) return kTooManyGroups;
   const PlanAny p = plan_any(plan, count, d_plan);
   const RecentBuffers buf{workspace + recent_sums_at(shape, TH), workspace, TH};
   hipError_t e;
