@@ -183,6 +183,7 @@ otas_status otas_attention_recent(otas_ctx* c, const otas_kv_cache* cache, const
     if (offsets[B] > 0 && (!qkv || !workspace || !o)) return OTAS_EINVAL;
     const otas_status st = cache_ok(c, cache);
     if (st != OTAS_OK) return st;
+    if (in_cache(c, cache, qkv, qkv_bytes(c, offsets[B], cache->kv_heads))) return OTAS_EINVAL;
     const Cache4Ref ref{(char*)cache->k, (char*)cache->v, nullptr, nullptr, cache->capacity, cache->kv_heads, c->desc.D / c->desc.H, 0};
     return attention_last(c, ref, false, cache->slots, qkv, offsets, slot, length, B, window, sinks, score, workspace, workspace_bytes, o,
                           [&](const void* p, size_t bytes) { return !in_cache(c, cache, p, bytes); });
