@@ -156,7 +156,7 @@ otas_status otas_attention_tree(otas_ctx* c, const otas_kv_cache* cache, const v
     if (T > 0 && workspace_bytes < floats * sizeof(float)) return OTAS_ENOMEM;
     const size_t in_bytes = qkv_bytes(c, T, cache->kv_heads), out_bytes = rows_bytes(c, T);
     if (overlap(qkv, in_bytes, o, out_bytes) || overlap(workspace, floats * sizeof(float), o, out_bytes) ||
-        overlap(workspace, floats * sizeof(float), qkv, in_bytes) || in_cache(c, cache, o, out_bytes) ||
+        overlap(workspace, floats * sizeof(float), qkv, in_bytes) || in_cache(c, cache, qkv, in_bytes) || in_cache(c, cache, o, out_bytes) ||
         in_cache(c, cache, workspace, floats * sizeof(float)))
       return OTAS_EINVAL;
     std::vector<int32_t> plan(3 * (size_t)B + 1 + (chains ? 0 : (size_t)(T + 3) / 4), 0);

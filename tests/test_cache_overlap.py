@@ -22,6 +22,6 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("which", ["last tokens"])
+@pytest.mark.parametrize("which", ["last tokens", "tree"])
 def test_rows_within_a_cache_are_refused(program, which):
     assert "cache overlap ok" in _run(program, which)
