@@ -58,7 +58,7 @@ inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 // Whether [a, a + bytes) and [b, b + more) have a byte in common.
 inline bool overlap(const void* a, size_t bytes, const void* b, size_t more) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + more && y < x + bytes;
+  return bytes > 0 && more > 0 && x < y + more && y < x + bytes;
 }
 
 inline size_t qkv_bytes(const otas_ctx* c, int64_t T, int kv) {

@@ -55,7 +55,7 @@ int main(int, char** argv) {
         IS(OTAS_EINVAL, call(which, in - 8 * row + 16, off, 3, o));        // its last bytes
         IS(OTAS_OK, call(which, in - 8 * row, off, 3, o));                 // right before it
         IS(OTAS_EINVAL, call(which, qkv, off, 3, in));
-        IS(OTAS_OK, call(which, in, empty, 1, nullptr));                   // no rows, no bytes
+        for (int at : {0, 4096}) IS(OTAS_OK, call(which, in + at, empty, 1, in + 2 * at));   // no rows, no bytes
       }
     }
     CHECK(otas_destroy(c) == OTAS_OK);
