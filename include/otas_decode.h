@@ -18,6 +18,9 @@
  *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, 2^26 of otas_norm_rotary, 2^24 of
  *     otas_cache_append, attention over very many queries of which one is very long (all are given as many workgroups as the longest).
  *     otas_cache_evict has a limit of its own.
+ *   - Attention adds up weighted values in float before it divides by the weights' sum, and weights may be up to 2^8 there.  Finite
+ *     values of a row's keys beyond 1e30 are not for these entry points: up to there no sum of 2^20 of them passes the largest
+ *     float, beyond it o may be infinite or NaN although the mean is a float.  (A cache in 4 bits holds, and reads, up to 6 2^125.)
  *   - Results do not depend on the order in which the device happens to run anything.
  */
 #ifndef OTAS_DECODE_H_

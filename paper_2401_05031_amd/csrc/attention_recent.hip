@@ -387,7 +387,7 @@ __global__ __launch_bounds__(256, R == 1 ? (FOUR && sizeof(T) == 2 ? 3 : 2) : 1)
           }
       }
       float mx = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])), fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3])));
-      if (__any(mx * last_factor > m[r] + 8.f)) {   // a weight may be up to 2^8: no accuracy is lost in a floating format
+      if (__any(mx * last_factor > m[r] + 8.f)) {   // a weight may be up to 2^8: no accuracy is lost in a floating format, and of its range 2^8
         const float top = fmaxf(m[r], xor16_max(xor32_max(mx)) * last_factor);
         const float alpha = m[r] == top ? 1.f : __builtin_amdgcn_exp2f(m[r] - top);   // equal: also where both are -inf
         m[r] = top;

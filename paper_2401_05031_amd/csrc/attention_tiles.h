@@ -318,7 +318,7 @@ template <int CAP, int NB> __device__ __forceinline__ void tile_capped(floatx16 
 }
 
 // The sums are rescaled only when a maximum has grown by more than 8 (a weight may be up to 2^8 then: no accuracy is lost in a
-// floating format).
+// floating format; of its range 2^8 is, so that 2^20 values of 1e30, what the header takes, still have a sum).
 template <int DH>
 __device__ __forceinline__ void raise_top(WaveRows<DH>& w, float mx) {
   if (__any(mx > w.m + 8.f)) {
