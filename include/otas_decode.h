@@ -15,9 +15,11 @@
  *     entry point says how many it has), else through the context's plan buffer.  Calls of the first kind may be captured into a
  *     HIP graph (their host numbers are part of it); of the second kind they are refused under capture (EUNSUPPORTED), and
  *     limited to 1048576 entries (ENOMEM).
- *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, 2^26 of otas_norm_rotary, 2^24 of
- *     otas_cache_append, attention over very many queries of which one is very long (all are given as many workgroups as the longest).
- *     otas_cache_evict has a limit of its own.
+ *   - A call whose launch would have 2^24 workgroups or more is refused (EUNSUPPORTED): 2^27 rows of otas_rotary, 2^26 of otas_norm_rotary,
+ *     attention over very many queries of which one is very long.  (otas_attention_masked and otas_attention_tree give all queries as many
+ *     workgroups as the longest; the attentions with a window do so where three quarters of those have rows, or where their host
+ *     numbers leave no room for B + 1 more, with which they count the queries' workgroups one by one.)  2^24 rows of otas_cache_append, otas_cache4_append or otas_cache4_read are
+ *     refused too, and otas_cache_evict has a limit of its own.
  *   - Attention adds up weighted values in float before it divides by the weights' sum, and weights may be up to 2^8 there.  Finite
  *     values of a row's keys beyond 1e30 are not for these entry points: up to there no sum of 2^20 of them passes the largest
  *     float, beyond it o may be infinite or NaN although the mean is a float.  (A cache in 4 bits holds, and reads, up to 6 2^125.)
@@ -67,6 +69,8 @@ otas_status otas_rotary(otas_ctx *ctx, const void *qkv, int64_t T, int32_t kv_he
 typedef struct {
   float scale;          /* finite; 0 = 1 / sqrt(d_h) */
   float cap;            /* finite, >= 0; 0 = none.  For the cap a bf16 logit is off by up to 1e-6 cap, or 4e-6 of itself where cap > 256.
+                         * Which of two forms of that accuracy a row's logits take hangs on those of the rows that are worked on with it, and in
+                         * otas_attention_masked also on keys of theirs that no row sees.
                          * scale / cap up to 1e38 (EINVAL) */
   const float *slopes;  /* dev [H] or NULL */
 } otas_score_desc;
@@ -163,9 +167,11 @@ otas_status otas_norm_rotary(otas_ctx *ctx, const void *qkv, int64_t T, int32_t 
 
 /* Attention over packed rows through a sliding window, with first tokens that stay visible: row i of a query sees row j of it where
  *   j <= i  and  (i - j < window or j < sinks)                                         (i, j counted within the query),
- * so at least itself.  window >= 1 (EINVAL), INT32_MAX or anything past the longest query: all rows before it;  sinks >= 0.
+ * so at least itself.  window >= 1 (EINVAL), INT32_MAX or anything past the longest query: all rows before it (for which
+ * otas_attention_masked with its defaults is the faster call, by 4 to 10 %);  sinks >= 0.
  * score, o, what infinities and NaN in rows that are not seen do (nothing), lengths as in otas_attention_masked; the distance for slopes is
- * i - j.  Keys outside window and sinks are not read.  Host numbers: B + 1. */
+ * i - j.  Keys that no row of a workgroup sees are read only where they share a tile, of 32 or 64 keys, with one that some row does.
+ * rows of a query (H / kv_heads) < 2^30 (EUNSUPPORTED).  Host numbers: B + 1. */
 otas_status otas_attention_window(otas_ctx *ctx, const void *qkv, int32_t kv_heads, const int32_t *offsets, int32_t B,
                                   int32_t window, int32_t sinks, const otas_score_desc *score, void *o);
 
