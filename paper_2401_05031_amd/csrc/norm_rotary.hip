@@ -10,7 +10,7 @@
 namespace otas {
 
 template <int L> __device__ __forceinline__ float lanes_sum(float v) {   // over every L lanes; all 64 active
-  if (L >= 64) v = xor32_sum(v);
+  static_assert(L <= 32, "128 elements, four and more a lane");
   if (L >= 32) v = xor16_sum(v);
   if (L >= 16) {   // a rotation by half of the period that the values have reached is the butterfly's partner
     v = dpp_sum<dpp_ror(8)>(v);

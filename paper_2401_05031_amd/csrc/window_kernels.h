@@ -195,9 +195,8 @@ hipError_t launch_attention_rows_bf16(bool four, const Cache4Ref& c, const void*
 // Packed rows: one share of all tiles.  Of fp32 products a workgroup has 32 rows of one head of `heads` H, else 128 of one of KV key heads.
 inline WindowShape packed_shape(int dtype, int dh, int H, int KV, int max_n, int window, int sinks) {
   const bool many = dtype != 0 && bf16_width(dh);
-  WindowShape t{window, sinks, many ? kRowsShift : kRecentShift, many ? kManyRows : 32, 0, 0, 1, 1, 0};
+  WindowShape t{window, sinks, many ? kRowsShift : kRecentShift, many ? kManyRows : 32, 0, 1, 1, 1, 0};   // `each` is not looked at
   t.groups = (int)(((int64_t)max_n * (many ? H / KV : 1) + t.rows - 1) / t.rows);
-  t.each = std::max(1, window_tiles(t.shift, 0, max_n - 1, window, sinks).count);   // all that a group can see
   return t;
 }
 // plan: off [B+1], then what the shape has counted
