@@ -7,8 +7,9 @@
 //   Keys of the model's dtype travel from global memory straight into LDS.  Keys in 4 bits are asked for a tile ahead, 16 bytes of a
 // group a thread, and written to LDS as bf16, which holds them exactly, beneath the products of the tile before.
 //   Products, exponentials and a start and end of 10 us or more that all workgroups of a round have at once add up: 8192 rows, 16 heads on 2 of 128, window
-// 1024: 97.5 us, 660 TFLOP/s of 64.7 GFLOP (matrix cores busy for 39 % of it, the vector ALU for 48 %); 12 x 600 .. 1500 rows, 12 heads on 4 of 64, window 300, capped:
-// 45 us; 4 x 256 rows over 2291 .. 4000 entries in 4 bits, 16 heads on 2 of 128, capped: 42 us and the join of its four parts 10.
+// 1024: 88 us, 735 TFLOP/s of 64.7 GFLOP (matrix cores busy for 39 % of it, the vector ALU for 46 %); 12 x 600 .. 1500 rows, 12 heads on 4 of 64, window 300, capped:
+// 42 us; 4 x 256 rows over 2291 .. 4000 entries in 4 bits, 16 heads on 2 of 128, capped: 39 us and the join of its four parts 10.  (After some hundred launches in
+// a row; the first twenty take 97, 46 and 42.)
 #include "attention_tiles.h"
 #include "cache4.h"
 
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void attention_rows_bf16_kernel(PlanAny pla
       if (CAP && !BIAS && whole) done = tile_weights_capped<DH, NB>(w, s, cap);
       const int behind = place - from - 4 * fk;   // the row's distance from the lane's first key
       // Which keys the row sees, a bit each: two operations an element to take the others out, where comparisons are three and more (8192 rows, window
-      // 1024, width 128: 99.5 -> 97.9 us).
+      // 1024, width 128, first launches: 99.5 -> 97.9 us).
       uint32_t seen[NB];
       if (!whole) {
 #pragma unroll

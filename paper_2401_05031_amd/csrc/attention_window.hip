@@ -1,7 +1,8 @@
 // otas_attention_window with fp32 products (f32 models, and bf16 ones of head widths that attention_rows_bf16.hip is not built for):
 // row i sees row j of its query where j <= i and (i - j < window or j < sinks).  As attention_masked_f32_kernel, over the blocks of
 // 32 keys that any of a workgroup's 32 rows sees: first those of the sinks before its window, then the window's.  Bound by a workgroup's chain of
-// latencies: 3 x 182 .. 260 float rows, 12 heads on 4 of 64, window 64: 12 us.
+// latencies (launch, plan, queries, one block a wave, join: 8 us for 36 workgroups of one row each) and by how many workgroups go through it side by side:
+// 3 x 182 .. 260 float rows, 12 heads on 4 of 64, window 64, 324 workgroups of one to four blocks: 12 us, 144 of the same 9.
 #include "attention_rows_f32.h"
 #include "window_kernels.h"
 
